@@ -429,6 +429,70 @@ ptq_status ptq_lopro_linear_forward_static(const void* X, ptq_dtype xdt, int64_t
                                            int b_H, const uint8_t* U, const uint8_t* V, const uint16_t* sigma,
                                            int r, const double* s, float* O, int64_t ldo, ptq_stream stream);
 
+/* ---------------------------------------------------------------------------
+ * The 8-bit attention half of a decoder layer, as a quantized layer is served: tokens are put into 8 bits by the norm before
+ * a projection, projections multiply 8-bit codes, keys and values are quantized as they enter a paged cache, and attention
+ * reads them there.  Inference only.  Tokens of all sequences lie one after the other; cu_* are the b + 1 places where
+ * the sequences begin and the last one ends.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Root-mean-square norm of token rows, with the residual's addition, into 8-bit codes and a scale per token:
+ *
+ *   y = round(x + residual)        to the storage type; x itself without a residual
+ *   u = float32(y gamma)           (y without gamma),   A = max_j |u_j|
+ *   code_j = rne(127 u_j / A),     scale = A / 127 / sqrt(mean_j(y_j^2) + eps)     (normalize == 0: A / 127)
+ *
+ * so that scale code_j stands for the row's value; |code| <= 127.  A row of zeros has codes 0 and scale 0; a row with an
+ * infinity or a NaN (after the addition, or times gamma) has codes 0 and scale NaN.  Without gamma and with normalize == 0
+ * it puts any rows into 8 bits: those of a weight for ptq_int8_linear, or attention's output.
+ *
+ * X         t x n, PTQ_F32 or PTQ_BF16, ldx >= n.    residual  the same type and shape, ldr >= n, or NULL.
+ * residual_out  where y goes, ldo >= n, or NULL; may be X or residual.  Needs a residual.
+ * gamma     n values of the same type, or NULL.       eps  finite, >= 0.
+ * codes     t x n int8, ldc >= n, ldc % 16 == 0, 16-byte aligned.       scales  t float32.
+ * n <= 32768.  Codes are exact; the sum of squares is float64.  No workspace.
+ * Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE.
+ */
+ptq_status ptq_rmsnorm_quantize(const void* X, ptq_dtype dt, int64_t ldx, int64_t t, int64_t n, const void* residual,
+                                int64_t ldr, void* residual_out, int64_t ldo, const void* gamma, double eps, int normalize,
+                                int8_t* codes, int64_t ldc, float* scales, ptq_stream stream);
+
+/*
+ * Quantizes keys and values into a paged cache.  Row h of token i (d values) takes the grid of ptq_quantize_layer for itself,
+ *   lo = min(0, min x), hi = max(0, max x), (lo, hi) = (-1, 1) if the row is all zero,
+ *   scale = float32((hi - lo) / (2^bits - 1)), zero = rne(-lo / scale), code = clamp(rne(x / scale) + zero, 0, 2^bits - 1)
+ * and stands for scale (code - zero).  A row with an infinity or a NaN has scale NaN; so has whatever it is read into.
+ * (Values so small that the scale is no float32 count as zeros.)
+ *
+ * K, V      token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_F32 / PTQ_BF16.
+ * slots     t int32: page * page size + place in the page.  A slot outside [0, pages * page) is not written (padding).
+ *           Slots of one call are different from each other.
+ * bits      8 or 4.   8: a byte per code.   4: eight codes make a little-endian 32-bit word, code 2 i of them in bits 4 i
+ *           and code 2 i + 1 in bits 16 + 4 i.
+ * codes     [2][pages][hkv][page][d bits / 8] bytes, 16-byte aligned: all keys, then all values.
+ * scales, zeros   [2][pages][hkv][page] float32 and bytes.
+ * page      tokens per page, a power of two up to 256; pages * page < 2^31.    d  a multiple of 16, at most 256.
+ * hkv <= 32767.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE.
+ */
+ptq_status ptq_kv_cache_write(const void* K, int64_t k_token, int64_t k_head, const void* V, int64_t v_token, int64_t v_head,
+                              ptq_dtype dt, int64_t t, int64_t hkv, int64_t d, const int32_t* slots, int bits, uint8_t* codes,
+                              float* scales, uint8_t* zeros, int64_t pages, int64_t page, ptq_stream stream);
+
+/*
+ * Reads sequences back out of the cache: row i of sequence s, 0 <= i < cu_kv[s + 1] - cu_kv[s], comes from place i % page of page
+ * table[s][i / page] and goes to row cu_kv[s] + i of K and V.
+ *
+ * table     b x ldt int32 page numbers, row by row.  A number outside [0, pages), or a page past ldt, reads as zeros.
+ * cu_kv     b + 1 int32 on the device.  A sequence that would begin before row 0 or end past `rows` is left out.
+ * max_kv    no sequence is longer (rows from there on are left out).      b <= 65535.
+ * K, V      rows of PTQ_F32 / PTQ_BF16, strides as above.
+ */
+ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const uint8_t* zeros, int64_t pages, int64_t page,
+                             int64_t hkv, int64_t d, int bits, const int32_t* table, int64_t ldt, int64_t b, const int32_t* cu_kv,
+                             int64_t rows, int64_t max_kv, void* K, int64_t k_token, int64_t k_head, void* V, int64_t v_token,
+                             int64_t v_head, ptq_dtype dt, ptq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -89,6 +89,13 @@ def load_library() -> ctypes.CDLL:
     lib.ptq_scaled_r1svd.restype = c.c_int
     lib.ptq_scaled_r1svd.argtypes = [vp, c.c_int, i64, i64, i64, vp, vp, i64, c.c_int, c.c_int, vp, vp, vp, vp,
                                      i64, vp, sz, vp]
+    lib.ptq_rmsnorm_quantize.restype = c.c_int
+    lib.ptq_rmsnorm_quantize.argtypes = [vp, c.c_int, i64, i64, i64, vp, i64, vp, i64, vp, c.c_double, c.c_int, vp, i64, vp, vp]
+    lib.ptq_kv_cache_write.restype = c.c_int
+    lib.ptq_kv_cache_write.argtypes = [vp, i64, i64, vp, i64, i64, c.c_int, i64, i64, i64, vp, c.c_int, vp, vp, vp, i64, i64, vp]
+    lib.ptq_kv_cache_read.restype = c.c_int
+    lib.ptq_kv_cache_read.argtypes = [vp, vp, vp, i64, i64, i64, i64, c.c_int, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64,
+                                      i64, c.c_int, vp]
     _LIB = lib
     return lib
 
@@ -424,3 +431,66 @@ def ptq_lopro_linear_forward_static(X, packed, bits, scales_t, zeros_t, group, p
 
 def ptq_lopro_linear_forward_static_limit() -> int:
     return int(load_library().ptq_lopro_linear_forward_static_limit())
+
+
+def ptq_rmsnorm_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, gamma: torch.Tensor | None = None,
+                         residual: torch.Tensor | None = None, residual_out: torch.Tensor | None = None, eps: float = 1e-5,
+                         normalize: bool = True) -> None:
+    """codes (int8 t x n), scales (float32 t) <- the norm of X + residual (t x n, bfloat16 or float32) times gamma;
+    residual_out <- X + residual.  normalize=False: the rows as they are."""
+    _check_dev(X, codes, scales, gamma, residual, residual_out)
+    t, n = X.shape
+    assert X.stride(1) == 1 and codes.dtype == torch.int8 and codes.shape == (t, n) and codes.stride(1) == 1
+    assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.numel() == t
+    assert gamma is None or (gamma.dtype == X.dtype and gamma.is_contiguous() and gamma.shape == (n,))
+    for r in (residual, residual_out):
+        assert r is None or (r.dtype == X.dtype and r.shape == (t, n) and r.stride(1) == 1)
+    rc = load_library().ptq_rmsnorm_quantize(X.data_ptr(), _dtype_code(X), X.stride(0), t, n, _ptr(residual),
+                                             0 if residual is None else residual.stride(0), _ptr(residual_out),
+                                             0 if residual_out is None else residual_out.stride(0), _ptr(gamma), float(eps),
+                                             int(bool(normalize)), codes.data_ptr(), codes.stride(0), scales.data_ptr(), _stream())
+    if rc:
+        raise PtqError(rc, "ptq_rmsnorm_quantize")
+
+
+def _check_cache(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int, d: int) -> tuple[int, int, int]:
+    """(pages, heads, page) of a cache of rows of d values."""
+    assert codes.dtype == torch.uint8 and codes.is_contiguous() and codes.dim() == 5 and codes.shape[0] == 2
+    pages, hkv, page = codes.shape[1:4]
+    assert codes.shape[4] == d * bits // 8
+    assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.shape == (2, pages, hkv, page)
+    assert zeros.dtype == torch.uint8 and zeros.is_contiguous() and zeros.shape == (2, pages, hkv, page)
+    return pages, hkv, page
+
+
+def ptq_kv_cache_write(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, bits: int, codes: torch.Tensor,
+                       scales: torch.Tensor, zeros: torch.Tensor) -> None:
+    """Quantizes K and V (t x heads x d, bfloat16 or float32) into the cache rows that slots (int32 t) names."""
+    _check_dev(K, V, slots, codes, scales, zeros)
+    t, hkv, d = K.shape
+    pages, heads, page = _check_cache(codes, scales, zeros, bits, d)
+    assert heads == hkv and V.shape == K.shape and V.dtype == K.dtype and (K.stride(2) == 1 and V.stride(2) == 1)
+    assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == t
+    rc = load_library().ptq_kv_cache_write(K.data_ptr(), K.stride(0), K.stride(1), V.data_ptr(), V.stride(0), V.stride(1),
+                                           _dtype_code(K), t, hkv, d, slots.data_ptr(), bits, codes.data_ptr(),
+                                           scales.data_ptr(), zeros.data_ptr(), pages, page, _stream())
+    if rc:
+        raise PtqError(rc, "ptq_kv_cache_write")
+
+
+def ptq_kv_cache_read(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int, table: torch.Tensor,
+                      cu_kv: torch.Tensor, max_kv: int, K: torch.Tensor, V: torch.Tensor) -> None:
+    """K, V (rows x heads x d) <- the sequences whose pages table (int32 b x pages of a sequence) lists; sequence s is rows
+    cu_kv[s] .. cu_kv[s + 1] (int32, on the device), none longer than max_kv."""
+    _check_dev(codes, scales, zeros, table, cu_kv, K, V)
+    rows, hkv, d = K.shape
+    pages, heads, page = _check_cache(codes, scales, zeros, bits, d)
+    b = table.shape[0]
+    assert heads == hkv and V.shape == K.shape and V.dtype == K.dtype and (K.stride(2) == 1 and V.stride(2) == 1)
+    assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
+    assert cu_kv.dtype == torch.int32 and cu_kv.is_contiguous() and cu_kv.numel() == b + 1
+    rc = load_library().ptq_kv_cache_read(codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), pages, page, hkv, d, bits,
+                                          table.data_ptr(), table.shape[1], b, cu_kv.data_ptr(), rows, int(max_kv), K.data_ptr(),
+                                          K.stride(0), K.stride(1), V.data_ptr(), V.stride(0), V.stride(1), _dtype_code(K), _stream())
+    if rc:
+        raise PtqError(rc, "ptq_kv_cache_read")

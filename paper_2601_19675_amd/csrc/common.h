@@ -160,4 +160,17 @@ ptq_status linear_forward_launch(const void* X, ptq_dtype xdt, int64_t ldx, int6
                                  const uint8_t* V, const uint16_t* sigma, int r, const double* s, float* O,
                                  int64_t ldo, void* ws, hipStream_t st);
 
+
+int64_t rmsnorm_max_columns();
+ptq_status rmsnorm_quantize_launch(const void* X, ptq_dtype dt, int64_t ldx, int64_t t, int64_t n, const void* residual,
+                                   int64_t ldr, void* residual_out, int64_t ldo, const void* gamma, double eps, int normalize,
+                                   int8_t* codes, int64_t ldc, float* scales, hipStream_t s);
+ptq_status kv_cache_write_launch(const void* K, int64_t k_token, int64_t k_head, const void* V, int64_t v_token,
+                                 int64_t v_head, ptq_dtype dt, int64_t t, int hkv, int d, const int32_t* slots, int bits,
+                                 uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int page, hipStream_t s);
+ptq_status kv_cache_read_launch(const uint8_t* codes, const float* scales, const uint8_t* zeros, int64_t pages, int page,
+                                int hkv, int d, int bits, const int32_t* table, int64_t ldt, int64_t b, const int32_t* cu_kv,
+                                int64_t rows, int64_t max_kv, void* K, int64_t k_token, int64_t k_head, void* V,
+                                int64_t v_token, int64_t v_head, ptq_dtype dt, hipStream_t s);
+
 }  // namespace ptq

@@ -17,6 +17,13 @@ bool rotation_shape_bad(int64_t n, int b_I, int b_H) {
   if (b_I < 0 || b_I > n || b_I % 4 != 0 || n % 4 != 0) return true;
   return (n - b_I) % b_H != 0;
 }
+// what the cache's calls ask of its layout
+ptq_status kv_cache_bad(int64_t hkv, int64_t d, int bits, int64_t pages, int64_t page) {
+  if (bits != 8 && bits != 4) return PTQ_ERR_ARG;
+  if (hkv <= 0 || hkv > 32767 || d <= 0 || d > 256 || d % 16 != 0) return PTQ_ERR_SHAPE;
+  if (page <= 0 || page > 256 || (page & (page - 1)) != 0 || pages < 0 || pages > INT32_MAX / page) return PTQ_ERR_SHAPE;
+  return PTQ_OK;
+}
 }  // namespace
 
 extern "C" {
@@ -309,6 +316,50 @@ ptq_status ptq_lopro_linear_forward_static(const void* X, ptq_dtype xdt, int64_t
   if (sc != PTQ_OK) return sc;
   return linear_forward_launch(X, xdt, ldx, tokens, m, n, packed, bits, scales, zeros, group, perm, b_I, b_H, U, V,
                                sigma, r, s, O, ldo, ws, static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_rmsnorm_quantize(const void* X, ptq_dtype dt, int64_t ldx, int64_t t, int64_t n, const void* residual,
+                                int64_t ldr, void* residual_out, int64_t ldo, const void* gamma, double eps, int normalize,
+                                int8_t* codes, int64_t ldc, float* scales, ptq_stream stream) {
+  if (dt != PTQ_F32 && dt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  if (!(eps >= 0.0) || !std::isfinite(eps)) return PTQ_ERR_ARG;
+  if (t < 0 || n < 0 || n > rmsnorm_max_columns() || t > INT32_MAX / 2 || ldx < n || ldc < n || ldc % 16 != 0) return PTQ_ERR_SHAPE;
+  if ((residual && ldr < n) || (residual_out && ldo < n)) return PTQ_ERR_SHAPE;
+  if (residual_out && !residual) return PTQ_ERR_ARG;
+  if (t == 0 || n == 0) return PTQ_OK;
+  if (!X || !codes || !scales || misaligned(codes, 16)) return PTQ_ERR_ARG;
+  return rmsnorm_quantize_launch(X, dt, ldx, t, n, residual, ldr, residual_out, ldo, gamma, eps, normalize, codes, ldc, scales,
+                                 static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_kv_cache_write(const void* K, int64_t k_token, int64_t k_head, const void* V, int64_t v_token, int64_t v_head,
+                              ptq_dtype dt, int64_t t, int64_t hkv, int64_t d, const int32_t* slots, int bits, uint8_t* codes,
+                              float* scales, uint8_t* zeros, int64_t pages, int64_t page, ptq_stream stream) {
+  if (dt != PTQ_F32 && dt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  const ptq_status bad = kv_cache_bad(hkv, d, bits, pages, page);
+  if (bad != PTQ_OK) return bad;
+  if (t < 0 || t > INT32_MAX / 2 || k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return PTQ_ERR_SHAPE;
+  if (t == 0) return PTQ_OK;
+  if (!K || !V || !slots || !codes || !scales || !zeros || misaligned(codes, 16)) return PTQ_ERR_ARG;
+  return kv_cache_write_launch(K, k_token, k_head, V, v_token, v_head, dt, t, (int)hkv, (int)d, slots, bits, codes, scales, zeros,
+                               pages, (int)page, static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const uint8_t* zeros, int64_t pages, int64_t page,
+                             int64_t hkv, int64_t d, int bits, const int32_t* table, int64_t ldt, int64_t b, const int32_t* cu_kv,
+                             int64_t rows, int64_t max_kv, void* K, int64_t k_token, int64_t k_head, void* V, int64_t v_token,
+                             int64_t v_head, ptq_dtype dt, ptq_stream stream) {
+  if (dt != PTQ_F32 && dt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  const ptq_status bad = kv_cache_bad(hkv, d, bits, pages, page);
+  if (bad != PTQ_OK) return bad;
+  if (b < 0 || b > 65535 || ldt < 0 || rows < 0 || max_kv < 0 || max_kv > INT32_MAX / 2 || k_token < 0 || k_head < 0 || v_token < 0 ||
+      v_head < 0)
+    return PTQ_ERR_SHAPE;
+  if (b == 0 || rows == 0 || max_kv == 0) return PTQ_OK;
+  if (pages == 0) return PTQ_ERR_SHAPE;
+  if (!codes || !scales || !zeros || !table || !cu_kv || !K || !V || misaligned(codes, 16)) return PTQ_ERR_ARG;
+  return kv_cache_read_launch(codes, scales, zeros, pages, (int)page, (int)hkv, (int)d, bits, table, ldt, b, cu_kv, rows, max_kv, K,
+                              k_token, k_head, V, v_token, v_head, dt, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

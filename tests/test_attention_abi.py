@@ -1,0 +1,58 @@
+"""What the calls of the 8-bit attention path refuse, seen on the host (none of these reaches a launch)."""
+import os
+
+import pytest
+
+import paper_2601_19675_amd as ptq
+
+OK, ARG, SHAPE, DTYPE, WORKSPACE = 0, 1, 2, 3, 4
+P = 0x1000   # aligned, never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(ptq.lib_path()):
+        from paper_2601_19675_amd import build
+        build.build(verbose=False)
+    return ptq.load_library()
+
+
+def caller(fn, **defaults):
+    def call(**kw):
+        assert set(kw) <= set(defaults), kw
+        return fn(*[{**defaults, **kw}[k] for k in defaults])
+    return call
+
+
+def test_norm(lib):
+    call = caller(lib.ptq_rmsnorm_quantize, X=P, dt=1, ldx=64, t=4, n=64, residual=P, ldr=64, out=P, ldo=64, gamma=P, eps=1e-5,
+                  normalize=1, codes=P, ldc=64, scales=P, stream=None)
+    assert call(t=0) == OK and call(n=0) == OK
+    assert call(dt=2) == DTYPE and call(dt=7) == DTYPE
+    assert call(eps=-1.0) == ARG and call(eps=float("nan")) == ARG and call(eps=float("inf")) == ARG
+    assert call(X=None) == ARG and call(codes=None) == ARG and call(scales=None) == ARG and call(codes=P + 8) == ARG
+    assert call(residual=None) == ARG        # nowhere to take the sum from
+    assert call(t=-1) == SHAPE and call(n=-1) == SHAPE and call(n=32769, ldx=40000, ldc=40000, ldr=40000, ldo=40000) == SHAPE
+    assert call(ldx=63) == SHAPE and call(ldr=63) == SHAPE and call(ldo=63) == SHAPE and call(ldc=48) == SHAPE and call(ldc=72) == SHAPE
+
+
+def test_cache(lib):
+    write = caller(lib.ptq_kv_cache_write, K=P, kt=256, kh=64, V=P, vt=256, vh=64, dt=1, t=4, hkv=4, d=64, slots=P, bits=8, codes=P,
+                   scales=P, zeros=P, pages=8, page=16, stream=None)
+    read = caller(lib.ptq_kv_cache_read, codes=P, scales=P, zeros=P, pages=8, page=16, hkv=4, d=64, bits=8, table=P, ldt=2, b=2, cu=P,
+                  rows=40, max_kv=20, K=P, kt=256, kh=64, V=P, vt=256, vh=64, dt=1, stream=None)
+    assert write(t=0) == OK and read(b=0) == OK and read(rows=0) == OK and read(max_kv=0) == OK
+    for call in (write, read):
+        assert call(dt=2) == DTYPE and call(dt=-1) == DTYPE
+        assert call(bits=2) == ARG and call(bits=3) == ARG and call(bits=16) == ARG
+        assert call(d=0) == SHAPE and call(d=72) == SHAPE and call(d=272) == SHAPE
+        assert call(hkv=0) == SHAPE and call(hkv=32768) == SHAPE
+        assert call(page=0) == SHAPE and call(page=24) == SHAPE and call(page=512) == SHAPE
+        assert call(pages=-1) == SHAPE and call(pages=2 ** 31 // 16) == SHAPE
+        assert call(kt=-1) == SHAPE and call(vh=-1) == SHAPE
+        for name in ("K", "V", "codes", "scales", "zeros"):
+            assert call(**{name: None}) == ARG
+        assert call(codes=P + 8) == ARG
+    assert write(slots=None) == ARG and write(t=-1) == SHAPE
+    assert read(table=None) == ARG and read(cu=None) == ARG and read(pages=0) == SHAPE
+    assert read(b=65536) == SHAPE and read(ldt=-1) == SHAPE and read(rows=-1) == SHAPE and read(max_kv=-1) == SHAPE
