@@ -58,7 +58,8 @@ typedef enum {
   PTQ_OP_LOPRO_ROTATE_HESSIAN = 5,
   PTQ_OP_ACTIVATION_ABS_SUM = 6,
   PTQ_OP_SCALED_R1SVD = 7,
-  PTQ_OP_LINEAR_FORWARD = 8 /* t = tokens, block = rank r */
+  PTQ_OP_LINEAR_FORWARD = 8, /* t = tokens, block = rank r */
+  PTQ_OP_INT8_LINEAR = 10    /* t = tokens (9 is no operation) */
 } ptq_op;
 
 typedef void* ptq_stream; /* hipStream_t */
@@ -457,6 +458,21 @@ ptq_status ptq_lopro_linear_forward_static(const void* X, ptq_dtype xdt, int64_t
 ptq_status ptq_rmsnorm_quantize(const void* X, ptq_dtype dt, int64_t ldx, int64_t t, int64_t n, const void* residual,
                                 int64_t ldr, void* residual_out, int64_t ldo, const void* gamma, double eps, int normalize,
                                 int8_t* codes, int64_t ldc, float* scales, ptq_stream stream);
+
+/*
+ * 8-bit linear layer:   O[i][j] = (sum_k A[i][k] W[j][k]) a_scales[i] w_scales[j] + bias[j].
+ * Sums are exact 32-bit integers; the rest is float32 in that order, rounded once more where O is bfloat16.
+ *
+ * A   t x n int8 tokens (ptq_rmsnorm_quantize), lda >= n.     W   m x n int8, output channels by input channels, ldw >= n.
+ *     n, lda and ldw are multiples of 16, both 16-byte aligned; n <= 131056, lda and ldw <= 2^22.
+ * a_scales  t float32.   w_scales  m float32.   bias  m float32 or NULL.
+ * O   t x m, PTQ_F32 or PTQ_BF16, ldo >= m, element aligned.
+ * Workspace: PTQ_OP_INT8_LINEAR with m, n and t = tokens (may be 0 bytes: then NULL will do).
+ * Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE, PTQ_ERR_WORKSPACE.
+ */
+ptq_status ptq_int8_linear(const int8_t* A, int64_t lda, const float* a_scales, int64_t t, const int8_t* W, int64_t ldw,
+                           const float* w_scales, int64_t m, int64_t n, const float* bias, void* O, ptq_dtype odt, int64_t ldo,
+                           void* ws, size_t ws_bytes, ptq_stream stream);
 
 /*
  * Quantizes keys and values into a paged cache.  Row h of token i (d values) takes the grid of ptq_quantize_layer for itself,

@@ -17,6 +17,7 @@ PTQ_F32, PTQ_BF16, PTQ_F64 = 0, 1, 2
 OP_HESSIAN, OP_CHOLESKY_INV, OP_QUANTIZE, OP_LAYER_ERROR = 0, 1, 2, 3
 OP_LOPRO_ORDER, OP_LOPRO_ROTATE_HESSIAN = 4, 5
 OP_ACTIVATION_ABS_SUM, OP_SCALED_R1SVD, OP_LINEAR_FORWARD = 6, 7, 8
+OP_INT8_LINEAR = 10
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -91,6 +92,8 @@ def load_library() -> ctypes.CDLL:
                                      i64, vp, sz, vp]
     lib.ptq_rmsnorm_quantize.restype = c.c_int
     lib.ptq_rmsnorm_quantize.argtypes = [vp, c.c_int, i64, i64, i64, vp, i64, vp, i64, vp, c.c_double, c.c_int, vp, i64, vp, vp]
+    lib.ptq_int8_linear.restype = c.c_int
+    lib.ptq_int8_linear.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, vp, c.c_int, i64, vp, sz, vp]
     lib.ptq_kv_cache_write.restype = c.c_int
     lib.ptq_kv_cache_write.argtypes = [vp, i64, i64, vp, i64, i64, c.c_int, i64, i64, i64, vp, c.c_int, vp, vp, vp, i64, i64, vp]
     lib.ptq_kv_cache_read.restype = c.c_int
@@ -451,6 +454,27 @@ def ptq_rmsnorm_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
                                              int(bool(normalize)), codes.data_ptr(), codes.stride(0), scales.data_ptr(), _stream())
     if rc:
         raise PtqError(rc, "ptq_rmsnorm_quantize")
+
+
+def ptq_int8_linear(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, O: torch.Tensor,
+                    bias: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> None:
+    """O (bfloat16 or float32 t x m) <- (A W^T) a_scales w_scales + bias; A int8 t x n, W int8 m x n, the rest float32."""
+    _check_dev(A, a_scales, W, w_scales, O, bias)
+    t, n = A.shape
+    m = W.shape[0]
+    assert A.dtype == torch.int8 and A.stride(1) == 1 and W.dtype == torch.int8 and W.shape == (m, n) and W.stride(1) == 1
+    assert a_scales.dtype == torch.float32 and a_scales.is_contiguous() and a_scales.numel() == t
+    for c in (w_scales, bias):
+        assert c is None or (c.dtype == torch.float32 and c.is_contiguous() and c.numel() == m)
+    assert O.shape == (t, m) and O.stride(1) == 1
+    if ws is None:
+        need = ptq_workspace_bytes(OP_INT8_LINEAR, m, n, t)
+        ws = torch.empty(need, dtype=torch.uint8, device=A.device) if need else None
+    rc = load_library().ptq_int8_linear(A.data_ptr(), A.stride(0), a_scales.data_ptr(), t, W.data_ptr(), W.stride(0),
+                                        w_scales.data_ptr(), m, n, _ptr(bias), O.data_ptr(), _dtype_code(O), O.stride(0),
+                                        _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+    if rc:
+        raise PtqError(rc, "ptq_int8_linear")
 
 
 def _check_cache(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int, d: int) -> tuple[int, int, int]:

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libptq.so")
 PROBE_LIB = os.path.join(HERE, "libptq_probe.so")   # diagnostics for bench.py --mfma-control, not part of the product
-SOURCES = ["ptq_api.hip", "hessian.hip", "hessian_f32.hip", "cholesky.hip", "quantize.hip", "vq.hip", "layer_error.hip", "lopro.hip", "r1svd.hip", "r1svd_bf16.hip", "artifact.hip", "rmsnorm.hip", "kv_cache.hip"]
+SOURCES = ["ptq_api.hip", "hessian.hip", "hessian_f32.hip", "cholesky.hip", "quantize.hip", "vq.hip", "layer_error.hip", "lopro.hip", "r1svd.hip", "r1svd_bf16.hip", "artifact.hip", "rmsnorm.hip", "kv_cache.hip", "int8_linear.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
     # packed-FP32 instructions are kept out of every kernel
@@ -18,9 +18,9 @@ FLAGS = [
 ]
 # Accumulators of the float64 matrix instructions stay in ordinary VGPRs (those kernels fit
 # 256 registers, and the AGPR form costs copies around each MFMA).  The bf16 Hessian kernel
-# needs all 256 AGPRs for its accumulators and is compiled without the option.
+# and the 8-bit product need all 256 AGPRs for their accumulators and are compiled without the option.
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form"]
-NO_VGPR_FORM = {"hessian.hip"}
+NO_VGPR_FORM = {"hessian.hip", "int8_linear.hip"}
 
 
 def _hipcc() -> str:
@@ -128,6 +128,7 @@ ASSEMBLY_CHECKS = {
     "hessian.hip": check_lds_dma_wait_states,
     "layer_error.hip": check_lds_dma_wait_states,
     "artifact.hip": check_lds_dma_wait_states,
+    "int8_linear.hip": check_lds_dma_wait_states,
 }
 
 

@@ -165,6 +165,11 @@ int64_t rmsnorm_max_columns();
 ptq_status rmsnorm_quantize_launch(const void* X, ptq_dtype dt, int64_t ldx, int64_t t, int64_t n, const void* residual,
                                    int64_t ldr, void* residual_out, int64_t ldo, const void* gamma, double eps, int normalize,
                                    int8_t* codes, int64_t ldc, float* scales, hipStream_t s);
+int64_t int8_linear_max_columns();
+size_t int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t t);
+ptq_status int8_linear_launch(const int8_t* A, int64_t lda, const float* a_scales, int64_t t, const int8_t* W, int64_t ldw,
+                              const float* w_scales, int64_t m, int64_t n, const float* bias, void* O, ptq_dtype odt,
+                              int64_t ldo, void* ws, hipStream_t s);
 ptq_status kv_cache_write_launch(const void* K, int64_t k_token, int64_t k_head, const void* V, int64_t v_token,
                                  int64_t v_head, ptq_dtype dt, int64_t t, int hkv, int d, const int32_t* slots, int bits,
                                  uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int page, hipStream_t s);

@@ -1,0 +1,415 @@
+// Product of 8-bit tokens with an 8-bit weight:  O = (sum_k A[i][k] W[j][k]) a_scale[i] w_scale[j] + bias[j].
+//
+// Both operands have k side by side, which is how the matrix instructions want them: 16 bytes of a row are a lane's operand,
+// no transposition and no unpacking.  Sums are 32-bit integers, hence exact and independent of the order (n <= 131056 keeps
+// 128 * 128 * n below 2^31); the epilogue converts, scales twice and adds, each rounded to float32.
+//
+// Up to 64 tokens the weight's bytes are the bound: its rows go straight from memory into registers (skinny_kernel).  Beyond
+// that the products are: tiles of W rows x tokens staged in LDS (tile_kernel).
+#include <algorithm>
+
+#include "lds_dma.h"
+#include "stored_rows.h"
+
+namespace ptq {
+namespace {
+
+typedef __attribute__((__vector_size__(16 * sizeof(int)))) int i32x16;
+
+struct LinearArgs {
+  const int8_t* A; const float* as; const int8_t* W; const float* ws; const float* bias; void* O;
+  int64_t lda, ldw, ldo;
+  int t, m, n;
+};
+
+// N consecutive outputs of a token
+template <int DT, int N>
+__device__ __forceinline__ void store_outputs(const LinearArgs& a, int token, int row, float as, const int (&sum)[N],
+                                              const float (&ws)[N], const float (&bias)[N]) {
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (float)sum[i] * as * ws[i] + bias[i];
+  store_run<DT, N, true>(static_cast<typename StoredType<DT>::type*>(a.O) + token * a.ldo, row, a.m, v);
+}
+// scales and biases of N consecutive rows of W (past the last: its own)
+template <int N>
+__device__ __forceinline__ void load_channels(const LinearArgs& a, int row, float (&ws)[N], float (&bias)[N]) {
+  const float* b = a.bias ? a.bias : a.ws;   // no branch around a load
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int at = min(row + i, a.m - 1);
+    ws[i] = a.ws[at];
+    bias[i] = b[at];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) bias[i] = a.bias ? bias[i] : 0.f;
+}
+
+// ---- few tokens ---------------------------------------------------------------------------------------------
+// A workgroup takes 16 rows of W; its eight waves share out the 64-byte steps of k and meet in LDS.  Every byte of W is read
+// once, eight loads of 16 bytes a lane on their way: one trip to memory for n = 4096.  The tokens (columns of the matrix
+// instruction, TB x 16 of them) come from the L2.
+constexpr int kSkinnyWaves = 8, kSkinnyAhead = 8;
+
+template <int DT, int TB>
+__global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(LinearArgs a) {
+  __shared__ i32x4 part[kSkinnyWaves][TB][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int row0 = blockIdx.x * 16;
+  const int8_t* W = a.W + (int64_t)min(row0 + r, a.m - 1) * a.ldw;
+  const int8_t* A[TB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b) A[b] = a.A + (int64_t)min(b * 16 + r, a.t - 1) * a.lda;
+  i32x4 acc[TB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b) acc[b] = i32x4{0, 0, 0, 0};
+  constexpr int kAhead = TB > 2 ? kSkinnyAhead / 2 : kSkinnyAhead;
+  const int steps = (a.n + 63) / 64;
+  for (int s0 = wave; s0 < steps; s0 += kSkinnyWaves * kAhead) {
+    i32x4 w[kAhead], x[kAhead][TB];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int k = (s0 + i * kSkinnyWaves) * 64 + g * 16, at = k < a.n ? k : 0;
+      w[i] = *reinterpret_cast<const i32x4*>(W + at);
+#pragma unroll
+      for (int b = 0; b < TB; ++b) x[i][b] = *reinterpret_cast<const i32x4*>(A[b] + at);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int k = (s0 + i * kSkinnyWaves) * 64 + g * 16;
+      if (k >= a.n) w[i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int b = 0; b < TB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[i][b], acc[b], 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < TB; ++b) part[wave][b][lane] = acc[b];
+  __syncthreads();
+  if (wave >= TB) return;
+  i32x4 sum = part[0][wave][lane];
+#pragma unroll
+  for (int w = 1; w < kSkinnyWaves; ++w) sum += part[w][wave][lane];
+  const int token = wave * 16 + r, row = row0 + 4 * g;   // the instruction's columns are tokens, four rows to a lane
+  if (token >= a.t || row >= a.m) return;
+  float ws[4], bias[4];
+  load_channels<4>(a, row, ws, bias);
+  const int s[4] = {sum[0], sum[1], sum[2], sum[3]};
+  store_outputs<DT, 4>(a, token, row, a.as[token], s, ws, bias);
+}
+
+// ---- tiles --------------------------------------------------------------------------------------------------
+// Four waves, each 32 WM rows of W x 32 WN tokens on 32 x 32 x 32 instructions; the block tile is twice that both ways.
+// Stages of 64 bytes of k go from memory straight into LDS, into a ring of four: rows of 64 bytes, four chunks of 16, chunk c
+// of row r at position c ^ turn(r), which spreads the rows that a read touches together over all banks (the request applies
+// it on the memory's side).  Iteration s: products of the first 32 bytes of k of stage s | barrier | of the others; the next
+// operands are read from LDS beside the products, and behind the barrier, where nobody needs stage s any more, its slot is
+// asked to be filled with stage s + 4.
+//
+// The sums leave through LDS, 32 tokens of a wave at a time: a lane of the matrix instruction has four rows of W in a run of eight for
+// one token, and a store wants whole lines of a token.
+//
+// If n is not a multiple of 64 the stage that holds the rest comes first, with its lanes past n sent out of the buffer's range
+// (zeros): the main loop does not have to know about it.
+constexpr int kStageK = 64, kRing = 4;
+
+__device__ __forceinline__ int turn(int r) { return ((r >> 1) & 3) ^ ((r >> 3) & 1); }
+
+template <int WM, int WN>
+constexpr int tile_lds_bytes() { return kRing * (64 * WM + 64 * WN) * kStageK; }
+
+struct TilePlan {
+  int tiles_m, tiles_t, splits, stages;   // stages: of all k, per split at most stages_each
+  int stages_each;
+  int* partial;                           // splits > 1: [split][64 WN tiles_t][64 WM tiles_m]
+};
+
+// which tile and split a block works on: the blocks of a die (consecutive numbers modulo 8) get consecutive tiles, eight token
+// tiles deep, whose operands they share in the die's L2
+__device__ __forceinline__ void tile_of_block(const TilePlan& p, int id, int total, int& tm, int& tt, int& split) {
+  const int die = id & 7, each = total >> 3, rest = total & 7;
+  int i = die * each + min(die, rest) + (id >> 3);
+  const int tiles = p.tiles_m * p.tiles_t;
+  split = i / tiles;
+  i -= split * tiles;
+  const int deep = 8, group = i / (deep * p.tiles_m);
+  const int first = group * deep, here = min(deep, p.tiles_t - first);
+  i -= group * deep * p.tiles_m;
+  tm = i / here;
+  tt = first + i % here;
+}
+
+// DT < 0: the sums of a split, into p.partial
+template <int DT, int WM, int WN>
+__global__ __launch_bounds__(256) void tile_kernel(LinearArgs a, TilePlan p) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  typedef __attribute__((address_space(3))) char lds_char;
+  typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
+  lds_char* lds = (lds_char*)smem;
+  const uint32_t lbase = (uint32_t)(uintptr_t)lds;
+  constexpr int kPartW = 64 * WM * kStageK, kSlot = kPartW + 64 * WN * kStageK, L = WM + WN;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wt = wave & 1, h = lane >> 5;
+  int tm, tt, split;
+  tile_of_block(p, blockIdx.x, gridDim.x, tm, tt, split);
+  const int m0 = tm * 64 * WM, t0 = tt * 64 * WN;
+  const int first = split * p.stages_each, last = min(first + p.stages_each, p.stages);
+  const int nstage = last - first;
+
+  i32x16 acc[WM][WN];
+#pragma unroll
+  for (int x = 0; x < WM; ++x)
+#pragma unroll
+    for (int y = 0; y < WN; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x][y][r] = 0;
+
+  const int whole = a.n / kStageK, rest = a.n % kStageK;
+  const int k0 = (rest ? (first == 0 ? 0 : first - 1) : first) * kStageK;   // of the first stage that is whole
+  auto extent = [&](int rows, int64_t ld, int k) { return (int64_t)(rows - 1) * ld + a.n - k; };
+  const int rows_w = min(64 * WM, a.m - m0), rows_t = min(64 * WN, a.t - t0);
+  const int8_t* W0 = a.W + (int64_t)m0 * a.ldw;
+  const int8_t* A0 = a.A + (int64_t)t0 * a.lda;
+  i32x4 dw = buffer_at(W0 + k0, extent(rows_w, a.ldw, k0)), dt = buffer_at(A0 + k0, extent(rows_t, a.lda, k0));
+
+  // request q of a stage: 16 rows, four lanes each; the wave's share is every fourth 16
+  uint32_t vo[L];
+  auto chunk_of = [&](int q) {
+    const int row = (4 * (q < WM ? q : q - WM) + wave) * 16 + (lane >> 2);
+    return (lane & 3) ^ turn(row);
+  };
+#pragma unroll
+  for (int q = 0; q < L; ++q) {
+    const int row = (4 * (q < WM ? q : q - WM) + wave) * 16 + (lane >> 2);
+    vo[q] = (uint32_t)(row * (int)(q < WM ? a.ldw : a.lda) + 16 * chunk_of(q));
+  }
+  const uint32_t wbase = lbase + wave * 1024;
+  auto place = [](int q) constexpr { return (uint32_t)(q < WM ? q * 4096 : kPartW + (q - WM) * 4096); };
+  int asked = 0;   // stages asked for; those past the last one are asked of an empty buffer
+  auto advance = [&](i32x4& d) {
+    const uint64_t base = (((uint64_t)(uint32_t)d[1] << 32) | (uint32_t)d[0]) + kStageK;
+    d[0] = (int)__builtin_amdgcn_readfirstlane((uint32_t)base);
+    d[1] = (int)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32));
+    d[2] = asked < nstage ? d[2] - kStageK : 0;
+  };
+
+  // prologue: stages 0, 1, 2 and the first half of 3
+  auto ask = [&](int q, uint32_t slot, uint32_t v) {
+    if (q < WM) request_to_lds(dw, v, wbase + slot + place(q));
+    else request_to_lds(dt, v, wbase + slot + place(q));
+  };
+  const bool rest_first = rest != 0 && first == 0;
+  if (rest_first) {
+    const i32x4 sw = dw, st = dt;
+    dw = buffer_at(W0 + whole * kStageK, extent(rows_w, a.ldw, whole * kStageK));
+    dt = buffer_at(A0 + whole * kStageK, extent(rows_t, a.lda, whole * kStageK));
+#pragma unroll
+    for (int q = 0; q < L; ++q) ask(q, 0, 16 * chunk_of(q) < rest ? vo[q] : 0x80000000u);
+    dw = sw;
+    dt = st;
+    ++asked;
+    if (asked >= nstage) dw[2] = dt[2] = 0;
+    asm volatile("s_nop 4" : "+s"(dw), "+s"(dt));
+  }
+  static_for<kRing - 1>([&](auto s_) {
+    constexpr int s = decltype(s_)::value;
+    if (s == 0 && rest_first) return;
+#pragma unroll
+    for (int q = 0; q < L; ++q) ask(q, s * kSlot, vo[q]);
+    ++asked;
+    advance(dw);
+    advance(dt);
+  });
+#pragma unroll
+  for (int q = 0; q < L / 2; ++q) ask(q, (kRing - 1) * kSlot, vo[q]);
+  wait_requests<2 * L + L / 2>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");   // no read of LDS above the barrier
+
+  // where a lane finds its operands inside a slot: first and second half of the stage
+  uint32_t aw[2][WM], at[2][WN];
+#pragma unroll
+  for (int T = 0; T < WM; ++T) {
+    const int row = wm * 32 * WM + 32 * T + (lane & 31);
+    aw[0][T] = row * kStageK + 16 * (h ^ turn(row));
+    aw[1][T] = aw[0][T] ^ 32;
+  }
+#pragma unroll
+  for (int U = 0; U < WN; ++U) {
+    const int row = wt * 32 * WN + 32 * U + (lane & 31);
+    at[0][U] = kPartW + row * kStageK + 16 * (h ^ turn(row));
+    at[1][U] = at[0][U] ^ 32;
+  }
+  auto read_one = [&](uint32_t at_) { return *(lds_i32x4*)(lds + at_); };
+
+  // The products of 32 bytes of k on (fw, ft) while the next operands are read from `slot` (half HALF of the stage), and L / 2
+  // requests, q0 onwards, go into slot `dst`, spread over the products.
+  auto half = [&](auto half_, auto q0_, const i32x4 (&fw)[WM], const i32x4 (&ft)[WN], i32x4 (&nw)[WM], i32x4 (&nt)[WN],
+                  uint32_t slot, uint32_t dst) {
+    constexpr int HALF = decltype(half_)::value, Q0 = decltype(q0_)::value;
+    static_for<WM>([&](auto x_) {
+      constexpr int x = decltype(x_)::value;
+      nw[x] = read_one(slot + aw[HALF][x]);
+      if constexpr (x < WN) nt[x] = read_one(slot + at[HALF][x]);
+#pragma unroll
+      for (int y = 0; y < WN; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[x], ft[y], acc[x][y], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (x < L / 2) ask(Q0 + x, dst, vo[Q0 + x]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  using std::integral_constant;
+  i32x4 fw0[WM], ft0[WN], fw1[WM], ft1[WN];
+#pragma unroll
+  for (int T = 0; T < WM; ++T) fw0[T] = read_one(aw[0][T]);
+#pragma unroll
+  for (int U = 0; U < WN; ++U) ft0[U] = read_one(at[0][U]);
+  int s = 0;
+  do {   // (there is one stage at least: no way around the loop, on which the sums would have to be copied)
+    const uint32_t slot = (s & (kRing - 1)) * kSlot, before = ((s + kRing - 1) & (kRing - 1)) * kSlot,
+                   next = ((s + 1) & (kRing - 1)) * kSlot;
+    half(integral_constant<int, 1>{}, integral_constant<int, L / 2>{}, fw0, ft0, fw1, ft1, slot, before);
+    ++asked;
+    advance(dw);
+    advance(dt);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    wait_requests<2 * L>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    half(integral_constant<int, 0>{}, integral_constant<int, 0>{}, fw1, ft1, fw0, ft0, next, slot);
+  } while (++s < nstage);
+  wait_requests<0>();   // nothing may land in this LDS after the workgroup has left it
+
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+
+  constexpr int kPitch = 32 * WM * 4 + 16;             // bytes of a token; the odd 16 spread the tokens over the banks
+  constexpr int kLanes = 4 * WM, kTokens = 64 / kLanes;  // eight outputs a lane
+  static_assert(4 * 32 * kPitch <= tile_lds_bytes<WM, WN>(), "");
+  lds_char* area = lds + wave * 32 * kPitch;
+  const int col = 8 * (lane % kLanes), row = m0 + wm * 32 * WM + col;
+  float ws[8], bias[8];
+  if constexpr (DT >= 0) load_channels<8>(a, row, ws, bias);
+#pragma unroll
+  for (int U = 0; U < WN; ++U) {
+#pragma unroll
+    for (int T = 0; T < WM; ++T)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(lds_i32x4*)(area + (lane & 31) * kPitch + (32 * T + 8 * q + 4 * h) * 4) =
+            i32x4{acc[T][U][4 * q], acc[T][U][4 * q + 1], acc[T][U][4 * q + 2], acc[T][U][4 * q + 3]};
+#pragma unroll 1
+    for (int i = 0; i < 32; i += kTokens) {
+      const int token = wt * 32 * WN + 32 * U + i + lane / kLanes;
+      const i32x4 lo = *(lds_i32x4*)(area + (i + lane / kLanes) * kPitch + col * 4);
+      const i32x4 hi = *(lds_i32x4*)(area + (i + lane / kLanes) * kPitch + col * 4 + 16);
+      if constexpr (DT < 0) {
+        int* out = p.partial + ((int64_t)split * p.tiles_t * 64 * WN + t0 + token) * (p.tiles_m * 64 * WM) + row;
+        *reinterpret_cast<i32x4*>(out) = lo;
+        *reinterpret_cast<i32x4*>(out + 4) = hi;
+      } else if (t0 + token < a.t && row < a.m) {
+        const int v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        store_outputs<DT, 8>(a, t0 + token, row, a.as[t0 + token], v, ws, bias);
+      }
+    }
+  }
+}
+
+// adds the splits' sums and writes the outputs: eight outputs of a token a thread
+template <int DT>
+__global__ __launch_bounds__(256) void split_sum_kernel(LinearArgs a, const int* __restrict__ partial, int splits, int rows, int cols) {
+  const int row = (blockIdx.x * 256 + threadIdx.x) * 8, token = blockIdx.y;
+  if (row >= a.m) return;
+  int v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const int* in = partial + (int64_t)token * cols + row;
+  for (int s = 0; s < splits; ++s, in += (int64_t)rows * cols) {
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(in), hi = *reinterpret_cast<const i32x4*>(in + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] += lo[e];
+      v[4 + e] += hi[e];
+    }
+  }
+  float ws[8], bias[8];
+  load_channels<8>(a, row, ws, bias);
+  store_outputs<DT, 8>(a, token, row, a.as[token], v, ws, bias);
+}
+
+constexpr int kSkinnyTokens = 64;
+struct Form {
+  bool skinny, big;
+  TilePlan plan;
+};
+// 256 x 256 tiles where there are enough of them for the chip's 256 compute units, else 128 x 128, two to a compute unit, k split
+// until there are 512 of them (eight stages each at least)
+Form form_of(int64_t t, int64_t m, int64_t n) {
+  Form f{};
+  f.skinny = t <= kSkinnyTokens;
+  if (f.skinny) return f;
+  f.big = ceil_div(t, 256) * ceil_div(m, 256) >= 192;
+  const int side = f.big ? 256 : 128;
+  TilePlan& p = f.plan;
+  p.tiles_m = (int)ceil_div(m, side);
+  p.tiles_t = (int)ceil_div(t, side);
+  p.stages = (int)ceil_div(n, kStageK);
+  p.splits = 1;
+  if (!f.big) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(512 / ((int64_t)p.tiles_m * p.tiles_t), p.stages / 8));
+  p.stages_each = (int)ceil_div(p.stages, p.splits);
+  p.splits = (int)ceil_div(p.stages, p.stages_each);
+  return f;
+}
+
+template <int DT>
+ptq_status launch(const LinearArgs& a, void* ws, hipStream_t s) {
+  Form f = form_of(a.t, a.m, a.n);
+  if (f.skinny) {
+    const dim3 grid((unsigned)ceil_div(a.m, 16));
+    if (a.t <= 16) skinny_kernel<DT, 1><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
+    else if (a.t <= 32) skinny_kernel<DT, 2><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
+    else skinny_kernel<DT, 4><<<grid, kSkinnyWaves * 64, 0, s>>>(a);
+    return PTQ_OK;
+  }
+  TilePlan& p = f.plan;
+  p.partial = p.splits > 1 ? static_cast<int*>(ws) : nullptr;
+  const int64_t blocks = (int64_t)p.tiles_m * p.tiles_t * p.splits;
+  if (blocks > INT32_MAX) return PTQ_ERR_SHAPE;
+  if (f.big) {
+    if (!lds_opt_in<tile_kernel<DT, 4, 4>>(tile_lds_bytes<4, 4>())) return PTQ_ERR_HIP;
+    tile_kernel<DT, 4, 4><<<(unsigned)blocks, 256, tile_lds_bytes<4, 4>(), s>>>(a, p);
+  } else {
+    constexpr int kBytes = tile_lds_bytes<2, 2>();
+    if (!p.partial) {
+      if (!lds_opt_in<tile_kernel<DT, 2, 2>>(kBytes)) return PTQ_ERR_HIP;
+      tile_kernel<DT, 2, 2><<<(unsigned)blocks, 256, kBytes, s>>>(a, p);
+    } else {
+      if (!lds_opt_in<tile_kernel<-1, 2, 2>>(kBytes)) return PTQ_ERR_HIP;
+      tile_kernel<-1, 2, 2><<<(unsigned)blocks, 256, kBytes, s>>>(a, p);
+      split_sum_kernel<DT><<<dim3((unsigned)ceil_div(a.m, 2048), (unsigned)a.t), 256, 0, s>>>(a, p.partial, p.splits, p.tiles_t * 128,
+                                                                                              p.tiles_m * 128);
+    }
+  }
+  return PTQ_OK;
+}
+
+}  // namespace
+
+int64_t int8_linear_max_columns() { return 131056; }
+
+size_t int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t t) {
+  if (m <= 0 || n <= 0 || t <= 0) return 0;
+  const Form f = form_of(t, m, n);
+  if (f.skinny || f.plan.splits <= 1) return 0;
+  return (size_t)f.plan.splits * f.plan.tiles_m * f.plan.tiles_t * 128 * 128 * sizeof(int);
+}
+
+ptq_status int8_linear_launch(const int8_t* A, int64_t lda, const float* a_scales, int64_t t, const int8_t* W, int64_t ldw,
+                              const float* w_scales, int64_t m, int64_t n, const float* bias, void* O, ptq_dtype odt,
+                              int64_t ldo, void* ws, hipStream_t s) {
+  const LinearArgs a{A, a_scales, W, w_scales, bias, O, lda, ldw, ldo, (int)t, (int)m, (int)n};
+  const ptq_status rc = odt == PTQ_BF16 ? launch<PTQ_BF16>(a, ws, s) : launch<PTQ_F32>(a, ws, s);
+  if (rc != PTQ_OK) return rc;
+  PTQ_HIP_CHECK_LAUNCH();
+  return PTQ_OK;
+}
+
+}  // namespace ptq

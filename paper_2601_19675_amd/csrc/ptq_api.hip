@@ -54,6 +54,7 @@ ptq_status ptq_workspace_bytes(ptq_op op, int64_t m, int64_t n, int64_t t, int64
     case PTQ_OP_ACTIVATION_ABS_SUM: *bytes = abs_sum_workspace_bytes(n); return PTQ_OK;
     case PTQ_OP_SCALED_R1SVD: *bytes = r1svd_workspace_bytes(m, n); return PTQ_OK;
     case PTQ_OP_LINEAR_FORWARD: *bytes = linear_forward_workspace_bytes(t, m, n, block); return PTQ_OK;
+    case PTQ_OP_INT8_LINEAR: *bytes = int8_linear_workspace_bytes(m, n, t); return PTQ_OK;
   }
   return PTQ_ERR_ARG;
 }
@@ -330,6 +331,19 @@ ptq_status ptq_rmsnorm_quantize(const void* X, ptq_dtype dt, int64_t ldx, int64_
   if (!X || !codes || !scales || misaligned(codes, 16)) return PTQ_ERR_ARG;
   return rmsnorm_quantize_launch(X, dt, ldx, t, n, residual, ldr, residual_out, ldo, gamma, eps, normalize, codes, ldc, scales,
                                  static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_int8_linear(const int8_t* A, int64_t lda, const float* a_scales, int64_t t, const int8_t* W, int64_t ldw,
+                           const float* w_scales, int64_t m, int64_t n, const float* bias, void* O, ptq_dtype odt, int64_t ldo,
+                           void* ws, size_t ws_bytes, ptq_stream stream) {
+  if (odt != PTQ_F32 && odt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  if (t < 0 || m < 0 || n <= 0 || n % 16 != 0 || n > int8_linear_max_columns() || lda < n || ldw < n || lda % 16 != 0 ||
+      ldw % 16 != 0 || lda > (1 << 22) || ldw > (1 << 22) || ldo < m || t > INT32_MAX / 2 || m > INT32_MAX / 2)
+    return PTQ_ERR_SHAPE;
+  if (t == 0 || m == 0) return PTQ_OK;
+  if (!A || !a_scales || !W || !w_scales || !O || misaligned(A, 16) || misaligned(W, 16)) return PTQ_ERR_ARG;
+  if (ws_bad(ws, ws_bytes, int8_linear_workspace_bytes(m, n, t))) return PTQ_ERR_WORKSPACE;
+  return int8_linear_launch(A, lda, a_scales, t, W, ldw, w_scales, m, n, bias, O, odt, ldo, ws, static_cast<hipStream_t>(stream));
 }
 
 ptq_status ptq_kv_cache_write(const void* K, int64_t k_token, int64_t k_head, const void* V, int64_t v_token, int64_t v_head,

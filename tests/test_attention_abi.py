@@ -56,3 +56,21 @@ def test_cache(lib):
     assert write(slots=None) == ARG and write(t=-1) == SHAPE
     assert read(table=None) == ARG and read(cu=None) == ARG and read(pages=0) == SHAPE
     assert read(b=65536) == SHAPE and read(ldt=-1) == SHAPE and read(rows=-1) == SHAPE and read(max_kv=-1) == SHAPE
+
+
+def test_int8_linear(lib):
+    call = caller(lib.ptq_int8_linear, A=P, lda=64, asc=P, t=4, W=P, ldw=64, wsc=P, m=8, n=64, bias=None, O=P, odt=1, ldo=8, ws=None,
+                  bytes=0, stream=None)
+    assert call(t=0) == OK and call(m=0, ldo=0) == OK
+    assert call(odt=2) == DTYPE
+    assert call(n=0) == SHAPE and call(n=24) == SHAPE and call(lda=48) == SHAPE and call(lda=72) == SHAPE and call(ldw=48) == SHAPE
+    assert call(n=131072, lda=131072, ldw=131072) == SHAPE and call(lda=2 ** 22 + 16) == SHAPE and call(ldw=2 ** 22 + 16) == SHAPE
+    assert call(ldo=7) == SHAPE and call(t=-1) == SHAPE and call(m=-1) == SHAPE
+    for name in ("A", "asc", "W", "wsc", "O"):
+        assert call(**{name: None}) == ARG
+    assert call(A=P + 8) == ARG and call(W=P + 4) == ARG
+    need = ptq.ptq_workspace_bytes(ptq.OP_INT8_LINEAR, 4096, 11008, 333)
+    assert need > 0
+    big = dict(t=333, m=4096, n=11008, lda=11008, ldw=11008, ldo=4096)
+    assert call(**big) == WORKSPACE and call(**big, ws=P, bytes=need - 1) == WORKSPACE and call(**big, ws=P + 8, bytes=need) == WORKSPACE
+    assert ptq.ptq_workspace_bytes(ptq.OP_INT8_LINEAR, 4096, 4096, 1) == 0
