@@ -59,7 +59,8 @@ typedef enum {
   PTQ_OP_ACTIVATION_ABS_SUM = 6,
   PTQ_OP_SCALED_R1SVD = 7,
   PTQ_OP_LINEAR_FORWARD = 8, /* t = tokens, block = rank r */
-  PTQ_OP_INT8_LINEAR = 10    /* t = tokens (9 is no operation) */
+  PTQ_OP_INT8_LINEAR = 10,    /* t = tokens (9 is no operation) */
+  PTQ_OP_PAGED_ATTENTION = 11 /* m = query heads, n = d, t = tokens, block = max_kv */
 } ptq_op;
 
 typedef void* ptq_stream; /* hipStream_t */
@@ -508,6 +509,35 @@ ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const ui
                              int64_t hkv, int64_t d, int bits, const int32_t* table, int64_t ldt, int64_t b, const int32_t* cu_kv,
                              int64_t rows, int64_t max_kv, void* K, int64_t k_token, int64_t k_head, void* V, int64_t v_token,
                              int64_t v_head, ptq_dtype dt, ptq_stream stream);
+
+/*
+ * Softmax attention of new tokens over a paged quantized cache that holds their own keys and values already.
+ *
+ * Sequence s has the queries cu_q[s] .. cu_q[s + 1] and kv_lens[s] keys, key j at place j % page of page table[s][j / page].
+ * Query i of n stands at place kv_lens[s] - n + i.  It sees key j if the key's page is there, j < kv_lens[s], with causal != 0 also
+ * j <= its place, with window > 0 also j > its place - window.  Query head h reads key head h / (hq / hkv):
+ *
+ *   O = sum_j p_j v_j / sum_j p_j,   p_j = exp(softmax_scale q . k_j - max),   zeros if no key is seen
+ *
+ * Keys and values stand for scale (code - zero) exactly; scores, running maxima and sums are float32.  Weights are rounded to
+ * float16 (2^-11) before they meet the values; in chunks of queries the values are too.  A key that is not seen has no
+ * effect, whatever its scales hold; one that is seen and whose scales are NaN makes the row NaN.
+ *
+ * Q, O      token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_BF16.  O is not Q.
+ * cu_q, kv_lens   b + 1 and b int32 on the device.  A sequence that would begin before token 0 or end past t is left out; keys past
+ *           max_kv or the table's ldt pages are not there.
+ * max_q, max_kv   no sequence has more queries or keys (rows of queries from max_q on are left out).     b <= 65535.
+ * table     b x ldt int32; a number outside [0, pages) is a page that is not there.
+ * hq        a multiple of hkv, at most 65535.     softmax_scale  finite.     window  >= 0.     The rest as above.
+ * Workspace: PTQ_OP_PAGED_ATTENTION with m = hq, n = d, t and block = max_kv.  Results do not depend on what it holds.
+ * Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE, PTQ_ERR_WORKSPACE.
+ */
+ptq_status ptq_paged_attention(const void* Q, ptq_dtype qdt, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                               const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                               const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits, const int32_t* table,
+                               int64_t ldt, const int32_t* kv_lens, int64_t max_kv, double softmax_scale, int causal,
+                               int64_t window, void* O, int64_t o_token, int64_t o_head, void* ws, size_t ws_bytes,
+                               ptq_stream stream);
 
 #ifdef __cplusplus
 }

@@ -70,10 +70,13 @@ def pack_row(codes, bits: int):
 
 
 def unpack_row(raw, bits: int):
+    """Codes of rows of bytes (any leading dimensions)."""
     raw = np.ascontiguousarray(raw, dtype=np.uint8)
     if bits == 8:
         return raw.astype(np.int64)
-    return np.array([(int(w) >> (4 * (i // 2) + 16 * (i % 2))) & 15 for w in raw.view("<u4") for i in range(8)], dtype=np.int64)
+    words = raw.view("<u4").astype(np.int64)[..., None]
+    i = np.arange(8)
+    return ((words >> (4 * (i // 2) + 16 * (i % 2))) & 15).reshape(raw.shape[:-1] + (-1,))
 
 
 def cache_write(K, V, slots, bits: int, codes, scales, zeros):
@@ -92,43 +95,54 @@ def cache_write(K, V, slots, bits: int, codes, scales, zeros):
 
 def cache_rows(codes, scales, zeros, bits: int, table, length: int, which: int):
     """What the cache holds of one sequence: ([length, heads, d] float64, [length] whether the page is there)."""
-    pages, heads, page = codes.shape[1:4]
-    d = codes.shape[4] * 8 // bits
-    X, there = np.zeros((length, heads, d)), np.zeros(length, dtype=bool)
-    for i in range(length):
-        p = int(table[i // page]) if i // page < len(table) else -1
-        if not 0 <= p < pages:
-            continue
-        there[i] = True
-        for h in range(heads):
-            at = (which, p, h, i % page)
-            X[i, h] = float(scales[at]) * (unpack_row(codes[at], bits) - int(zeros[at]))
+    pages, _, page = codes.shape[1:4]
+    i = np.arange(length)
+    p = np.full(length, -1, dtype=np.int64)
+    listed = i // page < len(table)
+    p[listed] = np.asarray(table, dtype=np.int64)[i[listed] // page]
+    there = (p >= 0) & (p < pages)
+    p = np.where(there, p, 0)
+    X = unpack_row(codes[which][p, :, i % page], bits) - zeros[which][p, :, i % page].astype(np.int64)[..., None]
+    X = scales[which][p, :, i % page].astype(np.float64)[..., None] * X
+    X[~there] = 0.0
     return X, there
 
 
-def attention(Q, cu_q, codes, scales, zeros, bits: int, table, kv_lens, softmax_scale: float, causal=True, window=0):
+def attention(Q, cu_q, codes, scales, zeros, bits: int, table, kv_lens, softmax_scale: float, causal=True, window=0, spread=False):
     """Query i of a sequence of `new` queries and `length` keys stands at place length - new + i; it sees key j if j < length,
-    j's page is there, and (causal) j <= place, (window > 0) j > place - window.  No key: zeros."""
+    j's page is there, and (causal) j <= place, (window > 0) j > place - window.  No key: zeros.
+    spread: also sum p |v| / sum p and the largest softmax_scale sum |q| |k| of each (token, head), for error bounds."""
     Q = np.asarray(Q, dtype=np.float64)
-    hq, hkv = Q.shape[1], codes.shape[2]
-    O = np.zeros(Q.shape)
+    group = Q.shape[1] // codes.shape[2]
+    O, size, reach = np.zeros(Q.shape), np.zeros(Q.shape), np.zeros(Q.shape[:2])
     for s, length in enumerate(kv_lens):
-        a, b = int(cu_q[s]), int(cu_q[s + 1])
-        K, there = cache_rows(codes, scales, zeros, bits, table[s], int(length), 0)
-        V, _ = cache_rows(codes, scales, zeros, bits, table[s], int(length), 1)
-        j = np.arange(int(length))
-        for i in range(b - a):
-            place = int(length) - (b - a) + i
-            sees = there.copy()
-            if causal:
-                sees &= j <= place
-            if window:
-                sees &= j > place - window
-            if not sees.any():
-                continue
-            for h in range(hq):
-                g = h // (hq // hkv)
-                x = softmax_scale * (K[sees, g] @ Q[a + i, h])
-                p = np.exp(x - x.max())
-                O[a + i, h] = p @ V[sees, g] / p.sum()
-    return O
+        a, b, length = int(cu_q[s]), int(cu_q[s + 1]), int(length)
+        if a == b:
+            continue
+        K, there = cache_rows(codes, scales, zeros, bits, table[s], length, 0)
+        V, _ = cache_rows(codes, scales, zeros, bits, table[s], length, 1)
+        place, j = length - (b - a) + np.arange(b - a)[:, None], np.arange(length)[None]
+        sees = np.broadcast_to(there, (b - a, length)).copy()
+        if causal:
+            sees &= j <= place
+        if window:
+            sees &= j > place - window
+        some = sees.any(1)
+        if not some.any():
+            continue
+        for h in range(Q.shape[1]):
+            k, v = K[:, h // group], V[:, h // group]
+            for rows in np.array_split(np.nonzero(some)[0], max(1, int(some.sum()) * length // 4000000)):
+                # a key that a query does not see has no part in it, whatever it holds
+                with np.errstate(invalid="ignore"):
+                    x = np.where(sees[rows], softmax_scale * (Q[a + rows, h] @ np.where(np.isnan(k), 0.0, k).T), -np.inf)
+                x[sees[rows] & np.isnan(k).any(1)] = np.nan
+                p = np.exp(x - x.max(1, keepdims=True))
+                lost = (sees[rows] & np.isnan(v).any(1)).any(1)
+                O[a + rows, h] = p @ np.where(np.isnan(v), 0.0, v) / p.sum(1, keepdims=True)
+                O[a + rows[lost], h] = np.nan
+                if spread:
+                    size[a + rows, h] = p @ np.abs(np.where(np.isnan(v), 0.0, v)) / p.sum(1, keepdims=True)
+                    r = abs(softmax_scale) * (np.abs(Q[a + rows, h]) @ np.abs(np.where(np.isnan(k), 0.0, k)).T)
+                    reach[a + rows, h] = np.where(sees[rows], r, 0).max(1)
+    return (O, size, reach) if spread else O

@@ -17,7 +17,7 @@ PTQ_F32, PTQ_BF16, PTQ_F64 = 0, 1, 2
 OP_HESSIAN, OP_CHOLESKY_INV, OP_QUANTIZE, OP_LAYER_ERROR = 0, 1, 2, 3
 OP_LOPRO_ORDER, OP_LOPRO_ROTATE_HESSIAN = 4, 5
 OP_ACTIVATION_ABS_SUM, OP_SCALED_R1SVD, OP_LINEAR_FORWARD = 6, 7, 8
-OP_INT8_LINEAR = 10
+OP_INT8_LINEAR, OP_PAGED_ATTENTION = 10, 11
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -99,6 +99,9 @@ def load_library() -> ctypes.CDLL:
     lib.ptq_kv_cache_read.restype = c.c_int
     lib.ptq_kv_cache_read.argtypes = [vp, vp, vp, i64, i64, i64, i64, c.c_int, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64,
                                       i64, c.c_int, vp]
+    lib.ptq_paged_attention.restype = c.c_int
+    lib.ptq_paged_attention.argtypes = [vp, c.c_int, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, i64, i64, i64, c.c_int, vp,
+                                        i64, vp, i64, c.c_double, c.c_int, i64, vp, i64, i64, vp, sz, vp]
     _LIB = lib
     return lib
 
@@ -518,3 +521,29 @@ def ptq_kv_cache_read(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Te
                                           K.stride(0), K.stride(1), V.data_ptr(), V.stride(0), V.stride(1), _dtype_code(K), _stream())
     if rc:
         raise PtqError(rc, "ptq_kv_cache_read")
+
+
+def ptq_paged_attention(Q: torch.Tensor, cu_q: torch.Tensor, max_q: int, codes: torch.Tensor, scales: torch.Tensor,
+                        zeros: torch.Tensor, bits: int, table: torch.Tensor, kv_lens: torch.Tensor, max_kv: int,
+                        softmax_scale: float, O: torch.Tensor, causal: bool = True, window: int = 0,
+                        ws: torch.Tensor | None = None) -> None:
+    """O <- attention of Q (bfloat16 t x heads x d) over the cache; sequence s has the tokens cu_q[s] .. cu_q[s + 1] (int32, on
+    the device, no more than max_q) and kv_lens[s] keys (int32, no more than max_kv), its new tokens' own the last of them."""
+    _check_dev(Q, cu_q, codes, scales, zeros, table, kv_lens, O)
+    t, hq, d = Q.shape
+    pages, hkv, page = _check_cache(codes, scales, zeros, bits, d)
+    b = table.shape[0]
+    assert O.shape == Q.shape and O.dtype == Q.dtype and Q.stride(2) == 1 and O.stride(2) == 1
+    assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
+    assert cu_q.dtype == torch.int32 and cu_q.is_contiguous() and cu_q.numel() == b + 1
+    assert kv_lens.dtype == torch.int32 and kv_lens.is_contiguous() and kv_lens.numel() == b
+    if ws is None:
+        need = ptq_workspace_bytes(OP_PAGED_ATTENTION, hq, d, t, max_kv)
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
+    rc = load_library().ptq_paged_attention(Q.data_ptr(), _dtype_code(Q), Q.stride(0), Q.stride(1), t, hq, d, cu_q.data_ptr(), b,
+                                            int(max_q), codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), pages, page, hkv,
+                                            bits, table.data_ptr(), table.shape[1], kv_lens.data_ptr(), int(max_kv),
+                                            float(softmax_scale), int(bool(causal)), int(window), O.data_ptr(), O.stride(0),
+                                            O.stride(1), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+    if rc:
+        raise PtqError(rc, "ptq_paged_attention")

@@ -177,5 +177,12 @@ ptq_status kv_cache_read_launch(const uint8_t* codes, const float* scales, const
                                 int hkv, int d, int bits, const int32_t* table, int64_t ldt, int64_t b, const int32_t* cu_kv,
                                 int64_t rows, int64_t max_kv, void* K, int64_t k_token, int64_t k_head, void* V,
                                 int64_t v_token, int64_t v_head, ptq_dtype dt, hipStream_t s);
+size_t paged_attention_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t max_kv);
+ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                                  const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                                  const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits,
+                                  const int32_t* table, int64_t ldt, const int32_t* kv_lens, int64_t max_kv,
+                                  double softmax_scale, int causal, int64_t window, void* O, int64_t o_token, int64_t o_head,
+                                  void* ws, hipStream_t s);
 
 }  // namespace ptq

@@ -1,0 +1,419 @@
+// Attention over the paged quantized cache, for up to 16 query rows that share a key head: single tokens, or a few of them.
+//
+//   score_j = softmax_scale ks_j (q . (code_j - zero_j)),   O = sum_j p_j vs_j (code'_j - zero'_j) / sum_j p_j,   p_j = exp(score_j - max)
+//
+// Bound: the cache's bytes, read once.  The 16 columns of the matrix instruction are the query rows of a key head (heads of the
+// group times tokens), so the codes are loaded and made float16 once for all of them.  The context is split over
+// workgroups and over their four waves, 32 keys of a wave at a time, each part with a running maximum; parts meet in LDS, and
+// those of different workgroups in a second kernel.  Nothing is staged: a lane loads the codes that it feeds to the matrix
+// instruction.  Keys: row = lane, d / 4 codes side by side.  Values have to come as eight keys of one channel: a lane takes
+// d / 16 channels of eight keys and transposes them with byte permutes; which channels a row of the instruction stands for
+// is free, and so is the order of keys, which is that in which the scores leave the first product.
+//
+// The value's scale goes into the weight: with vs = mant 2^e, e enters the exponent that the running maximum is taken of, so
+// that the weights that are rounded to float16 are at most 2^8 whatever the scales are (rounding: 2^-11 of a weight, the
+// precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.
+#include <algorithm>
+
+#include "paged_attention.h"
+#include "stored_rows.h"
+
+namespace ptq {
+namespace {
+
+constexpr int kRows = 16, kBlock = 32, kWaves = 4;
+struct __attribute__((packed, aligned(4))) Four { float e[4]; };
+
+template <int BITS, int DP>
+struct Shape {
+  static constexpr int kKeyCodes = DP / 4;                    // of a key, per lane
+  static constexpr int kKeyWords = kKeyCodes * BITS / 32;
+  static constexpr int kValCodes = DP / 16;                   // of a value, per lane
+  static constexpr int kValWords = kValCodes * BITS / 32;     // 0: half a word
+};
+
+// FAST: d == DP and pages of at least four tokens, so that rows of four keys lie side by side
+template <int BITS, int DP, bool FAST>
+__global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) {
+  using S = Shape<BITS, DP>;
+  constexpr int kSteps = DP / 32;      // matrix instructions to a score
+  constexpr int kOut = DP / 16;        // ... to an output
+  extern __shared__ __attribute__((aligned(16))) float smem[];
+  float (*lds_o)[kRows][DP + 4] = reinterpret_cast<float (*)[kRows][DP + 4]>(smem);
+  float (*lds_ml)[kRows][2] = reinterpret_cast<float (*)[kRows][2]>(smem + kWaves * kRows * (DP + 4));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+  const Sequence q = sequence_of(a, seq);
+  const int rows = min(q.queries, a.max_q) * a.group;
+  if (rows == 0) return;
+  const int from = q.begin + split * a.split_keys, to = min(q.end, from + a.split_keys);
+  if (from >= to && split > 0) return;
+
+  // the lane's query row, d as the keys have it: channels [g DP / 4, (g + 1) DP / 4)
+  const int token = q.first + r / a.group, qhead = head * a.group + r % a.group;
+  const bool live = r < rows;
+  f16x8 fq[kSteps];
+  float factor;
+  {
+    float v[kSteps][8], top = 0.f;
+    const uint16_t* Q = a.Q + (live ? token * a.q_token + qhead * a.q_head : 0);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      const int c = g * (DP / 4) + 8 * u;
+      run_to_f32<PTQ_BF16, 8>(load_run<PTQ_BF16, 8, false>(Q, c, a.d), c, live ? a.d : 0, v[u]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = fabsf(v[u][i]);
+        top = fmaxf(top, x < INFINITY ? x : 0.f);
+      }
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    // a power of two of the row's own brings it below 2^15: bfloat16's eight bits are float16's too, but its exponents are not
+    const int e = __builtin_amdgcn_frexp_expf(top);
+    factor = ldexpf(a.scale, e - 15);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, to_f16(ldexpf(v[u][2 * i], 15 - e), ldexpf(v[u][2 * i + 1], 15 - e)));
+      fq[u] = f16x8_of(w[0], w[1], w[2], w[3]);
+    }
+  }
+  int lo, hi;
+  visible(a, q, live ? r / a.group : 0, lo, hi);
+
+  const int64_t plane = (a.c.pages * a.c.heads) << a.c.page_shift;   // rows of the keys, before those of the values
+  const uint8_t* VC = a.c.codes + plane * a.c.row_bytes;
+  const float* VS = a.c.scales + plane;
+  const uint8_t* VZ = a.c.zeros + plane;
+  const int32_t* table = a.table + seq * a.ldt;
+  const int inside = (1 << a.c.page_shift) - 1;
+
+  // what a block of 32 keys needs of the page table (-1: not there), and what the cache holds of it.  Key 4 g + i and 16 + 4 g + i
+  // (i < 4) are the lane's own where scores and values are concerned, key r and 16 + r where it feeds a key's row.
+  struct Pages { int key[2], own[FAST ? 2 : 8]; };
+  struct Block {
+    uint32_t k[2][S::kKeyWords], v[8][S::kValWords > 0 ? S::kValWords : 1];
+    float ks[8], vs[8];
+    uint32_t kz[2], vz[2];
+  };
+  auto page_of = [&](int key) {
+    const int p = table[min(key, q.length - 1) >> a.c.page_shift];
+    return key < to && (uint32_t)p < (uint64_t)a.c.pages ? p : -1;
+  };
+  auto pages_of = [&](int key0) {
+    Pages p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p.key[i] = page_of(key0 + 16 * i + r);
+#pragma unroll
+    for (int i = 0; i < (FAST ? 2 : 8); ++i) p.own[i] = page_of(key0 + (FAST ? 16 * i + 4 * g : 16 * (i >> 2) + 4 * g + (i & 3)));
+    return p;
+  };
+  auto row_of = [&](int page, int key) -> int64_t {
+    return page < 0 ? 0 : ((int64_t)(page * (int64_t)a.c.heads + head) << a.c.page_shift) + (key & inside);
+  };
+  const int vbyte = S::kValWords > 0 ? r * S::kValCodes * BITS / 8 : r * 2;
+  auto fetch = [&](int key0, const Pages& p, Block& b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t row = row_of(p.key[i], key0 + 16 * i + r);
+      const uint8_t* in = a.c.codes + row * a.c.row_bytes;
+      b.kz[i] = a.c.zeros[row];
+      if constexpr (FAST) {
+        const AnyWords<S::kKeyWords, 4> w = *reinterpret_cast<const AnyWords<S::kKeyWords, 4>*>(in + g * (S::kKeyCodes * BITS / 8));
+#pragma unroll
+        for (int j = 0; j < S::kKeyWords; ++j) b.k[i][j] = w.w[j];
+      } else {   // eight codes at a time; those past d meet zeros of the query
+#pragma unroll
+        for (int u = 0; u < kSteps; ++u) {
+          const int c = g * (DP / 4) + 8 * u;
+          const AnyWords<BITS / 4, 4> w = *reinterpret_cast<const AnyWords<BITS / 4, 4>*>(in + (c < a.d ? c * BITS / 8 : 0));
+#pragma unroll
+          for (int j = 0; j < BITS / 4; ++j) b.k[i][u * (BITS / 4) + j] = w.w[j];
+        }
+      }
+    }
+    const int at = vbyte < a.c.row_bytes ? vbyte : 0;
+    auto codes = [&](int i, int64_t row) {
+      const uint8_t* in = VC + row * a.c.row_bytes + at;
+      if constexpr (S::kValWords > 0) {
+        const AnyWords<S::kValWords, 4> w = *reinterpret_cast<const AnyWords<S::kValWords, 4>*>(in);
+#pragma unroll
+        for (int j = 0; j < S::kValWords; ++j) b.v[i][j] = w.w[j];
+      } else {
+        b.v[i][0] = *reinterpret_cast<const uint16_t*>(in);
+      }
+    };
+    if constexpr (FAST) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t row = row_of(p.own[i], key0 + 16 * i + 4 * g);
+        const Four ks = *reinterpret_cast<const Four*>(a.c.scales + row), vs = *reinterpret_cast<const Four*>(VS + row);
+        b.vz[i] = reinterpret_cast<const AnyWords<1, 1>*>(VZ + row)->w[0];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          b.ks[4 * i + j] = ks.e[j];
+          b.vs[4 * i + j] = vs.e[j];
+          codes(4 * i + j, row + j);
+        }
+      }
+    } else {
+      b.vz[0] = b.vz[1] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t row = row_of(p.own[i], key0 + 16 * (i >> 2) + 4 * g + (i & 3));
+        b.ks[i] = a.c.scales[row];
+        b.vs[i] = VS[row];
+        b.vz[i >> 2] |= (uint32_t)VZ[row] << (8 * (i & 3));
+        codes(i, row);
+      }
+    }
+  };
+
+  f32x4 acc[kOut];
+#pragma unroll
+  for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = kNoScore, l = 0.f;
+
+  auto compute = [&](int key0, const Pages& p, const Block& b) {
+    float x[8], mant[8];
+    int e[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t z = b.kz[i] | 0x6400u;
+      const Zeros zz = zeros_of<BITS>(z | (z << 16));
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < kSteps; ++u)
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(row_codes<BITS>(&b.k[i][u * (BITS / 4)], zz), fq[u], s, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[4 * i + j] = s[j];
+    }
+    float top = kNoScore;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int key = key0 + 16 * (i >> 2) + 4 * g + (i & 3);
+      const bool seen = key >= lo && key < hi && p.own[FAST ? i >> 2 : i] >= 0 && key < to;
+      e[i] = __builtin_amdgcn_frexp_expf(b.vs[i]);
+      mant[i] = seen ? __builtin_amdgcn_frexp_mantf(b.vs[i]) : 0.f;
+      x[i] = seen ? fmaf(x[i], b.ks[i] * factor, (float)e[i]) : -INFINITY;
+      top = fmaxf(top, x[i]);
+    }
+    // the maximum moves only when a score is 2^8 above it: until then weights stay small enough
+    if (__any(top > m + 8.f)) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float next = fmaxf(m, top), f = exp2_fast(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < kOut; ++i) acc[i] *= f;
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float p0 = exp2_fast(x[i] - m), p1 = exp2_fast(x[i + 1] - m);
+      l += ldexpf(p0, -e[i]) + ldexpf(p1, -e[i + 1]);
+      w[i >> 1] = __builtin_bit_cast(uint32_t, to_f16(p0 * mant[i], p1 * mant[i + 1]));
+    }
+    const f16x8 weights = f16x8_of(w[0], w[1], w[2], w[3]);
+    // channel by channel: eight keys of it
+    Zeros z[4];
+    z[0] = zeros_of<BITS>(low_bytes(b.vz[0]));
+    z[1] = zeros_of<BITS>(high_bytes(b.vz[0]));
+    z[2] = zeros_of<BITS>(low_bytes(b.vz[1]));
+    z[3] = zeros_of<BITS>(high_bytes(b.vz[1]));
+    if constexpr (BITS == 8) {
+#pragma unroll
+      for (int j = 0; j < S::kValWords; ++j) {
+        uint32_t even[4], odd[4];   // channels 0 and 1 | 2 and 3 of this word, pairs of keys
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          even[k] = perm(b.v[2 * k + 1][j], b.v[2 * k][j], 0x05010400u);
+          odd[k] = perm(b.v[2 * k + 1][j], b.v[2 * k][j], 0x07030602u);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t f[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t pair = c < 2 ? even[k] : odd[k];
+            f[k] = h2_sub(c & 1 ? high_bytes(pair) : low_bytes(pair), z[k].by1);
+          }
+          acc[4 * j + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(f[0], f[1], f[2], f[3]), weights, acc[4 * j + c], 0, 0, 0);
+        }
+      }
+    } else {
+      constexpr int kHalves = S::kValWords > 0 ? 2 * S::kValWords : 1;
+#pragma unroll
+      for (int j = 0; j < kHalves; ++j) {   // a half word: channels 0, 2, 4, 6 or 1, 3, 5, 7 of eight
+        uint32_t f[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t pair = perm(b.v[2 * k + 1][j >> 1], b.v[2 * k][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+          nibble_pairs(pair, z[k], f[k]);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          acc[4 * j + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(f[0][c], f[1][c], f[2][c], f[3][c]), weights, acc[4 * j + c], 0, 0, 0);
+      }
+    }
+  };
+
+  // blocks wave, wave + 4, ...: the next one's codes and the one after's pages are on their way during a block
+  int key0 = from + wave * kBlock;
+  if (key0 < to) {
+    constexpr int kStep = kWaves * kBlock;
+    Pages p0 = pages_of(key0), p1 = pages_of(key0 + kStep);
+    Block b0;
+    fetch(key0, p0, b0);
+    while (true) {
+      Block b1;
+      const Pages p2 = pages_of(key0 + 2 * kStep);
+      fetch(key0 + kStep, p1, b1);
+      compute(key0, p0, b0);
+      key0 += kStep;
+      if (key0 >= to) break;
+      p0 = p1;
+      p1 = p2;
+      b0 = b1;
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+  // the waves' parts meet: row 4 g + i of instruction n is lane 4 g + i's channel n
+#pragma unroll
+  for (int n = 0; n < kOut; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int s = 4 * g + i;
+      int c;
+      if constexpr (BITS == 8) c = s * S::kValCodes + n;
+      else if constexpr (S::kValWords > 0) c = s * S::kValCodes + 8 * (n >> 3) + 2 * (n & 3) + ((n >> 2) & 1);
+      else c = 8 * (s >> 1) + 2 * n + (s & 1);
+      lds_o[wave][r][c] = acc[n][i];
+    }
+  if (g == 0) {
+    lds_ml[wave][r][0] = m;
+    lds_ml[wave][r][1] = l;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * (DP / 4); i += kWaves * 64) {
+    const int row = i / (DP / 4), c = i % (DP / 4) * 4;
+    if (c >= a.d) continue;
+    float top = kNoScore, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][row][0]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = exp2_fast(lds_ml[w][row][0] - top);
+      sum += f * lds_ml[w][row][1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += f * lds_o[w][row][c + j];
+    }
+    const int tok = q.first + row / a.group, h = head * a.group + row % a.group;
+    if (a.splits > 1) {
+      const int64_t at = ((int64_t)split * a.t + tok) * a.hq + h;
+      *reinterpret_cast<f32x4*>(a.part + at * a.d + c) = f32x4{o[0], o[1], o[2], o[3]};
+      if (c == 0) {
+        a.ml[2 * at] = top;
+        a.ml[2 * at + 1] = sum;
+      }
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that sees nothing: zeros
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] *= inv;
+      store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, o);
+    }
+  }
+}
+
+// Adds the splits' parts of a (token, head): a lane has four channels.
+__global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
+  const int tok = blockIdx.x, h = blockIdx.y, c = threadIdx.x * 4;
+  int seq = 0;   // the sequence that the token belongs to
+  for (int n = a.b; n > 1;) {
+    const int half = n >> 1;
+    if (a.cu_q[seq + half] <= tok) seq += half;
+    n -= half;
+  }
+  const Sequence q = sequence_of(a, seq);
+  if (tok < q.first || tok - q.first >= min(q.queries, a.max_q) || c >= a.d) return;
+  const int parts = max(1, min(a.splits, (q.end - q.begin + a.split_keys - 1) / a.split_keys));
+  float top = kNoScore, sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const int64_t first = (int64_t)tok * a.hq + h, step = (int64_t)a.t * a.hq;
+  for (int s = 0; s < parts; ++s) top = fmaxf(top, a.ml[2 * (first + s * step)]);
+  for (int s = 0; s < parts; ++s) {
+    const int64_t at = first + s * step;
+    const float f = exp2_fast(a.ml[2 * at] - top);
+    sum += f * a.ml[2 * at + 1];
+    o += f * *reinterpret_cast<const f32x4*>(a.part + at * a.d + c);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, v);
+}
+
+constexpr int64_t kPartRows = 65536;   // rows times splits at most: what the workspace holds
+
+int64_t most_splits(int64_t rows, int64_t max_kv) {
+  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(max_kv, 256), kPartRows / std::max<int64_t>(rows, 1)));
+}
+
+template <int BITS, int DP, bool FAST>
+bool rows_form_launch(const AttendArgs& a, hipStream_t s) {
+  constexpr int kBytes = kWaves * kRows * (DP + 4 + 2) * (int)sizeof(float);
+  if (!lds_opt_in<attend_rows_kernel<BITS, DP, FAST>>(kBytes)) return false;
+  attend_rows_kernel<BITS, DP, FAST><<<dim3((unsigned)a.splits, (unsigned)a.c.heads, (unsigned)a.b), kWaves * 64, kBytes, s>>>(a);
+  return true;
+}
+template <int BITS, int DP>
+bool rows_launch(const AttendArgs& a, hipStream_t s) {
+  return a.d == DP && a.c.page_shift >= 2 ? rows_form_launch<BITS, DP, true>(a, s) : rows_form_launch<BITS, DP, false>(a, s);
+}
+
+}  // namespace
+
+size_t paged_attention_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
+  const int64_t rows = hq * t, splits = most_splits(rows, max_kv);
+  return splits <= 1 ? 0 : align_up((size_t)(splits * rows * (d + 2)) * sizeof(float), 256);
+}
+
+ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                                  const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                                  const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits,
+                                  const int32_t* table, int64_t ldt, const int32_t* kv_lens, int64_t max_kv,
+                                  double softmax_scale, int causal, int64_t window, void* O, int64_t o_token, int64_t o_head,
+                                  void* ws, hipStream_t s) {
+  AttendArgs a{};
+  a.Q = static_cast<const uint16_t*>(Q);
+  a.O = static_cast<uint16_t*>(O);
+  a.q_token = q_token, a.q_head = q_head, a.o_token = o_token, a.o_head = o_head;
+  a.cu_q = cu_q, a.table = table, a.kv_lens = kv_lens, a.ldt = ldt;
+  a.c = KvCache{const_cast<uint8_t*>(codes), const_cast<float*>(scales), const_cast<uint8_t*>(zeros), pages, (int)hkv,
+                __builtin_ctz((unsigned)page), (int)(d * bits / 8)};
+  a.scale = (float)(softmax_scale * 1.4426950408889634);
+  a.t = (int)t, a.b = (int)b, a.hq = (int)hq, a.group = (int)(hq / hkv), a.d = (int)d, a.max_q = (int)max_q, a.max_kv = (int)max_kv;
+  a.causal = causal, a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
+  const bool rows_form = max_q * a.group <= kRows;
+  // the keys a split has to get through: those in the window, if there is one
+  const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, window + max_q + 63) : max_kv;
+  const int64_t blocks = b * hkv;
+  a.splits = (int)std::min<int64_t>(most_splits(hq * t, max_kv), std::max<int64_t>(1, 2048 / blocks));
+  a.split_keys = (int)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), a.splits), 256) * 256);
+  a.splits = (int)std::max<int64_t>(1, ceil_div(keys, a.split_keys));
+  a.part = static_cast<float*>(ws);
+  a.ml = a.part + (int64_t)a.splits * t * hq * d;
+  if (!rows_form) return PTQ_ERR_SHAPE;
+  const bool launched = bits == 8 ? (d <= 64 ? rows_launch<8, 64>(a, s) : d <= 128 ? rows_launch<8, 128>(a, s) : rows_launch<8, 256>(a, s))
+                                  : (d <= 64 ? rows_launch<4, 64>(a, s) : d <= 128 ? rows_launch<4, 128>(a, s) : rows_launch<4, 256>(a, s));
+  if (!launched) return PTQ_ERR_HIP;
+  if (a.splits > 1) attend_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(a);
+  PTQ_HIP_CHECK_LAUNCH();
+  return PTQ_OK;
+}
+
+}  // namespace ptq

@@ -55,6 +55,7 @@ ptq_status ptq_workspace_bytes(ptq_op op, int64_t m, int64_t n, int64_t t, int64
     case PTQ_OP_SCALED_R1SVD: *bytes = r1svd_workspace_bytes(m, n); return PTQ_OK;
     case PTQ_OP_LINEAR_FORWARD: *bytes = linear_forward_workspace_bytes(t, m, n, block); return PTQ_OK;
     case PTQ_OP_INT8_LINEAR: *bytes = int8_linear_workspace_bytes(m, n, t); return PTQ_OK;
+    case PTQ_OP_PAGED_ATTENTION: *bytes = paged_attention_workspace_bytes(m, n, t, block); return PTQ_OK;
   }
   return PTQ_ERR_ARG;
 }
@@ -374,6 +375,28 @@ ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const ui
   if (!codes || !scales || !zeros || !table || !cu_kv || !K || !V || misaligned(codes, 16)) return PTQ_ERR_ARG;
   return kv_cache_read_launch(codes, scales, zeros, pages, (int)page, (int)hkv, (int)d, bits, table, ldt, b, cu_kv, rows, max_kv, K,
                               k_token, k_head, V, v_token, v_head, dt, static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_paged_attention(const void* Q, ptq_dtype qdt, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                               const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                               const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits, const int32_t* table,
+                               int64_t ldt, const int32_t* kv_lens, int64_t max_kv, double softmax_scale, int causal,
+                               int64_t window, void* O, int64_t o_token, int64_t o_head, void* ws, size_t ws_bytes,
+                               ptq_stream stream) {
+  if (qdt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  const ptq_status bad = kv_cache_bad(hkv, d, bits, pages, page);
+  if (bad != PTQ_OK) return bad;
+  if (!std::isfinite(softmax_scale) || window < 0) return PTQ_ERR_ARG;
+  if (t < 0 || t > (1 << 24) || hq <= 0 || hq > 65535 || hq % hkv != 0 || b < 0 || b > 65535 || max_q < 0 || max_q > t || ldt < 0 ||
+      max_kv < 0 || max_kv > INT32_MAX / 4 || q_token < 0 || q_head < 0 || o_token < 0 || o_head < 0)
+    return PTQ_ERR_SHAPE;
+  if (t == 0 || b == 0 || max_q == 0) return PTQ_OK;
+  if (pages == 0) return PTQ_ERR_SHAPE;
+  if (!Q || !O || Q == O || !cu_q || !codes || !scales || !zeros || !table || !kv_lens || misaligned(codes, 16)) return PTQ_ERR_ARG;
+  if (ws_bad(ws, ws_bytes, paged_attention_workspace_bytes(hq, d, t, max_kv))) return PTQ_ERR_WORKSPACE;
+  return paged_attention_launch(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt,
+                                kv_lens, max_kv, softmax_scale, causal, window, O, o_token, o_head, ws,
+                                static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"
