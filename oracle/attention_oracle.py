@@ -76,7 +76,7 @@ def unpack_row(raw, bits: int):
         return raw.astype(np.int64)
     words = raw.view("<u4").astype(np.int64)[..., None]
     i = np.arange(8)
-    return ((words >> (4 * (i // 2) + 16 * (i % 2))) & 15).reshape(raw.shape[:-1] + (-1,))
+    return ((words >> (4 * (i // 2) + 16 * (i % 2))) & 15).reshape(raw.shape[:-1] + (2 * raw.shape[-1],))
 
 
 def cache_write(K, V, slots, bits: int, codes, scales, zeros):

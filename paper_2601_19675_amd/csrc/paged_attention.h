@@ -108,6 +108,7 @@ __device__ __forceinline__ f16x2 to_f16(float a, float b) {
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+int paged_attention_chunk_rows(int64_t d);   // query rows of a workgroup
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s);
 
 }  // namespace ptq

@@ -401,16 +401,20 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
   const bool rows_form = max_q * a.group <= kRows;
   // the keys a split has to get through: those in the window, if there is one
   const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, window + max_q + 63) : max_kv;
-  const int64_t blocks = b * hkv;
-  a.splits = (int)std::min<int64_t>(most_splits(hq * t, max_kv), std::max<int64_t>(1, 2048 / blocks));
+  const int64_t tiles = rows_form ? 1 : ceil_div(max_q * a.group, paged_attention_chunk_rows(d)), blocks = b * hkv * tiles;
+  a.splits = (int)std::min<int64_t>(most_splits(hq * t, max_kv), std::max<int64_t>(1, (rows_form ? 2048 : 512) / blocks));
   a.split_keys = (int)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), a.splits), 256) * 256);
   a.splits = (int)std::max<int64_t>(1, ceil_div(keys, a.split_keys));
   a.part = static_cast<float*>(ws);
   a.ml = a.part + (int64_t)a.splits * t * hq * d;
-  if (!rows_form) return PTQ_ERR_SHAPE;
-  const bool launched = bits == 8 ? (d <= 64 ? rows_launch<8, 64>(a, s) : d <= 128 ? rows_launch<8, 128>(a, s) : rows_launch<8, 256>(a, s))
-                                  : (d <= 64 ? rows_launch<4, 64>(a, s) : d <= 128 ? rows_launch<4, 128>(a, s) : rows_launch<4, 256>(a, s));
-  if (!launched) return PTQ_ERR_HIP;
+  if (rows_form) {
+    const bool launched = bits == 8 ? (d <= 64 ? rows_launch<8, 64>(a, s) : d <= 128 ? rows_launch<8, 128>(a, s) : rows_launch<8, 256>(a, s))
+                                    : (d <= 64 ? rows_launch<4, 64>(a, s) : d <= 128 ? rows_launch<4, 128>(a, s) : rows_launch<4, 256>(a, s));
+    if (!launched) return PTQ_ERR_HIP;
+  } else {
+    const ptq_status rc = paged_attention_chunk_launch(a, bits, s);
+    if (rc != PTQ_OK) return rc;
+  }
   if (a.splits > 1) attend_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(a);
   PTQ_HIP_CHECK_LAUNCH();
   return PTQ_OK;

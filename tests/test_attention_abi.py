@@ -74,3 +74,21 @@ def test_int8_linear(lib):
     big = dict(t=333, m=4096, n=11008, lda=11008, ldw=11008, ldo=4096)
     assert call(**big) == WORKSPACE and call(**big, ws=P, bytes=need - 1) == WORKSPACE and call(**big, ws=P + 8, bytes=need) == WORKSPACE
     assert ptq.ptq_workspace_bytes(ptq.OP_INT8_LINEAR, 4096, 4096, 1) == 0
+
+
+def test_paged_attention(lib):
+    call = caller(lib.ptq_paged_attention, Q=P, dt=1, qt=256, qh=64, t=4, hq=4, d=64, cu=P, b=2, max_q=3, codes=P, scales=P, zeros=P, pages=8,
+                  page=16, hkv=2, bits=8, table=P, ldt=2, lens=P, max_kv=20, scale=0.125, causal=1, window=0, O=2 * P, ot=256, oh=64,
+                  ws=None, bytes=0, stream=None)
+    assert call(t=0, max_q=0) == OK and call(b=0) == OK and call(max_q=0) == OK
+    assert call(dt=0) == DTYPE and call(dt=2) == DTYPE
+    assert call(bits=2) == ARG and call(scale=float("nan")) == ARG and call(scale=float("inf")) == ARG and call(window=-1) == ARG
+    assert call(d=72) == SHAPE and call(d=272) == SHAPE and call(page=24) == SHAPE and call(hkv=0) == SHAPE and call(pages=0) == SHAPE
+    assert call(hq=3) == SHAPE and call(hq=0) == SHAPE and call(b=65536) == SHAPE and call(max_q=5) == SHAPE and call(max_q=-1) == SHAPE
+    assert call(t=-1) == SHAPE and call(ldt=-1) == SHAPE and call(max_kv=-1) == SHAPE and call(qt=-1) == SHAPE and call(oh=-1) == SHAPE
+    for name in ("Q", "O", "cu", "codes", "scales", "zeros", "table", "lens"):
+        assert call(**{name: None}) == ARG
+    assert call(codes=P + 8) == ARG and call(O=P) == ARG
+    need = ptq.ptq_workspace_bytes(ptq.OP_PAGED_ATTENTION, 4, 64, 4, 5000)
+    assert need > 0 and call(max_kv=5000) == WORKSPACE and call(max_kv=5000, ws=P, bytes=need - 1) == WORKSPACE
+    assert ptq.ptq_workspace_bytes(ptq.OP_PAGED_ATTENTION, 32, 128, 3000, 16384) < 300 << 20
