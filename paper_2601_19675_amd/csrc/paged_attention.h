@@ -1,8 +1,9 @@
 // What the two forms of attention over the paged 8- or 4-bit cache share (paged_attention.hip: single tokens and their
 // kind; paged_attention_chunk.hip: chunks of tokens).  Not part of the C ABI.
 //
-// Codes become float16 whole numbers code - zero, exactly, by arithmetic on bits: the float16 whose bits are 0x6400 | c is
-// 1024 + c.  Products with them are exact, so the grids' scales can stay float32 and outside the matrix instructions.
+// Codes become float16 exactly, by their bits: those of c itself are the float16 c 2^-24 (below float16's normal numbers, which
+// the matrix instructions take as they are), 0x6400 | c is 1024 + c.  Products with them are exact, so the grids' scales can
+// stay float32 and outside the matrix instructions.
 #pragma once
 #include "kv_cache.h"
 

@@ -10,6 +10,12 @@
 // d / 16 channels of eight keys and transposes them with byte permutes; which channels a row of the instruction stands for
 // is free, and so is the order of keys, which is that in which the scores leave the first product.
 //
+// What the vector unit does to a code is what the kernel would be bound by else, so codes go in as c 2^-24 (8 bits: one byte permute to
+// a pair) or 16 c 2^-24 (4 bits: a mask), and the zeros' share is taken out of the sums: q . (c - z) = q . c - z sum q, and
+// sum p (c' - z') = sum p c' - sum p z', the latter one more instruction in the same form, so that codes that equal their zeros
+// give exact zeros.  The instruction sums such small numbers as if they were 2^-14 at least: its sums are good to 2^-21 of
+// the terms for 16 c and for 8 bits (scores), to 2^-17 for the values' channels that come as c of 4 bits.
+//
 // The value's scale goes into the weight: with vs = mant 2^e, e enters the exponent that the running maximum is taken of, so
 // that the weights that are rounded to float16 are at most 2^8 whatever the scales are (rounding: 2^-11 of a weight, the
 // precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.
@@ -32,19 +38,31 @@ struct Shape {
   static constexpr int kValWords = kValCodes * BITS / 32;     // 0: half a word
 };
 
-// FAST: d == DP and pages of at least four tokens, so that rows of four keys lie side by side
-template <int BITS, int DP, bool FAST>
+// eight codes of a key, in order, as c 2^-24 (8 bits) or 16 c 2^-24
+template <int BITS>
+__device__ __forceinline__ f16x8 key_codes(const uint32_t* w) {
+  if constexpr (BITS == 8) {
+    return f16x8_of(perm(0, w[0], 0x0c010c00u), perm(0, w[0], 0x0c030c02u), perm(0, w[1], 0x0c010c00u), perm(0, w[1], 0x0c030c02u));
+  } else {
+    return f16x8_of((w[0] << 4) & 0x00f000f0u, w[0] & 0x00f000f0u, (w[0] >> 4) & 0x00f000f0u, (w[0] >> 8) & 0x00f000f0u);
+  }
+}
+
+// HALVES: pages of 16 tokens and more, so that each half of a block lies in one page, whose number is the wave's (addresses are scalar
+// work); WHOLE: d == DP
+template <int BITS, int DP, bool HALVES, bool WHOLE>
 __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) {
   using S = Shape<BITS, DP>;
   constexpr int kSteps = DP / 32;      // matrix instructions to a score
   constexpr int kOut = DP / 16;        // ... to an output
+  constexpr int kCodeExp = BITS == 8 ? 24 : 20;   // a key's code c goes in as c 2^-kCodeExp
   extern __shared__ __attribute__((aligned(16))) float smem[];
   float (*lds_o)[kRows][DP + 4] = reinterpret_cast<float (*)[kRows][DP + 4]>(smem);
   float (*lds_ml)[kRows][2] = reinterpret_cast<float (*)[kRows][2]>(smem + kWaves * kRows * (DP + 4));
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int split = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
   const Sequence q = sequence_of(a, seq);
-  const int rows = min(q.queries, a.max_q) * a.group;
+  const int queries = min(q.queries, a.max_q), rows = queries * a.group;
   if (rows == 0) return;
   const int from = q.begin + split * a.split_keys, to = min(q.end, from + a.split_keys);
   if (from >= to && split > 0) return;
@@ -53,7 +71,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
   const int token = q.first + r / a.group, qhead = head * a.group + r % a.group;
   const bool live = r < rows;
   f16x8 fq[kSteps];
-  float factor;
+  float factor, qsum = 0.f;
   {
     float v[kSteps][8], top = 0.f;
     const uint16_t* Q = a.Q + (live ? token * a.q_token + qhead * a.q_head : 0);
@@ -71,107 +89,121 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
     top = fmaxf(top, __shfl_xor(top, 32));
     // a power of two of the row's own brings it below 2^15: bfloat16's eight bits are float16's too, but its exponents are not
     const int e = __builtin_amdgcn_frexp_expf(top);
-    factor = ldexpf(a.scale, e - 15);
+    factor = ldexpf(a.scale, e - 15 + kCodeExp);
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) {
       uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, to_f16(ldexpf(v[u][2 * i], 15 - e), ldexpf(v[u][2 * i + 1], 15 - e)));
+      for (int i = 0; i < 4; ++i) {
+        const f16x2 p = to_f16(ldexpf(v[u][2 * i], 15 - e), ldexpf(v[u][2 * i + 1], 15 - e));
+        qsum += (float)p[0] + (float)p[1];
+        w[i] = __builtin_bit_cast(uint32_t, p);
+      }
       fq[u] = f16x8_of(w[0], w[1], w[2], w[3]);
     }
+    qsum += __shfl_xor(qsum, 16);
+    qsum += __shfl_xor(qsum, 32);
+    qsum = ldexpf(qsum, -kCodeExp);
   }
-  int lo, hi;
+  int lo, hi, lo_all, hi_all, unused;   // the row's keys; those that every row sees
   visible(a, q, live ? r / a.group : 0, lo, hi);
+  visible(a, q, 0, unused, hi_all);
+  visible(a, q, queries - 1, lo_all, unused);
+  hi_all = min(hi_all, to);
 
   const int64_t plane = (a.c.pages * a.c.heads) << a.c.page_shift;   // rows of the keys, before those of the values
-  const uint8_t* VC = a.c.codes + plane * a.c.row_bytes;
-  const float* VS = a.c.scales + plane;
-  const uint8_t* VZ = a.c.zeros + plane;
   const int32_t* table = a.table + seq * a.ldt;
-  const int inside = (1 << a.c.page_shift) - 1;
+  const int inside = (1 << a.c.page_shift) - 1, row_bytes = a.c.row_bytes;
 
   // what a block of 32 keys needs of the page table (-1: not there), and what the cache holds of it.  Key 4 g + i and 16 + 4 g + i
   // (i < 4) are the lane's own where scores and values are concerned, key r and 16 + r where it feeds a key's row.
-  struct Pages { int key[2], own[FAST ? 2 : 8]; };
+  struct Pages { int key[2], own[HALVES ? 1 : 8]; };
   struct Block {
     uint32_t k[2][S::kKeyWords], v[8][S::kValWords > 0 ? S::kValWords : 1];
-    float ks[8], vs[8];
+    Four ks[2], vs[2];
     uint32_t kz[2], vz[2];
   };
   auto page_of = [&](int key) {
     const int p = table[min(key, q.length - 1) >> a.c.page_shift];
-    return key < to && (uint32_t)p < (uint64_t)a.c.pages ? p : -1;
+    return ((key < to) & ((uint32_t)p < (uint64_t)a.c.pages)) ? p : -1;
   };
   auto pages_of = [&](int key0) {
     Pages p;
+    if constexpr (HALVES) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p.key[i] = page_of(key0 + 16 * i + r);
+      for (int i = 0; i < 2; ++i) p.key[i] = page_of(key0 + 16 * i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < (FAST ? 2 : 8); ++i) p.own[i] = page_of(key0 + (FAST ? 16 * i + 4 * g : 16 * (i >> 2) + 4 * g + (i & 3)));
+      for (int i = 0; i < 2; ++i) p.key[i] = page_of(key0 + 16 * i + r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p.own[i] = page_of(key0 + 16 * (i >> 2) + 4 * g + (i & 3));
+    }
     return p;
   };
   auto row_of = [&](int page, int key) -> int64_t {
-    return page < 0 ? 0 : ((int64_t)(page * (int64_t)a.c.heads + head) << a.c.page_shift) + (key & inside);
+    return page < 0 ? 0 : (((int64_t)page * a.c.heads + head) << a.c.page_shift) + (key & inside);
   };
-  const int vbyte = S::kValWords > 0 ? r * S::kValCodes * BITS / 8 : r * 2;
-  auto fetch = [&](int key0, const Pages& p, Block& b) {
+  // a lane's part of a row of codes, in bytes
+  const int key_part = g * (S::kKeyCodes * BITS / 8), val_all = S::kValWords > 0 ? r * S::kValCodes * BITS / 8 : r * 2;
+  const int val_part = WHOLE || val_all < row_bytes ? val_all : 0;
+  auto key_load = [&](const uint8_t* in, uint32_t at, uint32_t (&k)[S::kKeyWords]) {
+    if constexpr (WHOLE) {
+      const AnyWords<S::kKeyWords, 4> w = *reinterpret_cast<const AnyWords<S::kKeyWords, 4>*>(in + at + key_part);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t row = row_of(p.key[i], key0 + 16 * i + r);
-      const uint8_t* in = a.c.codes + row * a.c.row_bytes;
-      b.kz[i] = a.c.zeros[row];
-      if constexpr (FAST) {
-        const AnyWords<S::kKeyWords, 4> w = *reinterpret_cast<const AnyWords<S::kKeyWords, 4>*>(in + g * (S::kKeyCodes * BITS / 8));
+      for (int j = 0; j < S::kKeyWords; ++j) k[j] = w.w[j];
+    } else {   // eight codes at a time; those past d meet zeros of the query
 #pragma unroll
-        for (int j = 0; j < S::kKeyWords; ++j) b.k[i][j] = w.w[j];
-      } else {   // eight codes at a time; those past d meet zeros of the query
+      for (int u = 0; u < kSteps; ++u) {
+        const int part = key_part + u * BITS;
+        const AnyWords<BITS / 4, 4> w = *reinterpret_cast<const AnyWords<BITS / 4, 4>*>(in + at + (part < row_bytes ? part : 0));
 #pragma unroll
-        for (int u = 0; u < kSteps; ++u) {
-          const int c = g * (DP / 4) + 8 * u;
-          const AnyWords<BITS / 4, 4> w = *reinterpret_cast<const AnyWords<BITS / 4, 4>*>(in + (c < a.d ? c * BITS / 8 : 0));
-#pragma unroll
-          for (int j = 0; j < BITS / 4; ++j) b.k[i][u * (BITS / 4) + j] = w.w[j];
-        }
+        for (int j = 0; j < BITS / 4; ++j) k[u * (BITS / 4) + j] = w.w[j];
       }
     }
-    const int at = vbyte < a.c.row_bytes ? vbyte : 0;
-    auto codes = [&](int i, int64_t row) {
-      const uint8_t* in = VC + row * a.c.row_bytes + at;
-      if constexpr (S::kValWords > 0) {
-        const AnyWords<S::kValWords, 4> w = *reinterpret_cast<const AnyWords<S::kValWords, 4>*>(in);
+  };
+  auto val_load = [&](const uint8_t* in, uint32_t at, uint32_t (&v)[S::kValWords > 0 ? S::kValWords : 1]) {
+    if constexpr (S::kValWords > 0) {
+      const AnyWords<S::kValWords, 4> w = *reinterpret_cast<const AnyWords<S::kValWords, 4>*>(in + at);
 #pragma unroll
-        for (int j = 0; j < S::kValWords; ++j) b.v[i][j] = w.w[j];
-      } else {
-        b.v[i][0] = *reinterpret_cast<const uint16_t*>(in);
-      }
-    };
-    if constexpr (FAST) {
+      for (int j = 0; j < S::kValWords; ++j) v[j] = w.w[j];
+    } else {
+      v[0] = *reinterpret_cast<const uint16_t*>(in + at);
+    }
+  };
+  auto fetch = [&](int key0, const Pages& p, Block& b) {
+    if constexpr (HALVES) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int64_t row = row_of(p.own[i], key0 + 16 * i + 4 * g);
-        const Four ks = *reinterpret_cast<const Four*>(a.c.scales + row), vs = *reinterpret_cast<const Four*>(VS + row);
-        b.vz[i] = reinterpret_cast<const AnyWords<1, 1>*>(VZ + row)->w[0];
+        const int64_t row = row_of(p.key[i], key0 + 16 * i);
+        const uint8_t* kc = a.c.codes + row * row_bytes;
+        const uint8_t* vc = kc + plane * row_bytes;
+        const float* ks = a.c.scales + row;
+        const uint8_t* kz = a.c.zeros + row;
+        key_load(kc, r * row_bytes, b.k[i]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          b.ks[4 * i + j] = ks.e[j];
-          b.vs[4 * i + j] = vs.e[j];
-          codes(4 * i + j, row + j);
-        }
+        for (int j = 0; j < 4; ++j) val_load(vc + j * row_bytes, 4 * g * row_bytes + val_part, b.v[4 * i + j]);
+        b.ks[i] = *reinterpret_cast<const Four*>(reinterpret_cast<const char*>(ks) + 16u * g);
+        b.vs[i] = *reinterpret_cast<const Four*>(reinterpret_cast<const char*>(ks + plane) + 16u * g);
+        b.kz[i] = reinterpret_cast<const AnyWords<1, 1>*>(kz + 4u * g)->w[0];
+        b.vz[i] = reinterpret_cast<const AnyWords<1, 1>*>(kz + plane + 4u * g)->w[0];
       }
     } else {
-      b.vz[0] = b.vz[1] = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) key_load(a.c.codes + row_of(p.key[i], key0 + 16 * i + r) * row_bytes, 0, b.k[i]);
+      b.kz[0] = b.kz[1] = b.vz[0] = b.vz[1] = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int64_t row = row_of(p.own[i], key0 + 16 * (i >> 2) + 4 * g + (i & 3));
-        b.ks[i] = a.c.scales[row];
-        b.vs[i] = VS[row];
-        b.vz[i >> 2] |= (uint32_t)VZ[row] << (8 * (i & 3));
-        codes(i, row);
+        b.ks[i >> 2].e[i & 3] = a.c.scales[row];
+        b.vs[i >> 2].e[i & 3] = a.c.scales[plane + row];
+        b.kz[i >> 2] |= (uint32_t)a.c.zeros[row] << (8 * (i & 3));
+        b.vz[i >> 2] |= (uint32_t)a.c.zeros[plane + row] << (8 * (i & 3));
+        val_load(a.c.codes + (plane + row) * row_bytes, val_part, b.v[i]);
       }
     }
   };
 
-  f32x4 acc[kOut];
+  f32x4 acc[kOut], acc_z[BITS == 8 ? 1 : 2] = {};   // (4 bits: for channels as c 2^-24, and as 16 c 2^-24)
 #pragma unroll
   for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = kNoScore, l = 0.f;
@@ -181,25 +213,33 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
     int e[8];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint32_t z = b.kz[i] | 0x6400u;
-      const Zeros zz = zeros_of<BITS>(z | (z << 16));
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < kSteps; ++u)
-        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(row_codes<BITS>(&b.k[i][u * (BITS / 4)], zz), fq[u], s, 0, 0, 0);
+        s = __builtin_amdgcn_mfma_f32_16x16x32_f16(key_codes<BITS>(&b.k[i][u * (BITS / 4)]), fq[u], s, 0, 0, 0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = s[j];
+      for (int j = 0; j < 4; ++j) {
+        const int n = 4 * i + j;
+        const float vs = b.vs[i].e[j];
+        e[n] = __builtin_amdgcn_frexp_expf(vs);
+        mant[n] = __builtin_amdgcn_frexp_mantf(vs);
+        x[n] = fmaf(fmaf(-(float)((b.kz[i] >> (8 * j)) & 255u), qsum, s[j]), b.ks[i].e[j] * factor, (float)e[n]);
+      }
+    }
+    bool all = (key0 >= lo_all) & (key0 + kBlock <= hi_all);
+    if constexpr (HALVES) all &= (p.key[0] >= 0) & (p.key[1] >= 0);
+    if (!HALVES || !all) {   // some row does not see some key
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = key0 + 16 * (i >> 2) + 4 * g + (i & 3);
+        const bool seen = (key >= lo) & (key < min(hi, to)) & ((HALVES ? p.key[i >> 2] : p.own[HALVES ? 0 : i]) >= 0);
+        mant[i] = seen ? mant[i] : 0.f;
+        x[i] = seen ? x[i] : -INFINITY;
+      }
     }
     float top = kNoScore;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int key = key0 + 16 * (i >> 2) + 4 * g + (i & 3);
-      const bool seen = key >= lo && key < hi && p.own[FAST ? i >> 2 : i] >= 0 && key < to;
-      e[i] = __builtin_amdgcn_frexp_expf(b.vs[i]);
-      mant[i] = seen ? __builtin_amdgcn_frexp_mantf(b.vs[i]) : 0.f;
-      x[i] = seen ? fmaf(x[i], b.ks[i] * factor, (float)e[i]) : -INFINITY;
-      top = fmaxf(top, x[i]);
-    }
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
     // the maximum moves only when a score is 2^8 above it: until then weights stay small enough
     if (__any(top > m + 8.f)) {
       top = fmaxf(top, __shfl_xor(top, 16));
@@ -207,6 +247,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
       const float next = fmaxf(m, top), f = exp2_fast(m - next);
       m = next;
       l *= f;
+#pragma unroll
+      for (f32x4& z : acc_z) z *= f;
 #pragma unroll
       for (int i = 0; i < kOut; ++i) acc[i] *= f;
     }
@@ -218,41 +260,35 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
       w[i >> 1] = __builtin_bit_cast(uint32_t, to_f16(p0 * mant[i], p1 * mant[i + 1]));
     }
     const f16x8 weights = f16x8_of(w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int n = 0; n < (BITS == 8 ? 1 : 2); ++n) {
+      const uint32_t z0 = b.vz[0] << (4 * n), z1 = b.vz[1] << (4 * n);
+      acc_z[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(perm(0, z0, 0x0c010c00u), perm(0, z0, 0x0c030c02u), perm(0, z1, 0x0c010c00u),
+                                                                 perm(0, z1, 0x0c030c02u)), weights, acc_z[n], 0, 0, 0);
+    }
     // channel by channel: eight keys of it
-    Zeros z[4];
-    z[0] = zeros_of<BITS>(low_bytes(b.vz[0]));
-    z[1] = zeros_of<BITS>(high_bytes(b.vz[0]));
-    z[2] = zeros_of<BITS>(low_bytes(b.vz[1]));
-    z[3] = zeros_of<BITS>(high_bytes(b.vz[1]));
     if constexpr (BITS == 8) {
 #pragma unroll
-      for (int j = 0; j < S::kValWords; ++j) {
-        uint32_t even[4], odd[4];   // channels 0 and 1 | 2 and 3 of this word, pairs of keys
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          even[k] = perm(b.v[2 * k + 1][j], b.v[2 * k][j], 0x05010400u);
-          odd[k] = perm(b.v[2 * k + 1][j], b.v[2 * k][j], 0x07030602u);
-        }
+      for (int j = 0; j < S::kValWords; ++j)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t f[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t pair = c < 2 ? even[k] : odd[k];
-            f[k] = h2_sub(c & 1 ? high_bytes(pair) : low_bytes(pair), z[k].by1);
-          }
+          for (int k = 0; k < 4; ++k) f[k] = perm(b.v[2 * k + 1][j], b.v[2 * k][j], 0x0c040c00u + 0x00010001u * c);
           acc[4 * j + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16x8_of(f[0], f[1], f[2], f[3]), weights, acc[4 * j + c], 0, 0, 0);
         }
-      }
     } else {
       constexpr int kHalves = S::kValWords > 0 ? 2 * S::kValWords : 1;
 #pragma unroll
-      for (int j = 0; j < kHalves; ++j) {   // a half word: channels 0, 2, 4, 6 or 1, 3, 5, 7 of eight
+      for (int j = 0; j < kHalves; ++j) {   // a half word: channels 0, 2, 4, 6 or 1, 3, 5, 7 of eight, the second and fourth 16-fold
         uint32_t f[4][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t pair = perm(b.v[2 * k + 1][j >> 1], b.v[2 * k][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-          nibble_pairs(pair, z[k], f[k]);
+          const uint32_t pair = perm(b.v[2 * k + 1][j >> 1], b.v[2 * k][j >> 1], j & 1 ? 0x07060302u : 0x05040100u), u = pair >> 8;
+          f[k][0] = pair & 0x000f000fu;
+          f[k][1] = pair & 0x00f000f0u;
+          f[k][2] = u & 0x000f000fu;
+          f[k][3] = u & 0x00f000f0u;
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -266,18 +302,20 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
   if (key0 < to) {
     constexpr int kStep = kWaves * kBlock;
     Pages p0 = pages_of(key0), p1 = pages_of(key0 + kStep);
-    Block b0;
+    Block b0, b1;
     fetch(key0, p0, b0);
     while (true) {
-      Block b1;
-      const Pages p2 = pages_of(key0 + 2 * kStep);
+      Pages p2 = pages_of(key0 + 2 * kStep);
       fetch(key0 + kStep, p1, b1);
       compute(key0, p0, b0);
-      key0 += kStep;
+      if (key0 + kStep >= to) break;
+      p0 = pages_of(key0 + 3 * kStep);
+      fetch(key0 + 2 * kStep, p2, b0);
+      compute(key0 + kStep, p1, b1);
+      key0 += 2 * kStep;
       if (key0 >= to) break;
-      p0 = p1;
-      p1 = p2;
-      b0 = b1;
+      p1 = p0;
+      p0 = p2;
     }
   }
   l += __shfl_xor(l, 16);
@@ -293,7 +331,7 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
       if constexpr (BITS == 8) c = s * S::kValCodes + n;
       else if constexpr (S::kValWords > 0) c = s * S::kValCodes + 8 * (n >> 3) + 2 * (n & 3) + ((n >> 2) & 1);
       else c = 8 * (s >> 1) + 2 * n + (s & 1);
-      lds_o[wave][r][c] = acc[n][i];
+      lds_o[wave][r][c] = BITS == 4 && (n & 1) ? (acc[n][i] - acc_z[BITS == 8 ? 0 : 1][i]) * 0x1p20f : (acc[n][i] - acc_z[0][i]) * 0x1p24f;
     }
   if (g == 0) {
     lds_ml[wave][r][0] = m;
@@ -363,16 +401,17 @@ int64_t most_splits(int64_t rows, int64_t max_kv) {
   return std::max<int64_t>(1, std::min<int64_t>(ceil_div(max_kv, 256), kPartRows / std::max<int64_t>(rows, 1)));
 }
 
-template <int BITS, int DP, bool FAST>
+template <int BITS, int DP, bool HALVES, bool WHOLE>
 bool rows_form_launch(const AttendArgs& a, hipStream_t s) {
   constexpr int kBytes = kWaves * kRows * (DP + 4 + 2) * (int)sizeof(float);
-  if (!lds_opt_in<attend_rows_kernel<BITS, DP, FAST>>(kBytes)) return false;
-  attend_rows_kernel<BITS, DP, FAST><<<dim3((unsigned)a.splits, (unsigned)a.c.heads, (unsigned)a.b), kWaves * 64, kBytes, s>>>(a);
+  if (!lds_opt_in<attend_rows_kernel<BITS, DP, HALVES, WHOLE>>(kBytes)) return false;
+  attend_rows_kernel<BITS, DP, HALVES, WHOLE><<<dim3((unsigned)a.splits, (unsigned)a.c.heads, (unsigned)a.b), kWaves * 64, kBytes, s>>>(a);
   return true;
 }
 template <int BITS, int DP>
 bool rows_launch(const AttendArgs& a, hipStream_t s) {
-  return a.d == DP && a.c.page_shift >= 2 ? rows_form_launch<BITS, DP, true>(a, s) : rows_form_launch<BITS, DP, false>(a, s);
+  if (a.c.page_shift < 4) return rows_form_launch<BITS, DP, false, false>(a, s);
+  return a.d == DP ? rows_form_launch<BITS, DP, true, true>(a, s) : rows_form_launch<BITS, DP, true, false>(a, s);
 }
 
 }  // namespace
