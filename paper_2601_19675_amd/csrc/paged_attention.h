@@ -27,8 +27,10 @@ struct AttendArgs {
   float scale;                           // softmax_scale log2(e): scores are powers of two
   int t, b, hq, group, d, max_q, max_kv, causal, window;
   int splits, split_keys;                // splits > 1: partial results go to part and ml
-  float* part;                           // [split][token][head][d]: sums of weight times value
-  float* ml;                             // [split][token][head][2]: the maximum they are relative to, the sum of the weights
+  int least_share;                       // rows form: blocks of 128 keys that a workgroup takes at least
+  float* part;                           // [part][token][head][d]: sums of weight times value
+  float* ml;                             // [part][token][head][2]: the maximum they are relative to, the sum of the weights
+  int* parts;                            // rows form: [token], how many there are
 };
 
 // a sequence's queries and keys

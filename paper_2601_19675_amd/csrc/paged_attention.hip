@@ -3,10 +3,11 @@
 //   score_j = softmax_scale ks_j (q . (code_j - zero_j)),   O = sum_j p_j vs_j (code'_j - zero'_j) / sum_j p_j,   p_j = exp(score_j - max)
 //
 // Bound: the cache's bytes, read once.  The 16 columns of the matrix instruction are the query rows of a key head (heads of the
-// group times tokens), so the codes are loaded and made float16 once for all of them.  The context is split over
-// workgroups and over their four waves, 32 keys of a wave at a time, each part with a running maximum; parts meet in LDS, and
-// those of different workgroups in a second kernel.  Nothing is staged: a lane loads the codes that it feeds to the matrix
-// instruction.  Keys: row = lane, d / 4 codes side by side.  Values have to come as eight keys of one channel: a lane takes
+// group times tokens), so the codes are loaded and made float16 once for all of them.  A workgroup's four waves share out
+// its keys, 32 of a wave at a time, each with a running maximum, and meet in LDS.  Where there is more to do than a wave of workgroups
+// per sequence and key head would share evenly, the contexts of all sequences are laid end to end (128 keys a block) and dealt out in
+// equal shares, two workgroups to a compute unit; what a sequence got from several workgroups meets in a second kernel.
+// Nothing is staged: a lane loads the codes that it feeds to the matrix instruction.  Keys: row = lane, d / 4 codes side by side.  Values have to come as eight keys of one channel: a lane takes
 // d / 16 channels of eight keys and transposes them with byte permutes; which channels a row of the instruction stands for
 // is free, and so is the order of keys, which is that in which the scores leave the first product.
 //
@@ -21,13 +22,19 @@
 // precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.
 #include <algorithm>
 
+#include "lds_dma.h"
 #include "paged_attention.h"
 #include "stored_rows.h"
 
 namespace ptq {
 namespace {
 
-constexpr int kRows = 16, kBlock = 32, kWaves = 4;
+constexpr int kRows = 16, kBlock = 32, kWaves = 4, kShareBlock = kWaves * kBlock;
+
+// blocks that a sequence counts for in the shares: one at least, if it has queries (somebody has to write their zeros)
+__device__ __forceinline__ int share_blocks(const AttendArgs& a, const Sequence& q) {
+  return q.queries == 0 ? 0 : max(1, (q.end - q.begin + kShareBlock - 1) / kShareBlock);
+}
 struct __attribute__((packed, aligned(4))) Four { float e[4]; };
 
 template <int BITS, int DP>
@@ -51,7 +58,7 @@ __device__ __forceinline__ f16x8 key_codes(const uint32_t* w) {
 // HALVES: pages of 16 tokens and more, so that each half of a block lies in one page, whose number is the wave's (addresses are scalar
 // work); WHOLE: d == DP
 template <int BITS, int DP, bool HALVES, bool WHOLE>
-__global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   using S = Shape<BITS, DP>;
   constexpr int kSteps = DP / 32;      // matrix instructions to a score
   constexpr int kOut = DP / 16;        // ... to an output
@@ -60,12 +67,52 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
   float (*lds_o)[kRows][DP + 4] = reinterpret_cast<float (*)[kRows][DP + 4]>(smem);
   float (*lds_ml)[kRows][2] = reinterpret_cast<float (*)[kRows][2]>(smem + kWaves * kRows * (DP + 4));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x, head = blockIdx.y, seq = blockIdx.z;
+  const int head = blockIdx.y;
+  // the workgroup's share: blocks [off, off + left) of sequence seq and on, `before` blocks before that sequence
+  int seq = blockIdx.z, off = 0;
+  int before = 0, share = 1, left = INT32_MAX;
+  if (a.splits > 1) {
+    int total = 0;
+    for (int s0 = 0; s0 < a.b; s0 += kWave) total += s0 + lane < a.b ? share_blocks(a, sequence_of(a, s0 + lane)) : 0;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o);
+    total = __builtin_amdgcn_readfirstlane(total);
+    share = max(a.least_share, (int)((total + gridDim.x - 1) / gridDim.x));
+    const int64_t mine = (int64_t)blockIdx.x * share;
+    if (mine >= total) return;
+    left = min(share, total - (int)mine);
+    for (int s0 = 0;; s0 += kWave) {   // the first sequence that reaches past `mine`
+      const int n = s0 + lane < a.b ? share_blocks(a, sequence_of(a, s0 + lane)) : 0;
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+      }
+      const uint64_t past = __ballot(before + upto > mine);
+      if (past) {
+        const int s = __builtin_ctzll(past);
+        seq = s0 + s;
+        before += __builtin_amdgcn_readlane(upto, s) - __builtin_amdgcn_readlane(n, s);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    off = (int)mine - before;
+  }
+
+  for (;; ++seq) {
+  if (seq >= a.b) return;
   const Sequence q = sequence_of(a, seq);
   const int queries = min(q.queries, a.max_q), rows = queries * a.group;
-  if (rows == 0) return;
-  const int from = q.begin + split * a.split_keys, to = min(q.end, from + a.split_keys);
-  if (from >= to && split > 0) return;
+  if (rows == 0) {
+    if (a.splits == 1) return;
+    continue;
+  }
+  const int blocks = share_blocks(a, q), take = min(blocks - off, left);
+  const int from = q.begin + off * kShareBlock, to = min(q.end, from + take * kShareBlock);
+  const bool alone = take == blocks;   // nobody else has keys of this sequence
+  const int part = alone ? 0 : (int)blockIdx.x - before / share;
 
   // the lane's query row, d as the keys have it: channels [g DP / 4, (g + 1) DP / 4)
   const int token = q.first + r / a.group, qhead = head * a.group + r % a.group;
@@ -297,25 +344,29 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
     }
   };
 
-  // blocks wave, wave + 4, ...: the next one's codes and the one after's pages are on their way during a block
+  // blocks wave, wave + 4, ...: the next one's codes and the page numbers of the one after are on their way during a block (two blocks'
+  // codes, where the registers hold them, brought nothing)
   int key0 = from + wave * kBlock;
   if (key0 < to) {
-    constexpr int kStep = kWaves * kBlock;
-    Pages p0 = pages_of(key0), p1 = pages_of(key0 + kStep);
-    Block b0, b1;
-    fetch(key0, p0, b0);
-    while (true) {
-      Pages p2 = pages_of(key0 + 2 * kStep);
-      fetch(key0 + kStep, p1, b1);
-      compute(key0, p0, b0);
-      if (key0 + kStep >= to) break;
-      p0 = pages_of(key0 + 3 * kStep);
-      fetch(key0 + 2 * kStep, p2, b0);
-      compute(key0 + kStep, p1, b1);
-      key0 += 2 * kStep;
-      if (key0 >= to) break;
-      p1 = p0;
-      p0 = p2;
+    constexpr int kStep = kWaves * kBlock, kAhead = 1, kBuffers = kAhead + 1;
+    Pages p[kBuffers + 1];
+    Block b[kBuffers];
+#pragma unroll
+    for (int i = 0; i <= kAhead; ++i) p[i] = pages_of(key0 + i * kStep);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(key0 + i * kStep, p[i], b[i]);
+    bool more = true;
+    while (more) {
+      static_for<kBuffers>([&](auto i_) {
+        constexpr int i = decltype(i_)::value;
+        if (!more) return;
+        p[kBuffers] = pages_of(key0 + kBuffers * kStep);
+        fetch(key0 + kAhead * kStep, p[(i + kAhead) % kBuffers], b[(i + kAhead) % kBuffers]);
+        compute(key0, p[i], b[i]);
+        p[i] = p[kBuffers];
+        key0 += kStep;
+        more = key0 < to;
+      });
     }
   }
   l += __shfl_xor(l, 16);
@@ -352,8 +403,8 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
       for (int j = 0; j < 4; ++j) o[j] += f * lds_o[w][row][c + j];
     }
     const int tok = q.first + row / a.group, h = head * a.group + row % a.group;
-    if (a.splits > 1) {
-      const int64_t at = ((int64_t)split * a.t + tok) * a.hq + h;
+    if (!alone) {
+      const int64_t at = ((int64_t)part * a.t + tok) * a.hq + h;
       *reinterpret_cast<f32x4*>(a.part + at * a.d + c) = f32x4{o[0], o[1], o[2], o[3]};
       if (c == 0) {
         a.ml[2 * at] = top;
@@ -366,11 +417,22 @@ __global__ __launch_bounds__(kWaves * 64) void attend_rows_kernel(AttendArgs a) 
       store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, o);
     }
   }
+  if (a.splits == 1) return;
+  if (off == 0 && head == 0) {
+    const int parts = alone ? 1 : (before + blocks - 1) / share - before / share + 1;
+    for (int i = threadIdx.x; i < queries; i += kWaves * 64) a.parts[q.first + i] = parts;
+  }
+  left -= take;
+  if (left <= 0) return;
+  before += blocks;
+  off = 0;
+  __syncthreads();   // the next sequence's parts go where this one's were
+  }
 }
 
-// Adds the splits' parts of a (token, head): a lane has four channels.
+// Adds the splits' parts of a (token, head): a lane looks at one part's maximum and sum, and has four channels of all parts.
 __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
-  const int tok = blockIdx.x, h = blockIdx.y, c = threadIdx.x * 4;
+  const int tok = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, c = lane * 4;
   int seq = 0;   // the sequence that the token belongs to
   for (int n = a.b; n > 1;) {
     const int half = n >> 1;
@@ -378,18 +440,32 @@ __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
     n -= half;
   }
   const Sequence q = sequence_of(a, seq);
-  if (tok < q.first || tok - q.first >= min(q.queries, a.max_q) || c >= a.d) return;
-  const int parts = max(1, min(a.splits, (q.end - q.begin + a.split_keys - 1) / a.split_keys));
-  float top = kNoScore, sum = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (tok < q.first || tok - q.first >= min(q.queries, a.max_q)) return;
+  const int parts = a.parts ? a.parts[tok] : max(1, min(a.splits, (q.end - q.begin + a.split_keys - 1) / a.split_keys));
+  if (a.parts && parts == 1) return;   // written by the one workgroup that had it
   const int64_t first = (int64_t)tok * a.hq + h, step = (int64_t)a.t * a.hq;
-  for (int s = 0; s < parts; ++s) top = fmaxf(top, a.ml[2 * (first + s * step)]);
-  for (int s = 0; s < parts; ++s) {
-    const int64_t at = first + s * step;
-    const float f = exp2_fast(a.ml[2 * at] - top);
-    sum += f * a.ml[2 * at + 1];
-    o += f * *reinterpret_cast<const f32x4*>(a.part + at * a.d + c);
+  float top = kNoScore, sum = 0.f;
+  for (int s = lane; s < parts; s += 64) top = fmaxf(top, a.ml[2 * (first + s * step)]);
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const float* part = a.part + first * a.d + (c < a.d ? c : 0);
+  for (int s0 = 0; s0 < parts; s0 += 64) {
+    const int s = min(s0 + lane, parts - 1);
+    const float f = s0 + lane < parts ? exp2_fast(a.ml[2 * (first + s * step)] - top) : 0.f;
+    sum += f * a.ml[2 * (first + s * step) + 1];
+    const int here = min(64, parts - s0);
+    for (int i = 0; i < here; i += 8) {   // (f is 0 past the last part)
+      f32x4 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const f32x4*>(part + (s0 + min(i + j, here - 1)) * step * a.d);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o += __shfl(f, i + j) * v[j];
+    }
   }
+#pragma unroll
+  for (int n = 1; n < kWave; n <<= 1) sum += __shfl_xor(sum, n);
+  if (c >= a.d) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, v);
@@ -401,11 +477,15 @@ int64_t most_splits(int64_t rows, int64_t max_kv) {
   return std::max<int64_t>(1, std::min<int64_t>(ceil_div(max_kv, 256), kPartRows / std::max<int64_t>(rows, 1)));
 }
 
+constexpr int kShares = 512;          // workgroups that share the contexts: two to a compute unit
+int64_t shares(int64_t hkv) { return std::max<int64_t>(1, kShares / hkv); }
+
 template <int BITS, int DP, bool HALVES, bool WHOLE>
 bool rows_form_launch(const AttendArgs& a, hipStream_t s) {
   constexpr int kBytes = kWaves * kRows * (DP + 4 + 2) * (int)sizeof(float);
   if (!lds_opt_in<attend_rows_kernel<BITS, DP, HALVES, WHOLE>>(kBytes)) return false;
-  attend_rows_kernel<BITS, DP, HALVES, WHOLE><<<dim3((unsigned)a.splits, (unsigned)a.c.heads, (unsigned)a.b), kWaves * 64, kBytes, s>>>(a);
+  const dim3 grid = a.splits > 1 ? dim3((unsigned)shares(a.c.heads), (unsigned)a.c.heads, 1) : dim3(1, (unsigned)a.c.heads, (unsigned)a.b);
+  attend_rows_kernel<BITS, DP, HALVES, WHOLE><<<grid, kWaves * 64, kBytes, s>>>(a);
   return true;
 }
 template <int BITS, int DP>
@@ -418,7 +498,7 @@ bool rows_launch(const AttendArgs& a, hipStream_t s) {
 
 size_t paged_attention_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
   const int64_t rows = hq * t, splits = most_splits(rows, max_kv);
-  return splits <= 1 ? 0 : align_up((size_t)(splits * rows * (d + 2)) * sizeof(float), 256);
+  return splits <= 1 ? 0 : align_up((size_t)(splits * rows * (d + 2) + t) * sizeof(float), 256);
 }
 
 ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
@@ -440,12 +520,22 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
   const bool rows_form = max_q * a.group <= kRows;
   // the keys a split has to get through: those in the window, if there is one
   const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, window + max_q + 63) : max_kv;
-  const int64_t tiles = rows_form ? 1 : ceil_div(max_q * a.group, paged_attention_chunk_rows(d)), blocks = b * hkv * tiles;
-  a.splits = (int)std::min<int64_t>(most_splits(hq * t, max_kv), std::max<int64_t>(1, (rows_form ? 2048 : 512) / blocks));
-  a.split_keys = (int)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), a.splits), 256) * 256);
-  a.splits = (int)std::max<int64_t>(1, ceil_div(keys, a.split_keys));
+  const int64_t most = most_splits(hq * t, max_kv);
+  if (rows_form) {
+    // Shares cost a second kernel and its launch (4 us), which 2048 keys in one workgroup take (6 us from 256 keys on): shorter contexts
+    // stay whole, and so do more sequences and heads than four rounds of workgroups.
+    a.splits = keys < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)most;
+    // 512 keys at least to a share, and a sequence's parts fit the workspace
+    a.least_share = a.splits > 1 ? (int)std::max<int64_t>(4, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
+  } else {
+    const int64_t blocks = b * hkv * ceil_div(max_q * a.group, paged_attention_chunk_rows(d));
+    a.splits = (int)std::min<int64_t>(most, std::max<int64_t>(1, 512 / blocks));
+    a.split_keys = (int)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), a.splits), 256) * 256);
+    a.splits = (int)std::max<int64_t>(1, ceil_div(keys, a.split_keys));
+  }
   a.part = static_cast<float*>(ws);
   a.ml = a.part + (int64_t)a.splits * t * hq * d;
+  a.parts = rows_form ? reinterpret_cast<int*>(a.ml + (int64_t)a.splits * t * hq * 2) : nullptr;
   if (rows_form) {
     const bool launched = bits == 8 ? (d <= 64 ? rows_launch<8, 64>(a, s) : d <= 128 ? rows_launch<8, 128>(a, s) : rows_launch<8, 256>(a, s))
                                     : (d <= 64 ? rows_launch<4, 64>(a, s) : d <= 128 ? rows_launch<4, 128>(a, s) : rows_launch<4, 256>(a, s));

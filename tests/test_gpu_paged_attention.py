@@ -194,3 +194,13 @@ def test_sequences_that_do_not_fit_are_left_out():
     p.cu[3] = 9   # past the tokens there are
     O = p.run(O=torch.full_like(ok, 5.0))
     assert torch.equal(O[:2], ok[:2]) and (O[2] == 5.0).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d,bits,page,window", [(4, 2, 64, 4, 16, 0), (8, 8, 128, 8, 64, 0), (16, 1, 64, 8, 1, 0), (8, 2, 64, 8, 16, 2100)])
+def test_contexts_of_many_sequences_are_dealt_out(hq, hkv, d, bits, page, window):
+    # more sequences than a wave looks at together, some without queries or keys, shares that end anywhere
+    g = np.random.default_rng(hq + d)
+    kv = [int(c) for c in np.exp(g.uniform(0, np.log(5000), 69))] + [0, 6000, 1, 0]
+    new = [1] * len(kv)
+    new[5] = new[40] = new[71] = 0
+    Problem(kv, new, hq, hkv, d, bits, page, seed=hq).check(True, window, absolute=True)
