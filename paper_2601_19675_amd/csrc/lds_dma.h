@@ -6,10 +6,8 @@
 // address from it, five between a vector instruction that writes a scalar register (readfirstlane) and a request that has it
 // in its descriptor or offset.  build.py checks both on the generated assembly.
 #pragma once
-#include <type_traits>
-#include <utility>
-
 #include "common.h"
+#include "static_for.h"
 
 namespace ptq {
 
@@ -62,16 +60,6 @@ __device__ __forceinline__ void request_to_lds_at(i32x4 rsrc, uint32_t voff, uin
 template <int N>
 __device__ __forceinline__ void wait_requests() {
   __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x0f70);
-}
-
-// f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>)
-template <class F, int... Is>
-__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, Is...>) {
-  (f(std::integral_constant<int, Is>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void static_for(F&& f) {
-  static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
 
 }  // namespace ptq

@@ -22,8 +22,8 @@
 // precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.
 #include <algorithm>
 
-#include "lds_dma.h"
 #include "paged_attention.h"
+#include "static_for.h"
 #include "stored_rows.h"
 
 namespace ptq {

@@ -69,9 +69,9 @@ def test_int8_linear(lib):
     for name in ("A", "asc", "W", "wsc", "O"):
         assert call(**{name: None}) == ARG
     assert call(A=P + 8) == ARG and call(W=P + 4) == ARG
-    need = ptq.ptq_workspace_bytes(ptq.OP_INT8_LINEAR, 4096, 11008, 333)
+    need = ptq.ptq_workspace_bytes(ptq.OP_INT8_LINEAR, 1000, 11008, 100)   # a size whose sums are split
     assert need > 0
-    big = dict(t=333, m=4096, n=11008, lda=11008, ldw=11008, ldo=4096)
+    big = dict(t=100, m=1000, n=11008, lda=11008, ldw=11008, ldo=1000)
     assert call(**big) == WORKSPACE and call(**big, ws=P, bytes=need - 1) == WORKSPACE and call(**big, ws=P + 8, bytes=need) == WORKSPACE
     assert ptq.ptq_workspace_bytes(ptq.OP_INT8_LINEAR, 4096, 4096, 1) == 0
 
