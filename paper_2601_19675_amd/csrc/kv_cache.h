@@ -15,15 +15,17 @@ struct KvCache {
   int heads, page_shift, row_bytes;
 };
 
-// row of (keys 0 or values 1, page, head, place in the page): an index into scales and zeros, times row_bytes into codes
-__device__ __forceinline__ int64_t kv_row(const KvCache& c, int which, int64_t page, int head, int offset) {
-  return ((((int64_t)which * c.pages + page) * c.heads + head) << c.page_shift) + offset;
+// Rows of one head, keys (0) or values (1): place `offset` of a page is row first + page * per_page + offset, an index into scales and
+// zeros, times row_bytes into codes.
+struct KvRows {
+  int64_t first;
+  uint32_t per_page;
+};
+__device__ __forceinline__ KvRows kv_rows(const KvCache& c, int which, int head) {
+  return KvRows{((int64_t)which * c.pages * c.heads + head) << c.page_shift, (uint32_t)c.heads << c.page_shift};
 }
-
-// one operand of a lane exchange inside 16 lanes (see dpp_move)
-template <int CTRL>
-__device__ __forceinline__ float dpp_move_f32(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+__device__ __forceinline__ int64_t kv_row(const KvRows& r, uint32_t page, uint32_t offset) {
+  return r.first + (int64_t)((uint64_t)page * r.per_page + offset);
 }
 
 }  // namespace ptq

@@ -7,6 +7,7 @@
 // d / 8 lanes.  The division that gives the scale is in float64, as the definition has it: the grid's width may need more
 // than 24 bits.
 #include "kv_cache.h"
+#include "static_for.h"
 #include "stored_rows.h"
 
 namespace ptq {
@@ -22,16 +23,21 @@ struct WriteArgs {
   KvCache c;
 };
 
-// min or max over the LANES lanes of a row
-template <int LANES, bool MAX>
-__device__ __forceinline__ float row_extreme(float v) {
-  auto pick = [](float a, float b) { return MAX ? fmaxf(a, b) : fminf(a, b); };
-  v = pick(v, dpp_move_f32<kDppSwapPairs>(v));
-  v = pick(v, dpp_move_f32<kDppSwapHalfQuads>(v));
-  v = pick(v, dpp_move_f32<kDppHalfMirror>(v));
-  if constexpr (LANES >= 16) v = pick(v, dpp_move_f32<kDppMirror>(v));
-  if constexpr (LANES >= 32) v = pick(v, __shfl_xor(v, 16));
+// the largest over the LANES lanes of a row
+template <int LANES, class T>
+__device__ __forceinline__ T row_max(T v) {
+  v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppSwapPairs, 0xf, 0xf, true));
+  v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppSwapHalfQuads, 0xf, 0xf, true));
+  v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppHalfMirror, 0xf, 0xf, true));
+  if constexpr (LANES >= 16) v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppMirror, 0xf, 0xf, true));
+  if constexpr (LANES >= 32) v = max(v, (T)__shfl_xor((int)v, 16));
   return v;
+}
+
+// what lane I of every four lanes has
+template <int I>
+__device__ __forceinline__ float of_four(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x55 * I, 0xf, 0xf, true));
 }
 
 // the quotient of d by a small whole number, correctly rounded: r = d - q by is exact, its share is added once
@@ -40,76 +46,107 @@ __device__ __forceinline__ double divided(double d, double by, double inv) {
   return fma(fma(-q, by, d), inv, q);
 }
 
-// LANES lanes to a row; consecutive groups take consecutive tokens of one head, whose rows lie side by side in a page
+// LANES lanes to a row; consecutive groups take consecutive tokens of one head, whose rows lie side by side in a page.  Consecutive
+// workgroups take the heads of the same tokens: a head's rows alone, 8 KB apart in a projection's output, would fall on few of the
+// memory's channels (20000 tokens x 32 heads x 128 into 4 bits that way: 155 us).
 template <int DT, int BITS, int LANES>
 __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
   constexpr int kGroups = 256 / LANES;
   constexpr double kTop = (1 << BITS) - 1;
   using ST = typename StoredType<DT>::type;
-  const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, head = blockIdx.y, which = blockIdx.z;
+  const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, which = blockIdx.y;
+  const int tile = blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads;
   const int c = lane * 8;
   const ST* X = static_cast<const ST*>(which ? a.X[1] : a.X[0]) + head * (which ? a.head[1] : a.head[0]);
   const int64_t stride = which ? a.token[1] : a.token[0];
-  const int64_t places = a.c.pages << a.c.page_shift;
+  const uint32_t places = (uint32_t)(a.c.pages << a.c.page_shift);
+  const KvRows rows = kv_rows(a.c, which, head);
   Run<DT, 8> x[kRowsPerLane];
   int slot[kRowsPerLane];
 #pragma unroll
   for (int i = 0; i < kRowsPerLane; ++i) {
-    const int token = (blockIdx.x * kRowsPerLane + i) * kGroups + group;
-    const int safe = min(token, a.t - 1);
+    const int token = (tile * kRowsPerLane + i) * kGroups + group, safe = min(token, a.t - 1);
     slot[i] = token < a.t ? a.slots[safe] : -1;
     x[i] = load_run<DT, 8, false>(X + safe * stride, c, a.d);
   }
+  // Bits tell a row's extremes, and whether all of it is finite: as signed numbers those of the largest value come last, as
+  // unsigned ones those of the value furthest below 0, if one is.
+  int hi_bits = 0;
+  uint32_t lo_bits = 0;
 #pragma unroll
   for (int i = 0; i < kRowsPerLane; ++i) {
     float v[8];
     run_to_f32<DT, 8>(x[i], c, a.d, v);
-    float lo = 0.f, hi = 0.f;
-    bool finite = true;
+    int hi = 0;
+    uint32_t lo = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      lo = fminf(lo, v[e]);
-      hi = fmaxf(hi, v[e]);
-      finite &= (__float_as_uint(v[e]) & 0x7f800000u) != 0x7f800000u;
+      hi = max(hi, __float_as_int(v[e]));
+      lo = max(lo, __float_as_uint(v[e]));
     }
-    // a row with an infinity or a NaN: its scale becomes NaN, and so does whatever reads it
-    hi = finite ? hi : INFINITY;
-    lo = row_extreme<LANES, false>(lo);
-    hi = row_extreme<LANES, true>(hi);
-    finite = hi < INFINITY;
-    float scale = finite ? (float)divided((double)hi - (double)lo, kTop, 1.0 / kTop) : 1.f;
-    if (scale == 0.f) {   // nothing but zeros (or less than float32 can divide)
-      lo = -1.f;
-      scale = (float)(2.0 / kTop);
-    }
-    const float lift = scale < 0x1p-60f ? 0x1p90f : 1.f;   // exact, and 1 / scale stays a normal number
-    const float over = scale * lift, inv = 1.f / over;
-    const float below[1] = {-lo * lift};
-    float z[1], code[8];
-    whole_codes<1>(below, inv, 1.f, over, z);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= lift;
-    whole_codes<8>(v, inv, 1.f, over, code);
-    const int zero = finite ? (int)z[0] : 0;
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t k = finite ? (uint32_t)min(max((int)code[e] + zero, 0), (1 << BITS) - 1) : 0u;
-      if constexpr (BITS == 8) w[e >> 2] |= k << (8 * (e & 3));
-      else w[0] |= k << (4 * (e >> 1) + 16 * (e & 1));
-    }
-    if ((uint32_t)slot[i] >= (uint64_t)places) continue;
-    const int64_t row = kv_row(a.c, which, slot[i] >> a.c.page_shift, head, slot[i] & ((1 << a.c.page_shift) - 1));
-    if (c < a.d) {
-      uint8_t* out = a.c.codes + row * a.c.row_bytes + lane * BITS;
-      if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out) = uint2{w[0], w[1]};
-      else *reinterpret_cast<uint32_t*>(out) = w[0];
-    }
-    if (lane == 0) {
-      a.c.scales[row] = finite ? scale : __uint_as_float(0x7fc00000u);
-      a.c.zeros[row] = (uint8_t)zero;
+    hi = row_max<LANES>(hi);
+    lo = row_max<LANES>(lo);
+    // the grids of the group's four rows are worked out side by side: lane i of every four has row i
+    if ((lane & 3) == i) {
+      hi_bits = hi;
+      lo_bits = lo;
     }
   }
+  // a row with an infinity or a NaN: its scale becomes NaN, and so does whatever reads it; its codes 0 (x inv is NaN or 0)
+  const bool finite = hi_bits < 0x7f800000 && lo_bits < 0xff800000u;
+  const float hi = __int_as_float(hi_bits);
+  float lo = lo_bits > 0x80000000u ? __uint_as_float(lo_bits) : 0.f;
+  float scale = finite ? (float)divided((double)hi - (double)lo, kTop, 1.0 / kTop) : 1.f;
+  if (scale == 0.f) {   // nothing but zeros (or less than float32 can divide)
+    lo = -1.f;
+    scale = (float)(2.0 / kTop);
+  }
+  const float below[1] = {finite ? -lo : 0.f};
+  float inv = __builtin_amdgcn_rcpf(scale), z[1];
+  whole_codes<1>(below, inv, 1.f, scale, z);
+  // both ends rounded away from 0 (the only codes past the grid), or no float32 reciprocal: by the quotient, and clamped
+  const bool odd_grid = __any((scale < 0x1p-110f) | (scale > 0x1p110f) | (finite && rintf(hi * inv) + z[0] > (float)kTop));
+  inv = finite ? inv : 0.f;
+  {
+    int mine = slot[0];
+#pragma unroll
+    for (int i = 1; i < kRowsPerLane; ++i) mine = (lane & 3) == i ? slot[i] : mine;
+    if (lane < kRowsPerLane && (uint32_t)mine < places) {
+      const int64_t row = kv_row(rows, (uint32_t)mine >> a.c.page_shift, mine & ((1 << a.c.page_shift) - 1));
+      a.c.scales[row] = finite ? scale : __uint_as_float(0x7fc00000u);
+      a.c.zeros[row] = (uint8_t)z[0];
+    }
+  }
+  static_for<kRowsPerLane>([&](auto i_) {
+    constexpr int i = decltype(i_)::value;
+    const float inv_i = of_four<i>(inv), z_i = of_four<i>(z[0]);
+    float v[8];
+    run_to_f32<DT, 8>(x[i], c, a.d, v);
+    // 1.5 2^23 + a whole number has that number in its low bits, and adding it rounds there: code = rne(x inv + zero), which is rne(x / scale) + zero
+    // as long as x inv + zero, off by less than 2^-14 (see whole_codes; the sum adds 2^-17), is not that close to a middle
+    constexpr float kWhole = 12582912.f;
+    const float from = z_i + kWhole;
+    float u[8], far = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      u[e] = fmaf(v[e], inv_i, from);
+      far = fmaxf(far, fabsf(fmaf(v[e], inv_i, from - u[e])));
+    }
+    if (__any(far > 0.5f - 0x1p-14f) | odd_grid) {
+      const float s = of_four<i>(scale), good = of_four<i>(finite ? 1.f : 0.f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        u[e] = kWhole + (good != 0.f ? fminf((float)rint((double)v[e] / (double)s) + z_i, (float)kTop) : 0.f);
+    }
+    auto byte_pair = [&](int e0, int e1) { return __builtin_amdgcn_perm(__float_as_uint(u[e1]), __float_as_uint(u[e0]), 0x0c0c0400u); };
+    auto bytes = [&](int e0, int e1, int e2, int e3) { return __builtin_amdgcn_perm(byte_pair(e2, e3), byte_pair(e0, e1), 0x05040100u); };
+    if ((uint32_t)slot[i] < places && c < a.d) {
+      const int64_t row = kv_row(rows, (uint32_t)slot[i] >> a.c.page_shift, slot[i] & ((1 << a.c.page_shift) - 1));
+      uint8_t* out = a.c.codes + row * a.c.row_bytes + lane * BITS;
+      if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out) = uint2{bytes(0, 1, 2, 3), bytes(4, 5, 6, 7)};
+      else *reinterpret_cast<uint32_t*>(out) = bytes(0, 4, 1, 5) | (bytes(2, 6, 3, 7) << 4);
+    }
+  });
 }
 
 struct ReadArgs {
@@ -127,28 +164,29 @@ template <int DT, int BITS, int LANES>
 __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
   constexpr int kGroups = 256 / LANES;
   using ST = typename StoredType<DT>::type;
-  const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, seq = blockIdx.z;
-  const int head = blockIdx.y >> 1, which = blockIdx.y & 1, c = lane * 8;
+  const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, seq = blockIdx.z, which = blockIdx.y;
+  const int tile = blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads, c = lane * 8;
   const int64_t begin = a.cu[seq], end = a.cu[seq + 1];
   if (begin < 0 || end > a.rows) return;
   const int64_t length = min(end - begin, a.max_kv);
   ST* X = static_cast<ST*>(which ? a.X[1] : a.X[0]) + head * (which ? a.head[1] : a.head[0]);
   const int64_t stride = which ? a.token[1] : a.token[0];
-  int64_t place[kRowsPerLane], row[kRowsPerLane];
+  if ((int64_t)tile * kRowsPerLane * kGroups >= length) return;
+  const KvRows rows = kv_rows(a.c, which, head);
+  const int first = tile * kRowsPerLane * kGroups + group, inside = (1 << a.c.page_shift) - 1;
+  int page[kRowsPerLane];
+#pragma unroll
+  for (int i = 0; i < kRowsPerLane; ++i) {
+    const int at = min(first + i * kGroups, (int)length - 1) >> a.c.page_shift;
+    page[i] = a.table[seq * a.ldt + min((int64_t)at, a.ldt - 1)];
+    page[i] = at < a.ldt && (uint32_t)page[i] < (uint64_t)a.c.pages ? page[i] : -1;
+  }
   uint2 w[kRowsPerLane];
   float scale[kRowsPerLane];
   int zero[kRowsPerLane];
-  if ((int64_t)blockIdx.x * kRowsPerLane * kGroups >= length) return;
 #pragma unroll
   for (int i = 0; i < kRowsPerLane; ++i) {
-    place[i] = ((int64_t)blockIdx.x * kRowsPerLane + i) * kGroups + group;
-    const int64_t at = min(place[i], length - 1) >> a.c.page_shift;
-    const int page = at < a.ldt ? a.table[seq * a.ldt + at] : -1;
-    row[i] = (uint32_t)page < (uint64_t)a.c.pages ? kv_row(a.c, which, page, head, (int)(place[i] & ((1 << a.c.page_shift) - 1))) : -1;
-  }
-#pragma unroll
-  for (int i = 0; i < kRowsPerLane; ++i) {
-    const int64_t r = row[i] < 0 ? 0 : row[i];
+    const int64_t r = kv_row(rows, max(page[i], 0), (first + i * kGroups) & inside);
     const uint8_t* in = a.c.codes + r * a.c.row_bytes + (c < a.d ? lane * BITS : 0);
     if constexpr (BITS == 8) w[i] = *reinterpret_cast<const uint2*>(in);
     else w[i].x = *reinterpret_cast<const uint32_t*>(in);
@@ -157,16 +195,17 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
   }
 #pragma unroll
   for (int i = 0; i < kRowsPerLane; ++i) {
-    if (place[i] >= length || c >= a.d) continue;
+    if (first + i * kGroups >= length) continue;
+    const float s = page[i] < 0 ? 0.f : scale[i], z = (float)zero[i];   // a page that is not there: zeros
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      int k;
-      if constexpr (BITS == 8) k = ((e < 4 ? w[i].x : w[i].y) >> (8 * (e & 3))) & 255;
-      else k = (w[i].x >> (4 * (e >> 1) + 16 * (e & 1))) & 15;
-      v[e] = row[i] < 0 ? 0.f : scale[i] * (float)(k - zero[i]);
+      uint32_t k;
+      if constexpr (BITS == 8) k = ((e < 4 ? w[i].x : w[i].y) >> (8 * (e & 3))) & 255u;
+      else k = (((e >> 1) & 1 ? (w[i].x >> 4) & 0x0f0f0f0fu : w[i].x & 0x0f0f0f0fu) >> (8 * (e >> 2) + 16 * (e & 1))) & 255u;
+      v[e] = s * ((float)k - z);
     }
-    store_run<DT, 8, false>(X + (begin + place[i]) * stride, c, a.d, v);
+    store_run<DT, 8, false>(X + (begin + first + i * kGroups) * stride, c, a.d, v);
   }
 }
 
@@ -176,7 +215,7 @@ KvCache cache_of(uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, i
 
 template <int DT, int BITS>
 void write_lanes(const WriteArgs& a, hipStream_t s) {
-  auto grid = [&](int lanes) { return dim3((unsigned)ceil_div(a.t, kRowsPerLane * (256 / lanes)), (unsigned)a.c.heads, 2); };
+  auto grid = [&](int lanes) { return dim3((unsigned)(ceil_div(a.t, kRowsPerLane * (256 / lanes)) * a.c.heads), 2); };
   if (a.d <= 64) kv_write_kernel<DT, BITS, 8><<<grid(8), 256, 0, s>>>(a);
   else if (a.d <= 128) kv_write_kernel<DT, BITS, 16><<<grid(16), 256, 0, s>>>(a);
   else kv_write_kernel<DT, BITS, 32><<<grid(32), 256, 0, s>>>(a);
@@ -184,7 +223,7 @@ void write_lanes(const WriteArgs& a, hipStream_t s) {
 template <int DT, int BITS>
 void read_lanes(const ReadArgs& a, int b, hipStream_t s) {
   auto grid = [&](int lanes) {
-    return dim3((unsigned)ceil_div(a.max_kv, kRowsPerLane * (256 / lanes)), (unsigned)(2 * a.c.heads), (unsigned)b);
+    return dim3((unsigned)(ceil_div(a.max_kv, kRowsPerLane * (256 / lanes)) * a.c.heads), 2, (unsigned)b);
   };
   if (a.d <= 64) kv_read_kernel<DT, BITS, 8><<<grid(8), 256, 0, s>>>(a);
   else if (a.d <= 128) kv_read_kernel<DT, BITS, 16><<<grid(16), 256, 0, s>>>(a);

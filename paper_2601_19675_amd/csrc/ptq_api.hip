@@ -371,7 +371,7 @@ ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const ui
       v_head < 0)
     return PTQ_ERR_SHAPE;
   if (b == 0 || rows == 0 || max_kv == 0) return PTQ_OK;
-  if (pages == 0) return PTQ_ERR_SHAPE;
+  if (pages == 0 || ldt == 0) return PTQ_ERR_SHAPE;
   if (!codes || !scales || !zeros || !table || !cu_kv || !K || !V || misaligned(codes, 16)) return PTQ_ERR_ARG;
   return kv_cache_read_launch(codes, scales, zeros, pages, (int)page, (int)hkv, (int)d, bits, table, ldt, b, cu_kv, rows, max_kv, K,
                               k_token, k_head, V, v_token, v_head, dt, static_cast<hipStream_t>(stream));

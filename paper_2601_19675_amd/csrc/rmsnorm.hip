@@ -107,17 +107,13 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void rmsnorm_quantize_kernel
   }
   const bool finite = top < 0x7f800000u;
   const float A = __uint_as_float(top);
-  // 127 / A stays a normal number: rows of very small values are taken 2^90 times as large, which is exact
-  const float lift = A < 0x1p-60f ? 0x1p90f : 1.f;
-  const float over = A * lift, inv = top == 0 ? 0.f : 127.f / over;
+  const float inv = 127.f * __builtin_amdgcn_rcpf(A);
 #pragma unroll
   for (int p = 0; p < PER; ++p) {
     const int c = (p * ROW + at) * 8, count = a.n - c;
     if (count <= 0) continue;
     float code[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) u[p][i] *= lift;
-    if (finite && top != 0) whole_codes<8>(u[p], inv, 127.f, over, code);
+    if (finite && top != 0) whole_codes<8>(u[p], inv, 127.f, A, code);
     else
 #pragma unroll
       for (int i = 0; i < 8; ++i) code[i] = 0.f;

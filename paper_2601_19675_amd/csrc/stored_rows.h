@@ -89,21 +89,21 @@ __device__ __forceinline__ void store_run(void* row, int c, int n, const float (
   }
 }
 
-// rne(times x / over) for N values, |result| < 2^9, where inv is float32(times / over).  v = x inv is off by no more than
-// 2^-23 |v| < 2^-14, so only where v is that close to the middle of two codes does the quotient decide, in float64:
-// times x is exact there, and a quotient of two numbers of so few bits that is not a middle lies further from it than a
-// float64 rounds.  (The quotient for every value: two thirds of the kernel's instructions; one value in 8000 needs it.)
-// x and c are different arrays.
+// rne(times x / over) for N values, |result| <= 255.  inv is times / over to 1.5 * 2^-23 of itself (a reciprocal to the last bit and a
+// rounding), so v = x inv is off by no more than 2^-22 |v| < 2^-14: only where v is that close to the middle of two codes does the
+// quotient decide, in float64.  times x is exact there, and a quotient of two numbers of so few bits that is not a middle lies
+// further from it than a float64 rounds.  (One value in 8000 needs it; the quotient for every value was two thirds of the work.)
+// Where `over` is so small or large that it has no normal reciprocal, every value takes the quotient.  x and c are different arrays.
 template <int N>
 __device__ __forceinline__ void whole_codes(const float (&x)[N], float inv, float times, float over, float (&c)[N]) {
-  bool near = false;
+  float far = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float v = x[i] * inv;
     c[i] = rintf(v);
-    near |= fabsf(v - c[i]) > 0.5f - 0x1p-14f;
+    far = fmaxf(far, fabsf(v - c[i]));
   }
-  if (near) {
+  if (__any((far > 0.5f - 0x1p-14f) | (over < 0x1p-110f) | (over > 0x1p110f))) {   // (the wave's: or it would be computed for all)
 #pragma unroll
     for (int i = 0; i < N; ++i) c[i] = (float)rint((double)times * (double)x[i] / (double)over);
   }

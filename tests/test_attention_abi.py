@@ -55,7 +55,7 @@ def test_cache(lib):
         assert call(codes=P + 8) == ARG
     assert write(slots=None) == ARG and write(t=-1) == SHAPE
     assert read(table=None) == ARG and read(cu=None) == ARG and read(pages=0) == SHAPE
-    assert read(b=65536) == SHAPE and read(ldt=-1) == SHAPE and read(rows=-1) == SHAPE and read(max_kv=-1) == SHAPE
+    assert read(b=65536) == SHAPE and read(ldt=-1) == SHAPE and read(ldt=0) == SHAPE and read(rows=-1) == SHAPE and read(max_kv=-1) == SHAPE
 
 
 def test_int8_linear(lib):
