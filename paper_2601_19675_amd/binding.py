@@ -5,6 +5,9 @@ live on the GPU (torch is used for device memory and streams, nothing else),
 passes their raw pointers, sizes and the current HIP stream to the entry point
 of the same name, and raises PtqError on a non-zero status.  There is no CPU
 or PyTorch fallback: without the built library every call fails loudly.
+
+The calls that are made per layer and token (norm, 8-bit product, cache, attention)
+do the same in compiled code (csrc/tokens_binding.cpp).
 """
 from __future__ import annotations
 
@@ -439,22 +442,25 @@ def ptq_lopro_linear_forward_static_limit() -> int:
     return int(load_library().ptq_lopro_linear_forward_static_limit())
 
 
+_TOKENS = None
+
+
+def _tokens():
+    """The compiled marshalling of the calls below."""
+    global _TOKENS
+    if _TOKENS is None:
+        load_library()
+        from . import _tokens as module
+        _TOKENS = module
+    return _TOKENS
+
+
 def ptq_rmsnorm_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, gamma: torch.Tensor | None = None,
                          residual: torch.Tensor | None = None, residual_out: torch.Tensor | None = None, eps: float = 1e-5,
                          normalize: bool = True) -> None:
     """codes (int8 t x n), scales (float32 t) <- the norm of X + residual (t x n, bfloat16 or float32) times gamma;
     residual_out <- X + residual.  normalize=False: the rows as they are."""
-    _check_dev(X, codes, scales, gamma, residual, residual_out)
-    t, n = X.shape
-    assert X.stride(1) == 1 and codes.dtype == torch.int8 and codes.shape == (t, n) and codes.stride(1) == 1
-    assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.numel() == t
-    assert gamma is None or (gamma.dtype == X.dtype and gamma.is_contiguous() and gamma.shape == (n,))
-    for r in (residual, residual_out):
-        assert r is None or (r.dtype == X.dtype and r.shape == (t, n) and r.stride(1) == 1)
-    rc = load_library().ptq_rmsnorm_quantize(X.data_ptr(), _dtype_code(X), X.stride(0), t, n, _ptr(residual),
-                                             0 if residual is None else residual.stride(0), _ptr(residual_out),
-                                             0 if residual_out is None else residual_out.stride(0), _ptr(gamma), float(eps),
-                                             int(bool(normalize)), codes.data_ptr(), codes.stride(0), scales.data_ptr(), _stream())
+    rc = (_TOKENS or _tokens()).rmsnorm_quantize(X, codes, scales, gamma, residual, residual_out, eps, normalize)
     if rc:
         raise PtqError(rc, "ptq_rmsnorm_quantize")
 
@@ -462,45 +468,16 @@ def ptq_rmsnorm_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
 def ptq_int8_linear(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, O: torch.Tensor,
                     bias: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> None:
     """O (bfloat16 or float32 t x m) <- (A W^T) a_scales w_scales + bias; A int8 t x n, W int8 m x n, the rest float32."""
-    _check_dev(A, a_scales, W, w_scales, O, bias)
-    t, n = A.shape
-    m = W.shape[0]
-    assert A.dtype == torch.int8 and A.stride(1) == 1 and W.dtype == torch.int8 and W.shape == (m, n) and W.stride(1) == 1
-    assert a_scales.dtype == torch.float32 and a_scales.is_contiguous() and a_scales.numel() == t
-    for c in (w_scales, bias):
-        assert c is None or (c.dtype == torch.float32 and c.is_contiguous() and c.numel() == m)
-    assert O.shape == (t, m) and O.stride(1) == 1
-    if ws is None:
-        need = ptq_workspace_bytes(OP_INT8_LINEAR, m, n, t)
-        ws = torch.empty(need, dtype=torch.uint8, device=A.device) if need else None
-    rc = load_library().ptq_int8_linear(A.data_ptr(), A.stride(0), a_scales.data_ptr(), t, W.data_ptr(), W.stride(0),
-                                        w_scales.data_ptr(), m, n, _ptr(bias), O.data_ptr(), _dtype_code(O), O.stride(0),
-                                        _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+    rc = (_TOKENS or _tokens()).int8_linear(A, a_scales, W, w_scales, O, bias, ws)
     if rc:
         raise PtqError(rc, "ptq_int8_linear")
 
 
-def _check_cache(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, bits: int, d: int) -> tuple[int, int, int]:
-    """(pages, heads, page) of a cache of rows of d values."""
-    assert codes.dtype == torch.uint8 and codes.is_contiguous() and codes.dim() == 5 and codes.shape[0] == 2
-    pages, hkv, page = codes.shape[1:4]
-    assert codes.shape[4] == d * bits // 8
-    assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.shape == (2, pages, hkv, page)
-    assert zeros.dtype == torch.uint8 and zeros.is_contiguous() and zeros.shape == (2, pages, hkv, page)
-    return pages, hkv, page
-
-
 def ptq_kv_cache_write(K: torch.Tensor, V: torch.Tensor, slots: torch.Tensor, bits: int, codes: torch.Tensor,
                        scales: torch.Tensor, zeros: torch.Tensor) -> None:
-    """Quantizes K and V (t x heads x d, bfloat16 or float32) into the cache rows that slots (int32 t) names."""
-    _check_dev(K, V, slots, codes, scales, zeros)
-    t, hkv, d = K.shape
-    pages, heads, page = _check_cache(codes, scales, zeros, bits, d)
-    assert heads == hkv and V.shape == K.shape and V.dtype == K.dtype and (K.stride(2) == 1 and V.stride(2) == 1)
-    assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == t
-    rc = load_library().ptq_kv_cache_write(K.data_ptr(), K.stride(0), K.stride(1), V.data_ptr(), V.stride(0), V.stride(1),
-                                           _dtype_code(K), t, hkv, d, slots.data_ptr(), bits, codes.data_ptr(),
-                                           scales.data_ptr(), zeros.data_ptr(), pages, page, _stream())
+    """Quantizes K and V (t x heads x d, bfloat16 or float32) into the cache rows that slots (int32 t) names; codes
+    (uint8 2 x pages x heads x page x d bits / 8), scales (float32) and zeros (uint8) are the cache."""
+    rc = (_TOKENS or _tokens()).kv_cache_write(K, V, slots, bits, codes, scales, zeros)
     if rc:
         raise PtqError(rc, "ptq_kv_cache_write")
 
@@ -509,16 +486,7 @@ def ptq_kv_cache_read(codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Te
                       cu_kv: torch.Tensor, max_kv: int, K: torch.Tensor, V: torch.Tensor) -> None:
     """K, V (rows x heads x d) <- the sequences whose pages table (int32 b x pages of a sequence) lists; sequence s is rows
     cu_kv[s] .. cu_kv[s + 1] (int32, on the device), none longer than max_kv."""
-    _check_dev(codes, scales, zeros, table, cu_kv, K, V)
-    rows, hkv, d = K.shape
-    pages, heads, page = _check_cache(codes, scales, zeros, bits, d)
-    b = table.shape[0]
-    assert heads == hkv and V.shape == K.shape and V.dtype == K.dtype and (K.stride(2) == 1 and V.stride(2) == 1)
-    assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
-    assert cu_kv.dtype == torch.int32 and cu_kv.is_contiguous() and cu_kv.numel() == b + 1
-    rc = load_library().ptq_kv_cache_read(codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), pages, page, hkv, d, bits,
-                                          table.data_ptr(), table.shape[1], b, cu_kv.data_ptr(), rows, int(max_kv), K.data_ptr(),
-                                          K.stride(0), K.stride(1), V.data_ptr(), V.stride(0), V.stride(1), _dtype_code(K), _stream())
+    rc = (_TOKENS or _tokens()).kv_cache_read(codes, scales, zeros, bits, table, cu_kv, max_kv, K, V)
     if rc:
         raise PtqError(rc, "ptq_kv_cache_read")
 
@@ -529,21 +497,7 @@ def ptq_paged_attention(Q: torch.Tensor, cu_q: torch.Tensor, max_q: int, codes: 
                         ws: torch.Tensor | None = None) -> None:
     """O <- attention of Q (bfloat16 t x heads x d) over the cache; sequence s has the tokens cu_q[s] .. cu_q[s + 1] (int32, on
     the device, no more than max_q) and kv_lens[s] keys (int32, no more than max_kv), its new tokens' own the last of them."""
-    _check_dev(Q, cu_q, codes, scales, zeros, table, kv_lens, O)
-    t, hq, d = Q.shape
-    pages, hkv, page = _check_cache(codes, scales, zeros, bits, d)
-    b = table.shape[0]
-    assert O.shape == Q.shape and O.dtype == Q.dtype and Q.stride(2) == 1 and O.stride(2) == 1
-    assert table.dtype == torch.int32 and table.is_contiguous() and table.dim() == 2
-    assert cu_q.dtype == torch.int32 and cu_q.is_contiguous() and cu_q.numel() == b + 1
-    assert kv_lens.dtype == torch.int32 and kv_lens.is_contiguous() and kv_lens.numel() == b
-    if ws is None:
-        need = ptq_workspace_bytes(OP_PAGED_ATTENTION, hq, d, t, max_kv)
-        ws = torch.empty(need, dtype=torch.uint8, device=Q.device) if need else None
-    rc = load_library().ptq_paged_attention(Q.data_ptr(), _dtype_code(Q), Q.stride(0), Q.stride(1), t, hq, d, cu_q.data_ptr(), b,
-                                            int(max_q), codes.data_ptr(), scales.data_ptr(), zeros.data_ptr(), pages, page, hkv,
-                                            bits, table.data_ptr(), table.shape[1], kv_lens.data_ptr(), int(max_kv),
-                                            float(softmax_scale), int(bool(causal)), int(window), O.data_ptr(), O.stride(0),
-                                            O.stride(1), _ptr(ws), 0 if ws is None else ws.numel(), _stream())
+    rc = (_TOKENS or _tokens()).paged_attention(Q, cu_q, max_q, codes, scales, zeros, bits, table, kv_lens, max_kv, softmax_scale, O,
+                                                causal, window, ws)
     if rc:
         raise PtqError(rc, "ptq_paged_attention")

@@ -10,6 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libptq.so")
 PROBE_LIB = os.path.join(HERE, "libptq_probe.so")   # diagnostics for bench.py --mfma-control, not part of the product
+TOKENS_LIB = os.path.join(HERE, "_tokens.so")       # from torch tensors to the calls of the 8-bit attention path
 SOURCES = ["ptq_api.hip", "hessian.hip", "hessian_f32.hip", "cholesky.hip", "quantize.hip", "vq.hip", "layer_error.hip", "lopro.hip", "r1svd.hip", "r1svd_bf16.hip", "artifact.hip", "rmsnorm.hip", "kv_cache.hip", "int8_linear.hip", "paged_attention.hip", "paged_attention_chunk.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
@@ -147,6 +148,22 @@ def check_assembly(src: str) -> None:
         raise RuntimeError(f"{src}: none of the checked instructions found in the generated assembly (check out of date?)")
 
 
+def build_tokens_binding() -> None:
+    """Host code against torch's own headers and libraries (which are loaded by the time it is imported) and libptq.so."""
+    from importlib.util import find_spec
+    from sysconfig import get_paths
+
+    torch = os.path.dirname(find_spec("torch").origin)
+    r = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+                        *[f"-I{d}" for d in (os.path.join(torch, "include"), os.path.join(torch, "include/torch/csrc/api/include"),
+                                             "/opt/rocm/include", get_paths()["include"])],
+                        os.path.join(CSRC, "tokens_binding.cpp"), "-o", TOKENS_LIB, "-L" + os.path.join(torch, "lib"),
+                        "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_hip", "-L" + HERE, "-l:libptq.so", "-Wl,-rpath,$ORIGIN"],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"tokens binding failed:\n{r.stdout}\n{r.stderr}")
+
+
 def build(verbose: bool = True) -> str:
     """Compiles every source (always, also when a library is already there) and links."""
     hipcc = _hipcc()
@@ -173,6 +190,7 @@ def build(verbose: bool = True) -> str:
                        capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+    build_tokens_binding()
     # the register-only MFMA probe, a library of its own: one source, compiled in both accumulator forms
     probe_objs = []
     for tag, extra in (("agpr", []), ("vgpr", ["-DPTQ_PROBE_VGPR_FORM", *VGPR_FORM])):

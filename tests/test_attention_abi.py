@@ -92,3 +92,16 @@ def test_paged_attention(lib):
     need = ptq.ptq_workspace_bytes(ptq.OP_PAGED_ATTENTION, 4, 64, 4, 5000)
     assert need > 0 and call(max_kv=5000) == WORKSPACE and call(max_kv=5000, ws=P, bytes=need - 1) == WORKSPACE
     assert ptq.ptq_workspace_bytes(ptq.OP_PAGED_ATTENTION, 32, 128, 3000, 16384) < 300 << 20
+
+
+def test_python_calls_refuse_tensors_that_do_not_fit():
+    import torch
+    x, c = torch.zeros((2, 64)), torch.zeros((2, 64), dtype=torch.int8)
+    with pytest.raises(ValueError, match="device tensors"):
+        ptq.ptq_rmsnorm_quantize(x, c, torch.zeros(2))
+    with pytest.raises(ValueError, match="device tensors"):
+        ptq.ptq_int8_linear(c, torch.zeros(2), c, torch.zeros(2), torch.zeros((2, 2)))
+    with pytest.raises(TypeError):
+        ptq.ptq_rmsnorm_quantize(x.numpy(), c, torch.zeros(2))
+    with pytest.raises(TypeError):
+        ptq.ptq_kv_cache_write(None, x, c, 8, c, x, c)
