@@ -19,6 +19,7 @@
 #include <algorithm>
 
 #include "paged_attention.h"
+#include "static_for.h"
 #include "stored_rows.h"
 
 namespace ptq {
@@ -27,6 +28,8 @@ namespace {
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16v;
 
 constexpr int kTile = 64;   // keys
+constexpr int kNoExponent = -1000;   // E before the first value
+constexpr int kMetas = 8, kMetaAhead = 4;   // tiles whose Meta is in LDS, and how far before its turn it is brought there
 
 template <int DP>
 struct Chunk {
@@ -34,7 +37,13 @@ struct Chunk {
   static constexpr int kWaves = kThreads / 64, kRows = 32 * kWaves;
   static constexpr int kKeyPitch = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;   // bytes of a key
   static constexpr int kKeyBytes = kTile * kKeyPitch, kValBytes = DP * kTile * 2;
-  static constexpr int kBuffer = kKeyBytes + kValBytes;
+  static constexpr bool kTurns = DP <= 128;                  // two halves of the workgroup take turns at the matrix instructions
+  static constexpr int kRing = 2;                            // tiles of codes in LDS
+  static constexpr int kBuffers = kRing * (kKeyBytes + kValBytes);
+  // Steps of d whose queries wait in LDS: at d = 128 the registers of two waves to a SIMD do not hold all of them beside what a turn needs
+  // (and what the compiler spills goes to memory: 1584 us in place of TURNS)
+  static constexpr int kQuerySteps = DP == 128 ? 4 : 0;
+  static constexpr int kQueryBytes = kQuerySteps * 16 * 2 * kRows;
   static constexpr int kHalf = kThreads / 2;
   static constexpr int kKeyUnits = (4 * DP + kHalf - 1) / kHalf;   // 16 codes of a key each, per thread
   static constexpr int kValUnits = (2 * DP + kHalf - 1) / kHalf;   // eight channels of four keys each
@@ -74,7 +83,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   using C = Chunk<DP>;
   constexpr int kSteps = DP / 16, kOut = DP / 32;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  Meta* metas = reinterpret_cast<Meta*>(smem + 2 * C::kBuffer);
+  Meta* metas = reinterpret_cast<Meta*>(smem + C::kBuffers + C::kQueryBytes);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
 
   // groups (sequence, key head) go round the dies, so that a group's row tiles share its codes in one L2; the last rows, which
@@ -107,7 +116,9 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   const bool live = row < rows;
   visible(a, q, live ? row / a.group : 0, lo, hi);
   if (!live) hi = 0;
-  f16x8 fq[kSteps];
+  constexpr int kHeld = kSteps - C::kQuerySteps;   // steps of d of the queries in registers
+  f16x8 fq[kHeld];
+  char* const queries = smem + C::kBuffers + (wave * 64 + lane) * 16;   // the others: [step][wave][lane]
   float factor;
   {
     Run<PTQ_BF16, 8> raw[kSteps];
@@ -134,7 +145,8 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         w[i] = __builtin_bit_cast(uint32_t, to_f16(ldexpf(lift * v[2 * i], 15 - e), ldexpf(lift * v[2 * i + 1], 15 - e)));
-      fq[u] = f16x8_of(w[0], w[1], w[2], w[3]);
+      if (u < kHeld) fq[u < kHeld ? u : 0] = f16x8_of(w[0], w[1], w[2], w[3]);
+      else *reinterpret_cast<f16x8*>(queries + (u - kHeld) * C::kThreads * 16) = f16x8_of(w[0], w[1], w[2], w[3]);
     }
   }
 
@@ -143,7 +155,8 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   const int32_t* table = a.table + seq * a.ldt;
   const int inside = (1 << a.c.page_shift) - 1;
 
-  // ---- what comes before the codes: the first wave, a lane per key
+  // ---- what comes before the codes: a wave's tiles are every kWaves-th, a lane per key, so that it has that many tiles' time for its
+  // loads
   struct MetaLoad { int page; float ks, vs; int kz, vz; };
   auto page_of = [&](int t) {   // tile t's key `lane`
     const int key = begin + t * kTile + lane;
@@ -158,21 +171,24 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     MetaLoad m{page, a.c.scales[at], a.c.scales[plane + at], a.c.zeros[at], a.c.zeros[plane + at]};
     return m;
   };
-  int top_e = -1000;
-  auto meta_store = [&](int t, const MetaLoad& m) {
-    Meta& o = metas[t & 3];
-    const bool there = m.page >= 0, good = fabsf(m.vs) < INFINITY && there;
-    top_e = max(top_e, wave_max_int(good && m.vs != 0.f ? __builtin_amdgcn_frexp_expf(m.vs) : -1000));
+  auto there_of = [&](const MetaLoad& m) { return m.page >= 0; };
+  auto good_of = [&](const MetaLoad& m) { return m.page >= 0 && fabsf(m.vs) < INFINITY; };
+  auto exponent_of = [&](const MetaLoad& m) {   // of the tile's largest value scale
+    return wave_max_int(good_of(m) && m.vs != 0.f ? __builtin_amdgcn_frexp_expf(m.vs) : kNoExponent);
+  };
+  auto meta_store = [&](int t, const MetaLoad& m, int e) {
+    Meta& o = metas[t & (kMetas - 1)];
+    const bool there = there_of(m), good = good_of(m);
     o.at[lane] = row_of(t, m.page) * a.c.row_bytes;
     o.ks[lane] = good ? m.ks : there ? __uint_as_float(0x7fc00000u) : 0.f;
     const uint32_t z = 0x6400u | m.kz;
     o.kz[lane] = z | (z << 16);
     o.vz[lane] = (uint16_t)(0x6400u | m.vz);
-    o.vs[lane] = __builtin_bit_cast(uint16_t, (_Float16)(good ? ldexpf(m.vs, 7 - top_e) : 0.f));
+    o.vs[lane] = __builtin_bit_cast(uint16_t, (_Float16)(good ? ldexpf(m.vs, 7 - e) : 0.f));
     const uint64_t seen = __ballot(there);
     if (lane == 0) {
       o.seen = seen;
-      o.e = top_e;
+      o.e = e;
     }
   };
 
@@ -180,18 +196,25 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   constexpr int KW = BITS / 2, VW = BITS / 4;   // words of a unit: 16 codes | eight codes
   const bool key_half = wave < C::kWaves / 2;
   const int hid = tid % C::kHalf;
-  struct Codes { uint32_t w[C::kKeyUnits * KW > C::kValUnits * 4 * VW ? C::kKeyUnits * KW : C::kValUnits * 4 * VW]; };
-  auto codes_load = [&](int t, Codes& c) {
-    const Meta& m = metas[t & 3];
+  // (a vector, written as a whole: the compiler would merge the two halves' stores into an array, whose address is then not known, and send
+  // them through memory, right behind the loads)
+  constexpr int kCodeWords = C::kKeyUnits * KW > C::kValUnits * 4 * VW ? C::kKeyUnits * KW : C::kValUnits * 4 * VW;
+  typedef uint32_t Codes __attribute__((ext_vector_type(kCodeWords)));
+  auto codes_load = [&](int t) -> Codes {
+    const Meta& m = metas[t & (kMetas - 1)];
+    Codes c = 0u;
     if (key_half) {
+      Codes k = 0u;
 #pragma unroll
       for (int i = 0; i < C::kKeyUnits; ++i) {
         const int u = i * C::kHalf + hid, key = min(u / (DP / 16), kTile - 1), part = u % (DP / 16);
         const AnyWords<KW, 4> w = *reinterpret_cast<const AnyWords<KW, 4>*>(a.c.codes + m.at[key] + (16 * part < a.d ? part * 2 * BITS : 0));
 #pragma unroll
-        for (int j = 0; j < KW; ++j) c.w[i * KW + j] = w.w[j];
+        for (int j = 0; j < KW; ++j) k[i * KW + j] = w.w[j];
       }
+      c = k;
     } else {
+      Codes v = 0u;
 #pragma unroll
       for (int i = 0; i < C::kValUnits; ++i) {
         const int u = i * C::kHalf + hid, run = min(u / (DP / 8), kTile / 4 - 1), part = u % (DP / 8);
@@ -199,38 +222,72 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
         for (int k = 0; k < 4; ++k) {
           const AnyWords<VW, 4> w = *reinterpret_cast<const AnyWords<VW, 4>*>(VC + m.at[4 * run + k] + (8 * part < a.d ? part * BITS : 0));
 #pragma unroll
-          for (int j = 0; j < VW; ++j) c.w[(i * 4 + k) * VW + j] = w.w[j];
+          for (int j = 0; j < VW; ++j) v[(i * 4 + k) * VW + j] = w.w[j];
         }
       }
+      c = v;
     }
+    return c;
   };
-  auto codes_store = [&](int t, const Codes& c) {
-    const Meta& m = metas[t & 3];
-    char* buffer = smem + (t & 1) * C::kBuffer;
+  auto key_buffer = [&](int t) { return smem + t % C::kRing * C::kKeyBytes; };
+  auto val_buffer = [&](int t) { return smem + C::kRing * C::kKeyBytes + t % C::kRing * C::kValBytes; };
+  // what codes_store needs of Meta: zeros of the keys, or zeros and scales of the values
+  constexpr int kGridWords = C::kKeyUnits > 4 * C::kValUnits ? C::kKeyUnits : 4 * C::kValUnits;
+  typedef uint32_t Grids __attribute__((ext_vector_type(kGridWords)));
+  auto grids_load = [&](int t) -> Grids {
+    const Meta& m = metas[t & (kMetas - 1)];
+    Grids g = 0u;
     if (key_half) {
+      Grids k = 0u;
+#pragma unroll
+      for (int i = 0; i < C::kKeyUnits; ++i) k[i] = m.kz[min((i * C::kHalf + hid) / (DP / 16), kTile - 1)];
+      g = k;
+    } else {
+      Grids v = 0u;
+#pragma unroll
+      for (int i = 0; i < C::kValUnits; ++i) {
+        const int run = min((i * C::kHalf + hid) / (DP / 8), kTile / 4 - 1);
+        const uint2 z = *reinterpret_cast<const uint2*>(&m.vz[4 * run]), s = *reinterpret_cast<const uint2*>(&m.vs[4 * run]);
+        v[4 * i] = z.x;
+        v[4 * i + 1] = z.y;
+        v[4 * i + 2] = s.x;
+        v[4 * i + 3] = s.y;
+      }
+      g = v;
+    }
+    return g;
+  };
+  auto codes_store = [&](int t, const Codes c, const Grids grid) {
+    if (key_half) {
+      char* buffer = key_buffer(t);
 #pragma unroll
       for (int i = 0; i < C::kKeyUnits; ++i) {
         const int u = i * C::kHalf + hid, key = u / (DP / 16), part = u % (DP / 16);
         if (key >= kTile) continue;
-        const Zeros z = zeros_of<BITS>(m.kz[key]);
+        const Zeros z = zeros_of<BITS>(grid[i]);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          f16x8 f = row_codes<BITS>(&c.w[i * KW + j * (KW / 2)], z);
+          uint32_t w[KW / 2];
+#pragma unroll
+          for (int n = 0; n < KW / 2; ++n) w[n] = c[i * KW + j * (KW / 2) + n];
+          f16x8 f = row_codes<BITS>(w, z);
           if (DP != a.d && 16 * part >= a.d) f = f16x8_of(0, 0, 0, 0);
           *reinterpret_cast<f16x8*>(buffer + ((key * C::kKeyPitch + ((2 * part) ^ key_turn<DP>(key)) * 16) ^ (16 * j))) = f;
         }
       }
     } else {
+      char* buffer = val_buffer(t);
 #pragma unroll
       for (int i = 0; i < C::kValUnits; ++i) {
         const int u = i * C::kHalf + hid, run = u / (DP / 8), part = u % (DP / 8);
         if (run >= kTile / 4) continue;
-        const uint2 zz = *reinterpret_cast<const uint2*>(&m.vz[4 * run]), ss = *reinterpret_cast<const uint2*>(&m.vs[4 * run]);
-        const uint32_t* w = &c.w[i * 4 * VW];
+        uint32_t w[4 * VW];
+#pragma unroll
+        for (int n = 0; n < 4 * VW; ++n) w[n] = c[i * 4 * VW + n];
         uint32_t f[8][2];   // channel, pair of keys
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-          const Zeros z = zeros_of<BITS>(p ? zz.y : zz.x);
+          const Zeros z = zeros_of<BITS>(grid[4 * i + p]);
           const uint32_t *w0 = w + 2 * p * VW, *w1 = w0 + VW;
           if constexpr (BITS == 8) {
 #pragma unroll
@@ -251,7 +308,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
               f[2 * j + 1][p] = odd[j];
             }
           }
-          const f16x2 s = __builtin_bit_cast(f16x2, p ? ss.y : ss.x);
+          const f16x2 s = __builtin_bit_cast(f16x2, (uint32_t)grid[4 * i + 2 + p]);
 #pragma unroll
           for (int j = 0; j < 8; ++j) f[j][p] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, f[j][p]) * s);
         }
@@ -260,7 +317,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
         const int base = opaque(part * 8 * kTile * 2 + (((slot >> 1) ^ val_turn(8 * part)) * 16) + (slot & 1) * 8);
 #pragma unroll
         for (int j = 0; j < 8; ++j)   // val_turn(8 part + j) = val_turn(8 part) ^ j
-          *reinterpret_cast<uint2*>(buffer + C::kKeyBytes + (base ^ (16 * j)) + j * kTile * 2) = uint2{f[j][0], f[j][1]};
+          *reinterpret_cast<uint2*>(buffer + (base ^ (16 * j)) + j * kTile * 2) = uint2{f[j][0], f[j][1]};
       }
     }
   };
@@ -270,65 +327,109 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   for (int n = 0; n < kOut; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
-  float m = kNoScore, l = 0.f;   // m in units of 1 / factor
-  int e = -1000;
+  float m = kNoScore;   // in units of 1 / factor
+  // the sum of the weights, in every element: one more channel of the values, which are 1 there
+  f32x16v sum;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  const f16x8 ones = f16x8_of(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
+  int e = kNoExponent;
 
   const int key_at = r * C::kKeyPitch + ((h ^ key_turn<DP>(r)) * 16), val_at = r * kTile * 2 + ((h ^ val_turn(r)) * 16);
-  auto compute = [&](int t) {
-    const int key0 = begin + t * kTile;
-    const Meta& meta = metas[t & 3];
-    const char* buffer = smem + (t & 1) * C::kBuffer;
+  // What the matrix instructions do in one go: the values of tile t - 1 (with its weights), then the scores of tile t, either may be
+  // missing.  Groups of instructions -- the channels' blocks of 16 keys; two steps of d of both halves of the keys -- whose operands are
+  // read from LDS kReadAhead groups before: for itself the compiler reads each operand right before its instruction and waits.
+  constexpr int kReadAhead = 1, kGroups = 4 + kSteps / 2, kPer = kOut > 4 ? kOut : 4;
+  auto multiply = [&](auto had_, auto has_, int t, const f16x8 (&weights)[4], f32x16v (&s)[2]) {
+    constexpr int kFirst = decltype(had_)::value ? 0 : 4, kLast = decltype(has_)::value ? kGroups : 4;
+    const char *keys = key_buffer(t), *vals = val_buffer(t + C::kRing - 1);
     const int key_base = opaque(key_at), val_base = opaque(val_at);
+    f16x8 f[kReadAhead + 1][kPer], fql[kReadAhead + 1][2];
+    auto read = [&](auto g_) {
+      constexpr int g = decltype(g_)::value, at = g % (kReadAhead + 1);
+      if constexpr (g < 4) {
+#pragma unroll
+        for (int n = 0; n < kOut; ++n)   // val_turn(32 n + r) = val_turn(r) ^ 4 (n & 1)
+          f[at][n] = *reinterpret_cast<const f16x8*>(vals + (val_base ^ (32 * (g ^ (2 * (n & 1))))) + n * 32 * kTile * 2);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
+          const int u = 2 * (g - 4) + (i >> 1), k = i & 1;
+          f[at][i] = *reinterpret_cast<const f16x8*>(keys + (key_base ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kKeyPitch);
+          if (k == 0 && u >= kHeld) fql[at][i >> 1] = *reinterpret_cast<const f16x8*>(queries + (u - kHeld) * C::kThreads * 16);
+        }
+      }
+    };
+    static_for<kReadAhead>([&](auto i_) {
+      constexpr int g = kFirst + decltype(i_)::value;
+      if constexpr (g < kLast) read(std::integral_constant<int, g>{});
+    });
+    static_for<kLast - kFirst>([&](auto i_) {
+      constexpr int g = kFirst + decltype(i_)::value, at = g % (kReadAhead + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (g + kReadAhead < kLast) read(std::integral_constant<int, g + kReadAhead>{});
+      if constexpr (g < 4) {
+#pragma unroll
+        for (int n = 0; n < kOut; ++n) acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[at][n], weights[g], acc[n], 0, 0, 0);
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(ones, weights[g], sum, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int u = 2 * (g - 4) + (i >> 1), k = i & 1;
+          if (u == 0) s[k] = f32x16v{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+          s[k] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[at][i], u < kHeld ? fq[u < kHeld ? u : 0] : fql[at][i >> 1], s[k], 0, 0, 0);
+        }
+      }
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // the weights of tile t; what has been summed so far is brought to their maximum and to the tile's E
+  auto soften = [&](int t, f32x16v (&s)[2], f16x8 (&weights)[4]) {
+    const int key0 = begin + t * kTile;
+    const Meta& meta = metas[t & (kMetas - 1)];
     const uint64_t seen = meta.seen;
     const int now = __builtin_amdgcn_readfirstlane(meta.e);
     if (now != e) {   // (the first tile among others)
-      const float f = e == -1000 ? 1.f : ldexpf(1.f, e - now);
+      const float f = e == kNoExponent ? 1.f : ldexpf(1.f, e - now);
 #pragma unroll
       for (int n = 0; n < kOut; ++n) acc[n] *= f;
       e = now;
     }
-    float y[2][16];
-    float top = kNoScore;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      f32x16v s;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-      for (int u = 0; u < kSteps; ++u) {   // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
-        const f16x8 f = *reinterpret_cast<const f16x8*>(buffer + (key_base ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kKeyPitch);
-        s = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, fq[u], s, 0, 0, 0);
-      }
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const f32x4 ks = *reinterpret_cast<const f32x4*>(&meta.ks[32 * k + 8 * j + 4 * h]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[k][4 * j + i] = s[4 * j + i] * ks[i];
+        for (int i = 0; i < 4; ++i) s[k][4 * j + i] *= ks[i];
       }
-    }
     if (key0 < lo_b || key0 + kTile > hi_a || ~seen != 0) {   // some row does not see some key
+      // counted from the half wave's first key: what is left are constants
+      const int from_ = opaque(lo - key0 - 4 * h), to_ = opaque(hi - key0 - 4 * h);
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t there = (uint32_t)(seen >> (32 * k)) >> (4 * h);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int at = 32 * k + 8 * (i >> 2) + 4 * h + (i & 3), key = key0 + at;
-          if (!(key >= lo && key < hi && ((seen >> at) & 1))) y[k][i] = -INFINITY;
+          const int at = 8 * (i >> 2) + (i & 3);
+          s[k][i] = (32 * k + at >= from_) & (32 * k + at < to_) & (int)((there >> at) & 1) ? s[k][i] : -INFINITY;
         }
+      }
     }
+    float top = kNoScore;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, y[k][i]);
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[k][i]);
     if (__any((top - m) * factor > 8.f)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float next = fmaxf(m, top), f = exp2_fast((m - next) * factor);
       m = next;
-      l *= f;
+      sum *= f;
 #pragma unroll
       for (int n = 0; n < kOut; ++n) acc[n] *= f;
     }
     const float M = fmaxf(m * factor, kNoScore);   // (finite where nothing has been seen: -inf - M stays -inf)
-    f16x8 weights[4];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -336,51 +437,112 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p0 = exp2_fast(fmaf(y[k][8 * u + 2 * i], factor, -M)), p1 = exp2_fast(fmaf(y[k][8 * u + 2 * i + 1], factor, -M));
-          l += p0 + p1;
+          const float p0 = exp2_fast(fmaf(s[k][8 * u + 2 * i], factor, -M)), p1 = exp2_fast(fmaf(s[k][8 * u + 2 * i + 1], factor, -M));
           w[i] = __builtin_bit_cast(uint32_t, to_f16(p0, p1));
         }
         weights[2 * k + u] = f16x8_of(w[0], w[1], w[2], w[3]);
       }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int n = 0; n < kOut; ++n) {
-        // val_turn(32 n + r) = val_turn(r) ^ 4 (n & 1)
-        const f16x8 f = *reinterpret_cast<const f16x8*>(buffer + C::kKeyBytes + (val_base ^ (32 * (u ^ (2 * (n & 1))))) + n * 32 * kTile * 2);
-        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, weights[u], acc[n], 0, 0, 0);
-      }
+  };
+  auto meet = [&]() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   };
 
   if (count > 0) {
-    MetaLoad ml;
-    int next_page = -1;
-    if (wave == 0) {
-      meta_store(0, meta_load(0, page_of(0)));
-      meta_store(1, meta_load(1, page_of(1)));
-      next_page = page_of(2);
+    // the wave's own tile of Meta, and the pages of the one after
+    int mine = wave;
+    MetaLoad ml = meta_load(mine, page_of(mine));
+    int next_page = page_of(mine + C::kWaves);
+    auto meta_next = [&](int e) {
+      meta_store(mine, ml, e);
+      mine += C::kWaves;
+      ml = meta_load(mine, next_page);
+      next_page = page_of(mine + C::kWaves);
+    };
+    // the first ones come together and share an E
+    static_assert(kMetaAhead <= C::kWaves, "");
+    if (wave < kMetaAhead) {
+      const int e_own = exponent_of(ml);
+      if (lane == 0) metas[kMetas - 1 - wave].e = e_own;
     }
-    __syncthreads();
-    Codes c;
-    codes_load(0, c);
-    codes_store(0, c);
-    __syncthreads();
-    for (int t = 0; t < count; ++t) {
-      if (t + 1 < count) codes_load(t + 1, c);
-      if (wave == 0) {
-        ml = meta_load(t + 2, next_page);
-        next_page = page_of(t + 3);
+    meet();
+    int e_first = kNoExponent;
+#pragma unroll
+    for (int i = 0; i < kMetaAhead; ++i) e_first = max(e_first, metas[kMetas - 1 - i].e);
+    meet();
+    if (wave < kMetaAhead) meta_next(e_first);
+    meet();
+    // Tile t's codes are asked for two tiles before they are written to LDS, a tile before its turn.  Two tiles to a trip of the loop; those
+    // past the last are like any other, with keys that nobody sees.
+    const int trips = (count + 1) / 2;
+    Codes c0 = codes_load(0), c1 = codes_load(1);
+    codes_store(0, c0, grids_load(0));
+    c0 = codes_load(2);
+    meet();
+    auto meta_due = [&](int t) {
+      if (mine == t + kMetaAhead) {
+        const int before = __builtin_amdgcn_readfirstlane(metas[(t + kMetaAhead - 1) & (kMetas - 1)].e);
+        meta_next(max(before, exponent_of(ml)));
       }
-      const int key0 = begin + t * kTile;
-      if (working && key0 < hi_b && key0 + kTile > lo_a) compute(t);
-      if (t + 1 < count) codes_store(t + 1, c);
-      if (wave == 0) meta_store(t + 2, ml);
-      __syncthreads();
+    };
+    f32x16v s[2];
+    f16x8 weights[4];
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    if constexpr (C::kTurns) {
+      // One half of the waves -- one on each SIMD -- multiplies (the values of the tile before, the keys of this one) while the other
+      // half works out weights and makes the next tile's codes float16; then they change places.  The first half writes the
+      // keys, the second the values: a slot is written when both halves have read what was in it.
+      // (All waves in step, with a barrier per tile and one tile's codes on their way: 1006 us in place of TURNS for two chunks of up to 2048
+      // tokens, 32 heads of 128.)
+      const bool second = wave >= C::kWaves / 2;
+      if (second) meet();
+      if (working) multiply(no, yes, 0, weights, s);
+      meet();
+      for (int i = 0, t = 0; i < trips; ++i, t += 2) {
+        Grids g = grids_load(t + 1);
+        if (working) soften(t, s, weights);
+        codes_store(t + 1, c1, g);
+        meet();
+        c1 = codes_load(t + 3);
+        meta_due(t);
+        if (working) multiply(yes, yes, t + 1, weights, s);
+        meet();
+        g = grids_load(t + 2);
+        if (working) soften(t + 1, s, weights);
+        codes_store(t + 2, c0, g);
+        meet();
+        c0 = codes_load(t + 4);
+        meta_due(t + 1);
+        if (working) multiply(yes, yes, t + 2, weights, s);
+        meet();
+      }
+      if (!second) meet();
+    } else {
+      auto turn = [&](int t) {
+        if (!working) return;
+        multiply(no, yes, t, weights, s);
+        soften(t, s, weights);
+        multiply(yes, no, t + 1, weights, s);
+      };
+      for (int i = 0, t = 0; i < trips; ++i, t += 2) {
+        turn(t);
+        codes_store(t + 1, c1, grids_load(t + 1));
+        c1 = codes_load(t + 3);
+        meta_due(t);
+        meet();
+        turn(t + 1);
+        codes_store(t + 2, c0, grids_load(t + 2));
+        c0 = codes_load(t + 4);
+        meta_due(t + 1);
+        meet();
+      }
     }
   }
   if (!live) return;
-  l += __shfl_xor(l, 32);
-  const float unit = e == -1000 ? 0.f : ldexpf(1.f, e - 7);
+  const float l = sum[0];
+  const float unit = e == kNoExponent ? 0.f : ldexpf(1.f, e - 7);
   if (a.splits > 1) {
     const int64_t at = ((int64_t)split * a.t + token) * a.hq + qhead;
     if (h == 0) {
@@ -413,7 +575,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
 template <int BITS, int DP>
 bool chunk_launch(const AttendArgs& a, hipStream_t s) {
   using C = Chunk<DP>;
-  constexpr int kBytes = 2 * C::kBuffer + 4 * (int)sizeof(Meta);
+  constexpr int kBytes = C::kBuffers + C::kQueryBytes + kMetas * (int)sizeof(Meta);
   if (!lds_opt_in<attend_chunk_kernel<BITS, DP>>(kBytes)) return false;
   const int tiles = (int)ceil_div((int64_t)a.max_q * a.group, C::kRows);
   const int64_t blocks = ceil_div((int64_t)a.b * a.c.heads, 8) * 8 * tiles * a.splits;
