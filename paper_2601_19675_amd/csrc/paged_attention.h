@@ -26,11 +26,13 @@ struct AttendArgs {
   KvCache c;
   float scale;                           // softmax_scale log2(e): scores are powers of two
   int t, b, hq, group, d, max_q, max_kv, causal, window;
-  int splits, split_keys;                // splits > 1: partial results go to part and ml
+  int splits;                            // > 1: workgroups have shares of the work, and partial results go to part and ml
   int least_share;                       // rows form: blocks of 128 keys that a workgroup takes at least
-  float* part;                           // [part][token][head][d]: sums of weight times value
-  float* ml;                             // [part][token][head][2]: the maximum they are relative to, the sum of the weights
-  int* parts;                            // rows form: [token], how many there are
+  int slot_rows;                         // chunk form: rows of a part
+  // rows form: [part][token][head][...]; chunk form: [share][item it ends, item it begins][row][...]
+  float* part;                           // [...][d]: sums of weight times value
+  float* ml;                             // [...][2]: the maximum they are relative to, the sum of the weights
+  int* parts;                            // rows form: [token], how many there are; chunk form: [share][4], see there
 };
 
 // a sequence's queries and keys
@@ -111,7 +113,9 @@ __device__ __forceinline__ f16x2 to_f16(float a, float b) {
 }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-int paged_attention_chunk_rows(int64_t d);   // query rows of a workgroup
+constexpr int kChunkShares = 256, kChunkRows = 256;   // workgroups that have shares; query rows of a workgroup at most
+constexpr int kSharedChunkKeys = 2048;                 // shorter contexts are not shared out
+int64_t paged_attention_chunk_items(const AttendArgs& a);   // tiles of rows, at most
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s);
 
 }  // namespace ptq

@@ -441,8 +441,8 @@ __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
   }
   const Sequence q = sequence_of(a, seq);
   if (tok < q.first || tok - q.first >= min(q.queries, a.max_q)) return;
-  const int parts = a.parts ? a.parts[tok] : max(1, min(a.splits, (q.end - q.begin + a.split_keys - 1) / a.split_keys));
-  if (a.parts && parts == 1) return;   // written by the one workgroup that had it
+  const int parts = a.parts[tok];
+  if (parts == 1) return;   // written by the one workgroup that had it
   const int64_t first = (int64_t)tok * a.hq + h, step = (int64_t)a.t * a.hq;
   float top = kNoScore, sum = 0.f;
   for (int s = lane; s < parts; s += 64) top = fmaxf(top, a.ml[2 * (first + s * step)]);
@@ -477,6 +477,7 @@ int64_t most_splits(int64_t rows, int64_t max_kv) {
   return std::max<int64_t>(1, std::min<int64_t>(ceil_div(max_kv, 256), kPartRows / std::max<int64_t>(rows, 1)));
 }
 
+constexpr int64_t kLongKeys = 8192;
 constexpr int kShares = 512;          // workgroups that share the contexts: two to a compute unit
 int64_t shares(int64_t hkv) { return std::max<int64_t>(1, kShares / hkv); }
 
@@ -496,9 +497,12 @@ bool rows_launch(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
+// which form is taken is not known here: what the larger one needs
 size_t paged_attention_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
   const int64_t rows = hq * t, splits = most_splits(rows, max_kv);
-  return splits <= 1 ? 0 : align_up((size_t)(splits * rows * (d + 2) + t) * sizeof(float), 256);
+  const int64_t rows_form = splits <= 1 ? 0 : splits * rows * (d + 2) + t;
+  const int64_t chunk_form = max_kv < kSharedChunkKeys ? 0 : 2 * kChunkShares * std::min<int64_t>(kChunkRows, rows) * (d + 2) + 4 * kChunkShares;
+  return align_up((size_t)std::max(rows_form, chunk_form) * sizeof(float), 256);
 }
 
 ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
@@ -520,22 +524,28 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
   const bool rows_form = max_q * a.group <= kRows;
   // the keys a split has to get through: those in the window, if there is one
   const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, window + max_q + 63) : max_kv;
-  const int64_t most = most_splits(hq * t, max_kv);
   if (rows_form) {
     // Shares cost a second kernel and its launch (4 us), which 2048 keys in one workgroup take (6 us from 256 keys on): shorter contexts
     // stay whole, and so do more sequences and heads than four rounds of workgroups.
-    a.splits = keys < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)most;
+    a.splits = keys < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)most_splits(hq * t, max_kv);
     // 512 keys at least to a share, and a sequence's parts fit the workspace
     a.least_share = a.splits > 1 ? (int)std::max<int64_t>(4, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
   } else {
-    const int64_t blocks = b * hkv * ceil_div(max_q * a.group, paged_attention_chunk_rows(d));
-    a.splits = (int)std::min<int64_t>(most, std::max<int64_t>(1, 512 / blocks));
-    a.split_keys = (int)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), a.splits), 256) * 256);
-    a.splits = (int)std::max<int64_t>(1, ceil_div(keys, a.split_keys));
+    const int64_t items = paged_attention_chunk_items(a);
+    // Workgroups run in rounds, one to a compute unit, and the host does not know how much each has to do.  Shares cost each workgroup
+    // a second item's queries and half done outputs, and a second kernel: they are taken where the last round would leave a fifth of
+    // the compute units idle or more (us, whole | in shares, 128 channels: 8 items of 2048 keys 81 | 47, 128 of up to 1024 52 | 60, 256 of
+    // up to 4096 164 | 175; 64 channels: 324 of 2500 161 | 133, 576 of 5000 434 | 394), and for any number where contexts are long, which
+    // are seldom the same (768 items of 8192: 906 | 961; 320 of 16384: 1236 | 905; two sequences of 16384 and 8283: 914 | 836).
+    const int64_t rounds = ceil_div(items, kChunkShares), idle = rounds * kChunkShares - items;
+    const bool shared = keys >= kLongKeys || (keys >= kSharedChunkKeys && 5 * idle >= rounds * kChunkShares);
+    a.splits = !shared || items >= 4 * kChunkShares || items * ceil_div(max_kv, 64) > INT32_MAX / 4 ? 1 : 2;
+    a.slot_rows = (int)std::min<int64_t>(kChunkRows, hq * t);
   }
+  const int64_t part_rows = rows_form ? a.splits * t * hq : 2 * kChunkShares * a.slot_rows;
   a.part = static_cast<float*>(ws);
-  a.ml = a.part + (int64_t)a.splits * t * hq * d;
-  a.parts = rows_form ? reinterpret_cast<int*>(a.ml + (int64_t)a.splits * t * hq * 2) : nullptr;
+  a.ml = a.part + part_rows * d;
+  a.parts = reinterpret_cast<int*>(a.ml + part_rows * 2);
   if (rows_form) {
     const bool launched = bits == 8 ? (d <= 64 ? rows_launch<8, 64>(a, s) : d <= 128 ? rows_launch<8, 128>(a, s) : rows_launch<8, 256>(a, s))
                                     : (d <= 64 ? rows_launch<4, 64>(a, s) : d <= 128 ? rows_launch<4, 128>(a, s) : rows_launch<4, 256>(a, s));
@@ -544,7 +554,7 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
     const ptq_status rc = paged_attention_chunk_launch(a, bits, s);
     if (rc != PTQ_OK) return rc;
   }
-  if (a.splits > 1) attend_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(a);
+  if (rows_form && a.splits > 1) attend_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(a);
   PTQ_HIP_CHECK_LAUNCH();
   return PTQ_OK;
 }

@@ -2,20 +2,25 @@
 //
 // Rows are the (token, head) pairs of a key head's group.  A wave has 32 of them, the columns of the 32 x 32 x 16 matrix
 // instruction; the workgroup's eight waves (four for d > 128) go through the keys together, 64 at a time.  Half of them bring a tile's key
-// codes, the other half its value codes: they are asked for a tile ahead, made float16 in registers once for all rows, and
+// codes, the other half its value codes: they are asked for two tiles ahead, made float16 in registers once for all rows, and
 // written to LDS as the matrix instructions want them -- keys [key][d] as the whole numbers code - zero, values [d][key], transposed
-// with byte permutes.  What the page table, scales and zeros say of a tile is brought by the first wave another tile ahead.
+// with byte permutes.  What the page table, scales and zeros say of a tile is brought by the waves in turn, four tiles ahead.
 //
 //   S' = K Q'   (keys are rows, so a lane has scores of one query row, and they leave the instruction in the order in which the
 //               second product takes them: no exchange)        y = ks S',   p = 2^(y f - M),   O' = V' p
 //
 // Q' is the row times a power of two that makes it fit float16, f = softmax_scale log2(e) over that power.  The running maximum moves
 // only when a score is 2^8 above it; until then weights are below 2^8.  V' = vs 2^(7 - E) (code - zero) in float16, E the largest
-// exponent of a value's scale so far (all products stay below 2^15; when E grows, sums shrink).  Roundings beside those to float16:
-// float32.
+// exponent of a value's scale so far (all products stay below 2^15; when E grows, sums shrink).  Roundings: weights and V' to
+// float16, 2^-11 each, of which bfloat16 outputs see nothing; the sum of the weights is of the rounded ones, a channel of ones beside the
+// values', so that the rounding of a weight drops out where the values are alike.  All sums are float32.
 //
-// Bound: the matrix instructions (16 d flops a score) and the vector unit beside them (eight instruction slots a score, four of them
-// the power of two) in about equal parts at d = 128.
+// Bound: the vector unit (a score takes about eleven instruction slots, four of them the power of two; a tile's codes another third of
+// that) while the other half of the workgroup has the matrix unit (16 d flops a score, half of the time): 836 us for chunks of 2048
+// and 1035 tokens against 16384 and 8283 keys, 32 heads of 128 channels over 8: 770 TFLOP/s of float16 products.
+//
+// Tiles of rows differ in how many keys they see.  Where that would leave compute units idle, all tiles of keys of all tiles of rows are laid
+// end to end and dealt out in equal shares, and a second kernel joins what several workgroups have of a tile of rows.
 #include <algorithm>
 
 #include "paged_attention.h"
@@ -28,6 +33,9 @@ namespace {
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16v;
 
 constexpr int kTile = 64;   // keys
+// Workgroups that share the work, one to a compute unit.  It is counted in tiles of keys, and what comes before and after an item's
+// tiles (queries, first codes, outputs: 13000 cycles, a tile 3200 to 5900) as kStart of them.
+constexpr int kShares = kChunkShares, kStart = 4, kLeastShare = 2 * kStart;
 constexpr int kNoExponent = -1000;   // E before the first value
 constexpr int kMetas = 8, kMetaAhead = 4;   // tiles whose Meta is in LDS, and how far before its turn it is brought there
 
@@ -41,7 +49,7 @@ struct Chunk {
   static constexpr int kRing = 2;                            // tiles of codes in LDS
   static constexpr int kBuffers = kRing * (kKeyBytes + kValBytes);
   // Steps of d whose queries wait in LDS: at d = 128 the registers of two waves to a SIMD do not hold all of them beside what a turn needs
-  // (and what the compiler spills goes to memory: 1584 us in place of TURNS)
+  // (and what the compiler spills goes to memory: 1584 us in place of 914)
   static constexpr int kQuerySteps = DP == 128 ? 4 : 0;
   static constexpr int kQueryBytes = kQuerySteps * 16 * 2 * kRows;
   static constexpr int kHalf = kThreads / 2;
@@ -78,31 +86,107 @@ __device__ __forceinline__ int wave_max_int(int v) {
              max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 
+// the keys that some row of a tile of rows sees
+template <int ROWS>
+__device__ __forceinline__ void span_of(const AttendArgs& a, const Sequence& q, int tile, int& begin, int& end) {
+  const int rows = min(q.queries, a.max_q) * a.group;
+  int unused;
+  visible(a, q, tile * ROWS / a.group, begin, unused);
+  visible(a, q, (min((tile + 1) * ROWS, rows) - 1) / a.group, unused, end);
+  begin = max(q.begin, begin & ~(kTile - 1));
+  end = min(end, q.end);
+}
+// what a tile of rows counts for
+template <int ROWS>
+__device__ __forceinline__ int item_work(const AttendArgs& a, int seq, int tile) {
+  const Sequence q = sequence_of(a, seq);
+  if (tile * ROWS >= min(q.queries, a.max_q) * a.group) return 0;
+  int begin, end;
+  span_of<ROWS>(a, q, tile, begin, end);
+  return kStart + max(0, end - begin + kTile - 1) / kTile;
+}
+
 template <int BITS, int DP>
 __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(AttendArgs a, int tiles) {
   using C = Chunk<DP>;
   constexpr int kSteps = DP / 16, kOut = DP / 32;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   Meta* metas = reinterpret_cast<Meta*>(smem + C::kBuffers + C::kQueryBytes);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // groups (sequence, key head) go round the dies, so that a group's row tiles share its codes in one L2; the last rows, which
-  // see most, first
-  const int items = tiles * a.splits, die = blockIdx.x & 7, idx = blockIdx.x >> 3;
-  const int group = idx / items * 8 + die, item = idx % items;
-  if (group >= a.b * a.c.heads) return;
-  const int seq = group / a.c.heads, head = group % a.c.heads, tile = tiles - 1 - item % tiles, split = item / tiles;
+  // the workgroup's share: `left` pieces of work from piece `off` of an item on; `at` is the item's place in the order of all
+  int seq, head, tile, off = 0, left = INT32_MAX, at = 0, each = 1;
+  int4 begun{0, 0, 0, 0};   // parts of the item that this share begins and does not end (0: there is none); its sequence, key head, tile
+  int4* const begun_at = reinterpret_cast<int4*>(a.parts) + (blockIdx.x & 7) * (kShares / 8) + (blockIdx.x >> 3);
+  if (a.splits > 1) {
+    // consecutive shares on one die, where they find each other's codes in the L2
+    const int pairs = a.b * tiles, lane = threadIdx.x & 63;
+    int total = 0;   // of one key head
+    for (int p0 = 0; p0 < pairs; p0 += kWave) total += p0 + lane < pairs ? item_work<C::kRows>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o);
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int all = total * a.c.heads;
+    each = max(kLeastShare, (all + kShares - 1) / kShares);
+    const int64_t mine = ((blockIdx.x & 7) * (kShares / 8) + (blockIdx.x >> 3)) * (int64_t)each;
+    if (mine >= all) {
+      if (threadIdx.x == 0) *begun_at = begun;
+      return;
+    }
+    left = min(each, all - (int)mine);
+    head = (int)mine / total;
+    const int within = (int)mine % total;
+    int before = 0;
+    for (int p0 = 0;; p0 += kWave) {   // the first item that reaches past `within`
+      const int n = p0 + lane < pairs ? item_work<C::kRows>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+      int upto = n;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int v = __shfl_up(upto, o);
+        if (lane >= o) upto += v;
+      }
+      const uint64_t past = __ballot(before + upto > within);
+      if (past) {
+        const int p = __builtin_ctzll(past);
+        seq = (p0 + p) / tiles;
+        tile = (p0 + p) % tiles;
+        before += __builtin_amdgcn_readlane(upto, p) - __builtin_amdgcn_readlane(n, p);
+        break;
+      }
+      before += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    off = within - before;
+    at = (int)mine - off;
+  } else {
+    // groups (sequence, key head) go round the dies, so that a group's row tiles share its codes in one L2; the last rows, which
+    // see most, first
+    const int die = blockIdx.x & 7, idx = blockIdx.x >> 3, group = idx / tiles * 8 + die;
+    if (group >= a.b * a.c.heads) return;
+    seq = group / a.c.heads, head = group % a.c.heads, tile = tiles - 1 - idx % tiles;
+  }
+
+  for (;;) {
+  // (opaque: what follows from it is not kept in registers from one item to the next)
+  const int tid = opaque(threadIdx.x), lane = tid & 63, r = lane & 31, h = lane >> 5;
   const Sequence q = sequence_of(a, seq);
   const int rows = min(q.queries, a.max_q) * a.group, row0 = tile * C::kRows;
-  if (row0 >= rows) return;
-  const int from = q.begin + split * a.split_keys;
-  if (split > 0 && from >= q.end) return;
+  if (row0 >= rows) {   // (a share has something to do yet)
+    if (a.splits == 1) return;
+    tile = 0;
+    if (++seq == a.b) {
+      seq = 0;
+      ++head;
+    }
+    continue;
+  }
 
-  // the keys that some row of the workgroup sees, in this split
-  int lo, hi, lo_a, hi_a, lo_b, hi_b;
-  visible(a, q, row0 / a.group, lo, hi);
-  visible(a, q, (min(row0 + C::kRows, rows) - 1) / a.group, lo_b, hi_b);
-  const int begin = max(from, lo & ~(kTile - 1)), end = min(min(hi_b, q.end), a.splits > 1 ? from + a.split_keys : q.end);
+  // the keys that some row of the workgroup sees, and those of them in this share
+  int lo, hi, lo_a, hi_a, lo_b, hi_b, begin, end;
+  span_of<C::kRows>(a, q, tile, begin, end);
+  const int whole = kStart + max(0, end - begin + kTile - 1) / kTile, take = min(whole - off, left);
+  const bool alone = take == whole;
+  end = min(end, begin + max(0, off + take - kStart) * kTile);
+  begin += max(0, off - kStart) * kTile;
   const int count = end > begin ? (end - begin + kTile - 1) / kTile : 0;
   // ... and those that the wave's rows see: some of them [lo_a, hi_b), all of them [lo_b, hi_a)
   const int wrow = row0 + 32 * wave;
@@ -110,44 +194,6 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   if (working) {
     visible(a, q, wrow / a.group, lo_a, hi_a);
     visible(a, q, (min(wrow + 32, rows) - 1) / a.group, lo_b, hi_b);
-  }
-
-  const int row = wrow + r, token = q.first + row / a.group, qhead = head * a.group + row % a.group;
-  const bool live = row < rows;
-  visible(a, q, live ? row / a.group : 0, lo, hi);
-  if (!live) hi = 0;
-  constexpr int kHeld = kSteps - C::kQuerySteps;   // steps of d of the queries in registers
-  f16x8 fq[kHeld];
-  char* const queries = smem + C::kBuffers + (wave * 64 + lane) * 16;   // the others: [step][wave][lane]
-  float factor;
-  {
-    Run<PTQ_BF16, 8> raw[kSteps];
-    const uint16_t* Q = a.Q + (live ? token * a.q_token + qhead * a.q_head : 0);
-    float top = 0.f;
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) raw[u] = load_run<PTQ_BF16, 8, false>(Q, 16 * u + 8 * h, a.d);
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-      float v[8];
-      run_to_f32<PTQ_BF16, 8>(raw[u], 16 * u + 8 * h, live ? a.d : 0, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.f);
-    }
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const int e = __builtin_amdgcn_frexp_expf(top);
-    factor = fmaxf(ldexpf(fabsf(a.scale), e - 15), 0x1p-126f);   // positive: a score that is not there is -inf times it
-    const float lift = a.scale < 0.f ? -1.f : 1.f;
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
-      float v[8];
-      uint32_t w[4];
-      run_to_f32<PTQ_BF16, 8>(raw[u], 16 * u + 8 * h, live ? a.d : 0, v);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = __builtin_bit_cast(uint32_t, to_f16(ldexpf(lift * v[2 * i], 15 - e), ldexpf(lift * v[2 * i + 1], 15 - e)));
-      if (u < kHeld) fq[u < kHeld ? u : 0] = f16x8_of(w[0], w[1], w[2], w[3]);
-      else *reinterpret_cast<f16x8*>(queries + (u - kHeld) * C::kThreads * 16) = f16x8_of(w[0], w[1], w[2], w[3]);
-    }
   }
 
   const int64_t plane = (a.c.pages * a.c.heads) << a.c.page_shift;
@@ -161,7 +207,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   auto page_of = [&](int t) {   // tile t's key `lane`
     const int key = begin + t * kTile + lane;
     const int p = table[min(key, q.length - 1) >> a.c.page_shift];
-    return key < q.end && (uint32_t)p < (uint64_t)a.c.pages ? p : -1;
+    return key < end && (uint32_t)p < (uint64_t)a.c.pages ? p : -1;
   };
   auto row_of = [&](int t, int page) -> int64_t {
     return page < 0 ? 0 : (((int64_t)page * a.c.heads + head) << a.c.page_shift) + ((begin + t * kTile + lane) & inside);
@@ -191,6 +237,53 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
       o.e = e;
     }
   };
+
+  const int row = wrow + r, token = q.first + row / a.group, qhead = head * a.group + row % a.group;
+  const bool live = row < rows;
+  visible(a, q, live ? row / a.group : 0, lo, hi);
+  if (!live) hi = 0;
+  constexpr int kHeld = kSteps - C::kQuerySteps;   // steps of d of the queries in registers
+  f16x8 fq[kHeld];
+  char* const queries = smem + C::kBuffers + (wave * 64 + lane) * 16;   // the others: [step][wave][lane]
+  float factor;
+  MetaLoad ml;
+  int next_page = -1;
+  {
+    // the wave's first tile of Meta, and the pages of the one after: asked for around the queries
+    int page = -1;
+    if (count > 0) {
+      page = page_of(wave);
+      next_page = page_of(wave + C::kWaves);
+    }
+    Run<PTQ_BF16, 8> raw[kSteps];
+    const uint16_t* Q = a.Q + (live ? token * a.q_token + qhead * a.q_head : 0);
+    float top = 0.f;
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) raw[u] = load_run<PTQ_BF16, 8, false>(Q, 16 * u + 8 * h, a.d);
+    if (count > 0) ml = meta_load(wave, page);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      float v[8];
+      run_to_f32<PTQ_BF16, 8>(raw[u], 16 * u + 8 * h, live ? a.d : 0, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.f);
+    }
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const int e = __builtin_amdgcn_frexp_expf(top);
+    factor = fmaxf(ldexpf(fabsf(a.scale), e - 15), 0x1p-126f);   // positive: a score that is not there is -inf times it
+    const float lift = a.scale < 0.f ? -1.f : 1.f;
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      float v[8];
+      uint32_t w[4];
+      run_to_f32<PTQ_BF16, 8>(raw[u], 16 * u + 8 * h, live ? a.d : 0, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = __builtin_bit_cast(uint32_t, to_f16(ldexpf(lift * v[2 * i], 15 - e), ldexpf(lift * v[2 * i + 1], 15 - e)));
+      if (u < kHeld) fq[u < kHeld ? u : 0] = f16x8_of(w[0], w[1], w[2], w[3]);
+      else *reinterpret_cast<f16x8*>(queries + (u - kHeld) * C::kThreads * 16) = f16x8_of(w[0], w[1], w[2], w[3]);
+    }
+  }
 
   // ---- codes of tile t: loads, then float16 in LDS
   constexpr int KW = BITS / 2, VW = BITS / 4;   // words of a unit: 16 codes | eight codes
@@ -450,10 +543,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   };
 
   if (count > 0) {
-    // the wave's own tile of Meta, and the pages of the one after
-    int mine = wave;
-    MetaLoad ml = meta_load(mine, page_of(mine));
-    int next_page = page_of(mine + C::kWaves);
+    int mine = wave;   // the wave's tile of Meta
     auto meta_next = [&](int e) {
       meta_store(mine, ml, e);
       mine += C::kWaves;
@@ -494,8 +584,8 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
       // One half of the waves -- one on each SIMD -- multiplies (the values of the tile before, the keys of this one) while the other
       // half works out weights and makes the next tile's codes float16; then they change places.  The first half writes the
       // keys, the second the values: a slot is written when both halves have read what was in it.
-      // (All waves in step, with a barrier per tile and one tile's codes on their way: 1006 us in place of TURNS for two chunks of up to 2048
-      // tokens, 32 heads of 128.)
+      // (All waves in step, with a barrier per tile and one tile's codes on their way: 1006 us in place of 914 for two chunks of up to 2048
+      // tokens, 32 heads of 128 channels, 16384 keys.)
       const bool second = wave >= C::kWaves / 2;
       if (second) meet();
       if (working) multiply(no, yes, 0, weights, s);
@@ -540,36 +630,94 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
       }
     }
   }
-  if (!live) return;
-  const float l = sum[0];
-  const float unit = e == kNoExponent ? 0.f : ldexpf(1.f, e - 7);
-  if (a.splits > 1) {
-    const int64_t at = ((int64_t)split * a.t + token) * a.hq + qhead;
-    if (h == 0) {
-      a.ml[2 * at] = m == kNoScore ? kNoScore : m * factor;
-      a.ml[2 * at + 1] = l;
+  if (live) {
+    const float l = sum[0], unit = e == kNoExponent ? 0.f : ldexpf(1.f, e - 7);
+    if (!alone) {
+      // (an item that begins here is the share's last, one that began before is its first)
+      const int64_t slot_row = (int64_t)(2 * ((at + off) / each) + (off == 0)) * a.slot_rows + (row - row0);
+      if (h == 0) {
+        a.ml[2 * slot_row] = m == kNoScore ? kNoScore : m * factor;
+        a.ml[2 * slot_row + 1] = l;
+      }
+#pragma unroll
+      for (int n = 0; n < kOut; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = 32 * n + 8 * j + 4 * h;
+          if (d < a.d)
+            *reinterpret_cast<f32x4*>(a.part + slot_row * a.d + d) =
+                f32x4{acc[n][4 * j] * unit, acc[n][4 * j + 1] * unit, acc[n][4 * j + 2] * unit, acc[n][4 * j + 3] * unit};
+        }
+    } else {
+      const float inv = l == 0.f ? 0.f : unit / l;
+      uint16_t* O = a.O + token * a.o_token + qhead * a.o_head;
+#pragma unroll
+      for (int n = 0; n < kOut; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float v[4] = {acc[n][4 * j] * inv, acc[n][4 * j + 1] * inv, acc[n][4 * j + 2] * inv, acc[n][4 * j + 3] * inv};
+          const int d = 32 * n + 8 * j + 4 * h;
+          if (d < a.d) store_run<PTQ_BF16, 4, false>(O, d, a.d, v);
+        }
+    }
+  }
+  if (a.splits == 1) return;
+  if (off == 0 && !alone) begun = int4{(at + whole - 1) / each - at / each + 1, seq, head, tile};
+  left -= take;
+  if (left <= 0) break;
+  at += whole;
+  off = 0;
+  ++tile;
+  meet();   // the next item's codes go where this one's were
+  }
+  if (threadIdx.x == 0) *begun_at = begun;
+}
+
+// Joins what the shares have of an item that one of them begins: a thread has four channels of a row.
+template <int DP>
+__global__ __launch_bounds__(256) void join_chunk_kernel(AttendArgs a) {
+  using C = Chunk<DP>;
+  const int4 begun = reinterpret_cast<const int4*>(a.parts)[blockIdx.x];
+  const int parts = begun.x, seq = begun.y, head = begun.z, tile = begun.w;
+  const int i = blockIdx.y * 256 + threadIdx.x, local = i / (DP / 4), c = i % (DP / 4) * 4;
+  if (parts == 0 || c >= a.d) return;
+  const Sequence q = sequence_of(a, seq);
+  const int row = tile * C::kRows + local;
+  if (row >= min(q.queries, a.max_q) * a.group) return;
+  float top = kNoScore, sum = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  auto some = [&](int p0, auto n_) {   // parts p0, p0 + 1, ...; those past the last count nothing
+    constexpr int n = decltype(n_)::value;
+    f32x4 v[n];
+    f32x2 ml[n];
+    float t = top;
+#pragma unroll
+    for (int j = 0; j < n; ++j) {   // the first is in its share's second place, the others in their shares' first
+      const int p = min(p0 + j, parts - 1);
+      const int64_t at = (int64_t)(2 * (blockIdx.x + p) + (p == 0)) * a.slot_rows + local;
+      v[j] = *reinterpret_cast<const f32x4*>(a.part + at * a.d + c);
+      ml[j] = *reinterpret_cast<const f32x2*>(a.ml + 2 * at);
     }
 #pragma unroll
-    for (int n = 0; n < kOut; ++n)
+    for (int j = 0; j < n; ++j) t = fmaxf(t, ml[j][0]);
+    const float f = exp2_fast(top - t);
+    sum *= f;
+    o *= f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int d = 32 * n + 8 * j + 4 * h;
-        if (d < a.d)
-          *reinterpret_cast<f32x4*>(a.part + at * a.d + d) =
-              f32x4{acc[n][4 * j] * unit, acc[n][4 * j + 1] * unit, acc[n][4 * j + 2] * unit, acc[n][4 * j + 3] * unit};
-      }
-  } else {
-    const float inv = l == 0.f ? 0.f : unit / l;
-    uint16_t* O = a.O + token * a.o_token + qhead * a.o_head;
-#pragma unroll
-    for (int n = 0; n < kOut; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float v[4] = {acc[n][4 * j] * inv, acc[n][4 * j + 1] * inv, acc[n][4 * j + 2] * inv, acc[n][4 * j + 3] * inv};
-        const int d = 32 * n + 8 * j + 4 * h;
-        if (d < a.d) store_run<PTQ_BF16, 4, false>(O, d, a.d, v);
-      }
-  }
+    for (int j = 0; j < n; ++j) {
+      const float w = p0 + j < parts ? exp2_fast(ml[j][0] - t) : 0.f;
+      sum += w * ml[j][1];
+      o += w * v[j];
+    }
+    top = t;
+  };
+  int p = 0;
+  for (; parts - p > 4; p += 16) some(p, std::integral_constant<int, 16>{});
+  if (p < parts) some(p, std::integral_constant<int, 4>{});
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that sees nothing: zeros
+  const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  const int64_t token = q.first + row / a.group, qhead = head * a.group + row % a.group;
+  store_run<PTQ_BF16, 4, false>(a.O + token * a.o_token + qhead * a.o_head, c, a.d, v);
 }
 
 template <int BITS, int DP>
@@ -578,15 +726,20 @@ bool chunk_launch(const AttendArgs& a, hipStream_t s) {
   constexpr int kBytes = C::kBuffers + C::kQueryBytes + kMetas * (int)sizeof(Meta);
   if (!lds_opt_in<attend_chunk_kernel<BITS, DP>>(kBytes)) return false;
   const int tiles = (int)ceil_div((int64_t)a.max_q * a.group, C::kRows);
-  const int64_t blocks = ceil_div((int64_t)a.b * a.c.heads, 8) * 8 * tiles * a.splits;
+  const int64_t blocks = a.splits > 1 ? kShares : ceil_div((int64_t)a.b * a.c.heads, 8) * 8 * tiles;
   if (blocks > INT32_MAX) return false;
   attend_chunk_kernel<BITS, DP><<<(unsigned)blocks, C::kThreads, kBytes, s>>>(a, tiles);
+  if (a.splits > 1) join_chunk_kernel<DP><<<dim3(kShares, C::kRows * (DP / 4) / 256), 256, 0, s>>>(a);
   return true;
 }
 
 }  // namespace
 
-int paged_attention_chunk_rows(int64_t d) { return d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows; }
+int64_t paged_attention_chunk_items(const AttendArgs& a) {
+  const int64_t rows = a.d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows;
+  static_assert(Chunk<128>::kRows <= kChunkRows && Chunk<64>::kRows == Chunk<128>::kRows, "");
+  return (int64_t)a.b * a.c.heads * ceil_div((int64_t)a.max_q * a.group, rows);
+}
 
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s) {
   const bool launched = bits == 8 ? (a.d <= 64 ? chunk_launch<8, 64>(a, s) : a.d <= 96 ? chunk_launch<8, 96>(a, s)

@@ -94,6 +94,15 @@ def test_long_context_of_one_sequence_is_split():
     p.check(True, 2500, absolute=True)
 
 
+@pytest.mark.parametrize("bits,d,page", [(8, 128, 16), (4, 64, 16), (8, 256, 32), (4, 80, 1)])
+@pytest.mark.parametrize("window", [0, 700])
+def test_work_dealt_out_in_shares(bits, d, page, window):
+    """Tiles of rows that several workgroups share, others that one has whole, and sequences without queries or keys between them."""
+    p = Problem([3000, 700, 0, 5000, 90, 40, 1300], [300, 40, 20, 33, 0, 5, 130], 6, 2, d, bits, page, seed=12)
+    p.check(True, window, absolute=True)
+    p.check(False, window, absolute=True)
+
+
 @pytest.mark.parametrize("kv,new", [([4000, 900], [33, 1]), ([700, 650], [700, 600])])
 def test_its_stream_and_graph(kv, new):
     p = Problem(kv, new, 8, 2, 128, 8, 16, seed=7)
