@@ -458,7 +458,7 @@ def _tokens():
 def ptq_rmsnorm_quantize(X: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, gamma: torch.Tensor | None = None,
                          residual: torch.Tensor | None = None, residual_out: torch.Tensor | None = None, eps: float = 1e-5,
                          normalize: bool = True) -> None:
-    """codes (int8 t x n), scales (float32 t) <- the norm of X + residual (t x n, bfloat16 or float32) times gamma;
+    """codes (int8 t x n), scales (float32 t) <- the norm of X + residual (t x n, bfloat16 or float32) times gamma (n, of that type);
     residual_out <- X + residual.  normalize=False: the rows as they are."""
     rc = (_TOKENS or _tokens()).rmsnorm_quantize(X, codes, scales, gamma, residual, residual_out, eps, normalize)
     if rc:
