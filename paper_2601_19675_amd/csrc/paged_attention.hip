@@ -528,8 +528,9 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
     // Shares cost a second kernel and its launch (4 us), which 2048 keys in one workgroup take (6 us from 256 keys on): shorter contexts
     // stay whole, and so do more sequences and heads than four rounds of workgroups.
     a.splits = keys < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)most_splits(hq * t, max_kv);
-    // 512 keys at least to a share, and a sequence's parts fit the workspace
-    a.least_share = a.splits > 1 ? (int)std::max<int64_t>(4, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
+    // 256 keys at least to a share (two contexts of 4129, 32 heads of 128 channels over 8: 17.3 us, with 512 21.3; from four contexts of 8192
+    // on no difference), and a sequence's parts fit the workspace
+    a.least_share = a.splits > 1 ? (int)std::max<int64_t>(2, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
   } else {
     const int64_t items = paged_attention_chunk_items(a);
     // Workgroups run in rounds, one to a compute unit, and the host does not know how much each has to do.  Shares cost each workgroup
