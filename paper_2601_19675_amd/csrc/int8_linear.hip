@@ -4,8 +4,8 @@
 // no transposition and no unpacking.  Sums are 32-bit integers, hence exact and independent of the order (n <= 131056 keeps
 // 128 * 128 * n below 2^31); the epilogue converts, scales twice and adds, each rounded to float32.
 //
-// Up to 64 tokens the weight's bytes are the bound: its rows go straight from memory into registers (skinny_kernel).  Beyond
-// that the products are: tiles of W rows x tokens staged in LDS (tile_kernel).
+// With few tokens the weight's bytes are the bound: its rows go straight from memory into registers (skinny_kernel).  Beyond
+// that the products are: tiles of W rows x tokens staged in LDS (tile_kernel).  form_of has the rule.
 #include <algorithm>
 
 #include "lds_dma.h"
@@ -57,7 +57,7 @@ __device__ __forceinline__ void load_channels(const LinearArgs& a, int row, floa
 // ---- few tokens ---------------------------------------------------------------------------------------------
 // A workgroup takes 16 rows of W; its eight waves share out the 64-byte steps of k and meet in LDS.  Every byte of W is read
 // once, eight loads of 16 bytes a lane on their way: one trip to memory for n = 4096.  The tokens (columns of the matrix
-// instruction, TB x 16 of them) come from the L2.
+// instruction, TB x 16 of them) come from the L2.  One token, 4096 x 4096: 5.3 us for 16.8 MB (3.6 at the rate of a copy).
 constexpr int kSkinnyWaves = 8, kSkinnyAhead = 8;
 
 template <int DT, int TB>
@@ -119,6 +119,9 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(LinearArgs a)
 //
 // If n is not a multiple of 128 the stage that holds the rest comes first, with its lanes past n sent out of the buffer's range
 // (zeros): the main loop does not have to know about it.
+//
+// 8192 tokens x 11008 x 4096: 348 us, 2.1 POP/s, the rate of a large library product.  333 tokens x 4096 x 11008: 27.3 us, 1.1 POP/s: 192 tiles of
+// 86 stages that take 0.26 us each, of which the products are 0.11.
 
 __device__ __forceinline__ int turn(int r) { return (r & 7) ^ ((r >> 3) & 1); }
 
@@ -416,7 +419,7 @@ __global__ __launch_bounds__(64) void split_sum_kernel(LinearArgs a, const int* 
   store_outputs<DT, 8>(a, token, row, a.as[token], v, ws, bias);
 }
 
-constexpr int kSkinnyTokens = 64;
+constexpr int kSkinnyTokens = 64;   // that skinny_kernel has columns for
 struct Form {
   int tile;   // -1: few tokens
   TilePlan plan;
@@ -433,8 +436,6 @@ constexpr TileShape kTiles[] = {{4, 4, 10.0, 1.03, 1.70}, {2, 2, 5.0, 0.30, 0.55
 // 29.3.  Splits cost the partial sums' way through memory and a second kernel; only the smallest tile is worth them (few tokens, small m).
 Form form_of(int64_t t, int64_t m, int64_t n) {
   Form f{};
-  f.tile = -1;
-  if (t <= kSkinnyTokens) return f;
   const int64_t stages = ceil_div(n, SK);
   double best = 1e300;
   for (int i = 0; i < (int)(sizeof(kTiles) / sizeof(kTiles[0])); ++i) {
@@ -454,6 +455,13 @@ Form form_of(int64_t t, int64_t m, int64_t n) {
         f.plan = TilePlan{(int)tm, (int)tt, (int)used, (int)stages, (int)each, nullptr};
       }
     }
+  }
+  if (t <= kSkinnyTokens) {
+    // The few-token kernel by what it took, in us, beside tiles (m x n: tokens, few-token kernel | tiles): 4096 x 4096: 16 5.8 | 10.1, 32 7.8 | 10.4,
+    // 64 12.3 | 10.9; 11008 x 4096: 8 10.8 | 10.8, 16 12.9 | 11.0, 64 28.9 | 12.0; 4096 x 11008: 16 13.2 | 14.8, 32 19.2 | 15.2.  The
+    // estimate for tiles is a sixth high where they are so few.
+    const double few = 2.0 + (double)m * (double)n / 16777216.0 * (2.6 + 0.1 * (double)t + (t <= 16 ? 0.0 : t <= 32 ? 1.0 : 3.0));
+    if (few < 0.85 * best) f.tile = -1;
   }
   return f;
 }

@@ -14,7 +14,8 @@ def launched(t, m, n, odt=1):
 
 @pytest.mark.parametrize("t,m,n,kernel,blocks,summed", [
     (1, 4096, 4096, "skinny_kernelILi1ELi1E", 256, False), (17, 100, 64, "skinny_kernelILi1ELi2E", 7, False),
-    (64, 4096, 4096, "skinny_kernelILi1ELi4E", 256, False),
+    (64, 1024, 4096, "skinny_kernelILi1ELi4E", 64, False),
+    (64, 4096, 4096, "tile_kernelILi1ELi1ELi2E", 64, False),        # tokens enough for tiles, if not for all of one
     (512, 4096, 4096, "tile_kernelILi1ELi1ELi2E", 256, False),      # 64 x 128 tiles: one to a compute unit
     (65, 70, 11008, "tile_kernelILin1ELi1ELi2E", 30, True),          # few of them: k in splits
     (1024, 4096, 4096, "tile_kernelILi1ELi2ELi2E", 256, False),
