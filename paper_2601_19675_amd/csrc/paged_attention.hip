@@ -528,7 +528,7 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
   a.causal = causal, a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
   const bool rows_form = max_q * a.group <= kRows;
   // the keys a split has to get through: those in the window, if there is one
-  const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, window + max_q + 63) : max_kv;
+  const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, (int64_t)a.window + max_q + 63) : max_kv;
   if (rows_form) {
     // Shares cost a second kernel and its launch (4 us), which 2048 keys in one workgroup take (6 us from 256 keys on): shorter contexts
     // stay whole, and so do more sequences and heads than four rounds of workgroups.

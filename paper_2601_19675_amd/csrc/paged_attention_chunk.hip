@@ -636,7 +636,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
       // (an item that begins here is the share's last, one that began before is its first)
       const int64_t slot_row = (int64_t)(2 * ((at + off) / each) + (off == 0)) * a.slot_rows + (row - row0);
       if (h == 0) {
-        a.ml[2 * slot_row] = m == kNoScore ? kNoScore : m * factor;
+        a.ml[2 * slot_row] = m == kNoScore ? kNoScore : fmaxf(m * factor, kNoScore);
         a.ml[2 * slot_row + 1] = l;
       }
 #pragma unroll

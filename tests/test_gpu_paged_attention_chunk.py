@@ -103,6 +103,16 @@ def test_work_dealt_out_in_shares(bits, d, page, window):
     p.check(False, window, absolute=True)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+def test_pages_missing_and_scales_without_a_value_in_shares(bits):
+    p = Problem([5000, 2600], [40, 20], 4, 2, 64, bits, 16, seed=21)
+    p.table[0, 10:200] = -1
+    p.table[1, :] = 2 ** 30   # nothing there: zeros
+    p.check(absolute=True)
+    p.scales[1, p.table[0, 4000 // 16], 1, 0] = np.nan
+    p.check(absolute=True)
+
+
 @pytest.mark.parametrize("kv,new", [([4000, 900], [33, 1]), ([700, 650], [700, 600])])
 def test_its_stream_and_graph(kv, new):
     p = Problem(kv, new, 8, 2, 128, 8, 16, seed=7)
