@@ -15,9 +15,10 @@
 // float16, 2^-11 each, of which bfloat16 outputs see nothing; the sum of the weights is of the rounded ones, a channel of ones beside the
 // values', so that the rounding of a weight drops out where the values are alike.  All sums are float32.
 //
-// Bound: the vector unit (a score takes about eleven instruction slots, four of them the power of two; a tile's codes another third of
-// that) while the other half of the workgroup has the matrix unit (16 d flops a score, half of the time): 836 us for chunks of 2048
-// and 1035 tokens against 16384 and 8283 keys, 32 heads of 128 channels over 8: 770 TFLOP/s of float16 products.
+// Bound: a turn of one half of the workgroup, softmax (a score takes about eleven instruction slots, four of them the power of two) and the codes'
+// way to float16, while the other half has the matrix unit (16 d flops a score): vector instructions are issued 43 % of the time, the
+// matrix unit is busy 39 %.  Chunks of 2048 and 1035 tokens against 16384 and 8283 keys, 32 heads of 128 channels over 8: 823 us,
+// 785 TFLOP/s of float16 products.
 //
 // Tiles of rows differ in how many keys they see.  Where that would leave compute units idle, all tiles of keys of all tiles of rows are laid
 // end to end and dealt out in equal shares, and a second kernel joins what several workgroups have of a tile of rows.
