@@ -9,11 +9,15 @@
 //   S' = K Q'   (keys are rows, so a lane has scores of one query row, and they leave the instruction in the order in which the
 //               second product takes them: no exchange)        y = ks S',   p = 2^(y f - M),   O' = V' p
 //
-// Q' is the row times a power of two that makes it fit float16, f = softmax_scale log2(e) over that power.  The running maximum moves
-// only when a score is 2^8 above it; until then weights are below 2^8.  V' = vs 2^(7 - E) (code - zero) in float16, E the largest
-// exponent of a value's scale so far (all products stay below 2^15; when E grows, sums shrink).  Roundings: weights and V' to
-// float16, 2^-11 each, of which bfloat16 outputs see nothing; the sum of the weights is of the rounded ones, a channel of ones beside the
-// values', so that the rounding of a weight drops out where the values are alike.  All sums are float32.
+// Q' is the row times a power of two that makes it fit float16, f = softmax_scale log2(e) over that power.  The running maximum M, a whole
+// number, moves only when one of the row's scores is 2^8 above it; until then weights are below 2^8.  V' = 2^4 vs (code - zero) in float16, whose
+// normal numbers hold that for scales from 2^-18 up to 2^4 (4 bits: 2^8).  Roundings: weights and V' to float16, 2^-11 each, of which
+// bfloat16 outputs see nothing; the sum of the weights is of the rounded ones, a channel of ones beside the values', so that the rounding of a
+// weight drops out where the values are alike.  All sums are float32.
+//
+// A value's scale outside that range is brought to its nearer end by a power of two 2^x, which goes into the weights instead: a row that sees such a key
+// takes 2^(y f + x - A) with a running maximum A of its own for the numerator, 2^(y f - M) for the sum, and joins them at its end.  This is
+// decided by row, and nothing that the other rows see enters into it: a key that a row does not see leaves its result as it is, bit by bit.
 //
 // Bound: a turn of one half of the workgroup, softmax (a score takes about eleven instruction slots, four of them the power of two) and the codes'
 // way to float16, while the other half has the matrix unit (16 d flops a score): vector instructions are issued 43 % of the time, the
@@ -37,7 +41,7 @@ constexpr int kTile = 64;   // keys
 // Workgroups that share the work, one to a compute unit.  It is counted in tiles of keys, and what comes before and after an item's
 // tiles (queries, first codes, outputs: 13000 cycles, a tile 3200 to 5900) as kStart of them.
 constexpr int kShares = kChunkShares, kStart = 4, kLeastShare = 2 * kStart;
-constexpr int kNoExponent = -1000;   // E before the first value
+constexpr int kValueLift = 4;         // V' = 2^kValueLift vs (code - zero)
 constexpr int kMetas = 8, kMetaAhead = 4;   // tiles whose Meta is in LDS, and how far before its turn it is brought there
 
 template <int DP>
@@ -53,6 +57,7 @@ struct Chunk {
   // (and what the compiler spills goes to memory: 1584 us in place of 914)
   static constexpr int kQuerySteps = DP == 128 ? 4 : 0;
   static constexpr int kQueryBytes = kQuerySteps * 16 * 2 * kRows;
+  static constexpr int kApartBytes = 2 * 4 * kThreads;       // what a row that has seen a value out of range keeps, by lane
   static constexpr int kHalf = kThreads / 2;
   static constexpr int kKeyUnits = (4 * DP + kHalf - 1) / kHalf;   // 16 codes of a key each, per thread
   static constexpr int kValUnits = (2 * DP + kHalf - 1) / kHalf;   // eight channels of four keys each
@@ -73,19 +78,11 @@ struct Meta {
   float ks[kTile];        // scale of the key; NaN also where the value's is not finite
   uint32_t kz[kTile];     // bits of 1024 + zero, twice
   uint16_t vz[kTile];     // ... of the value, once
-  uint16_t vs[kTile];     // float16 of vs 2^(7 - E)
+  uint16_t vs[kTile];     // float16 of vs 2^(kValueLift - x)
+  float x[kTile];         // 0, or what brings vs into range
   uint64_t seen;          // keys that are there
-  int e;                  // E
+  int odd;                // whether an x is not 0
 };
-
-__device__ __forceinline__ int wave_max_int(int v) {
-  v = max(v, __builtin_amdgcn_update_dpp(v, v, kDppSwapPairs, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(v, v, kDppSwapHalfQuads, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(v, v, kDppHalfMirror, 0xf, 0xf, false));
-  v = max(v, __builtin_amdgcn_update_dpp(v, v, kDppMirror, 0xf, 0xf, false));
-  return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
-             max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
-}
 
 // the keys that some row of a tile of rows sees
 template <int ROWS>
@@ -112,7 +109,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   using C = Chunk<DP>;
   constexpr int kSteps = DP / 16, kOut = DP / 32;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  Meta* metas = reinterpret_cast<Meta*>(smem + C::kBuffers + C::kQueryBytes);
+  Meta* metas = reinterpret_cast<Meta*>(smem + C::kBuffers + C::kQueryBytes + C::kApartBytes);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
   // the workgroup's share: `left` pieces of work from piece `off` of an item on; `at` is the item's place in the order of all
@@ -218,24 +215,24 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     MetaLoad m{page, a.c.scales[at], a.c.scales[plane + at], a.c.zeros[at], a.c.zeros[plane + at]};
     return m;
   };
-  auto there_of = [&](const MetaLoad& m) { return m.page >= 0; };
-  auto good_of = [&](const MetaLoad& m) { return m.page >= 0 && fabsf(m.vs) < INFINITY; };
-  auto exponent_of = [&](const MetaLoad& m) {   // of the tile's largest value scale
-    return wave_max_int(good_of(m) && m.vs != 0.f ? __builtin_amdgcn_frexp_expf(m.vs) : kNoExponent);
-  };
-  auto meta_store = [&](int t, const MetaLoad& m, int e) {
+  auto meta_store = [&](int t, const MetaLoad& m) {
     Meta& o = metas[t & (kMetas - 1)];
-    const bool there = there_of(m), good = good_of(m);
+    // scales of mantissa 2^e, 0.5 <= mantissa < 1, that float16's normal numbers hold, 255 or 15 times as large too
+    constexpr int kLow = -13 - kValueLift, kHigh = (BITS == 8 ? 8 : 12) - kValueLift;
+    const bool there = m.page >= 0, good = there && fabsf(m.vs) < INFINITY;
+    const int e = __builtin_amdgcn_frexp_expf(m.vs), near = min(max(e, kLow), kHigh);
+    const int x = good && m.vs != 0.f ? e - near : 0;
     o.at[lane] = row_of(t, m.page) * a.c.row_bytes;
     o.ks[lane] = good ? m.ks : there ? __uint_as_float(0x7fc00000u) : 0.f;
     const uint32_t z = 0x6400u | m.kz;
     o.kz[lane] = z | (z << 16);
     o.vz[lane] = (uint16_t)(0x6400u | m.vz);
-    o.vs[lane] = __builtin_bit_cast(uint16_t, (_Float16)(good ? ldexpf(m.vs, 7 - e) : 0.f));
-    const uint64_t seen = __ballot(there);
+    o.vs[lane] = __builtin_bit_cast(uint16_t, (_Float16)(good ? ldexpf(m.vs, kValueLift - x) : 0.f));
+    o.x[lane] = (float)x;
+    const uint64_t seen = __ballot(there), odd = __ballot(x != 0);
     if (lane == 0) {
       o.seen = seen;
-      o.e = e;
+      o.odd = odd != 0;
     }
   };
 
@@ -421,13 +418,16 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   for (int n = 0; n < kOut; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
-  float m = kNoScore;   // in units of 1 / factor
-  // the sum of the weights, in every element: one more channel of the values, which are 1 there
+  float M = kNoScore;
+  // of a row that has seen a value out of range: the sum of its weights (before, a negative number) and what that is relative to
+  f32x2* const own = reinterpret_cast<f32x2*>(smem + C::kBuffers + C::kQueryBytes) + threadIdx.x;
+  *own = f32x2{-1.f, kNoScore};
+  bool apart = false;   // whether a row of the wave has
+  // the sum of the weights, in every element (the first one is used): one more channel of the values, which are 1 there
   f32x16v sum;
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
   const f16x8 ones = f16x8_of(0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u);
-  int e = kNoExponent;
 
   const int key_at = r * C::kKeyPitch + ((h ^ key_turn<DP>(r)) * 16), val_at = r * kTile * 2 + ((h ^ val_turn(r)) * 16);
   // What the matrix instructions do in one go: the values of tile t - 1 (with its weights), then the scores of tile t, either may be
@@ -477,18 +477,55 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     });
     __builtin_amdgcn_sched_barrier(0);
   };
-  // the weights of tile t; what has been summed so far is brought to their maximum and to the tile's E
+  // Some value of the tile is out of range, or was of one before.  A row that sees such a value, or has, adds up its weights here, relative to a
+  // maximum of their own, and goes on with log2 of weight times 2^x for a score; any other row keeps its scores.  Returns what they are to be multiplied
+  // by.  (Four at a time: the registers hold no more.)
+  auto out_of_range = [&](const Meta& meta, f32x16v (&s)[2]) {
+    float top = -INFINITY;
+    int sees = 0;
+    auto four = [&](int j) {
+      __builtin_amdgcn_sched_barrier(0);
+      return *reinterpret_cast<const f32x4*>(&meta.x[8 * j + opaque(4 * h)]);
+    };
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const f32x4 x = four(j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float y = s[j >> 2][4 * (j & 3) + i];
+        sees |= (x[i] != 0.f) & (y != -INFINITY);
+        top = fmaxf(top, y);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    sees |= __shfl_xor(sees, 32);
+    top = fmaxf(top, __shfl_xor(top, 32)) * factor;
+    f32x2 kept = *own;
+    if (sees && kept[0] < 0.f) kept = f32x2{sum[0], M};
+    const bool mine = !(kept[0] < 0.f);
+    apart = __any(mine);
+    const float m = top > kept[1] + 8.f ? ceilf(top) : kept[1];
+    float more = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const f32x4 x = four(j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float y = s[j >> 2][4 * (j & 3) + i];
+        more += exp2_fast(fmaf(y, factor, -m));
+        s[j >> 2][4 * (j & 3) + i] = mine ? fmaf(y, factor, x[i]) : y;
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    more += __shfl_xor(more, 32);
+    if (mine) *own = f32x2{kept[0] * exp2_fast(kept[1] - m) + more, m};
+    return mine ? 1.f : factor;
+  };
+  // the weights of tile t; what has been summed so far is brought to their maximum
   auto soften = [&](int t, f32x16v (&s)[2], f16x8 (&weights)[4]) {
     const int key0 = begin + t * kTile;
     const Meta& meta = metas[t & (kMetas - 1)];
     const uint64_t seen = meta.seen;
-    const int now = __builtin_amdgcn_readfirstlane(meta.e);
-    if (now != e) {   // (the first tile among others)
-      const float f = e == kNoExponent ? 1.f : ldexpf(1.f, e - now);
-#pragma unroll
-      for (int n = 0; n < kOut; ++n) acc[n] *= f;
-      e = now;
-    }
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -510,20 +547,22 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
         }
       }
     }
-    float top = kNoScore;
+    float f = factor;
+    if (apart | (__builtin_amdgcn_readfirstlane(meta.odd) != 0)) f = out_of_range(meta, s);
+    float top = -INFINITY;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[k][i]);
-    if (__any((top - m) * factor > 8.f)) {
+    top *= f;
+    if (__any(top > M + 8.f)) {
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = fmaxf(m, top), f = exp2_fast((m - next) * factor);
-      m = next;
-      sum *= f;
+      const float next = top > M + 8.f ? ceilf(top) : M, shrink = exp2_fast(M - next);
+      M = next;
+      sum *= shrink;
 #pragma unroll
-      for (int n = 0; n < kOut; ++n) acc[n] *= f;
+      for (int n = 0; n < kOut; ++n) acc[n] *= shrink;
     }
-    const float M = fmaxf(m * factor, kNoScore);   // (finite where nothing has been seen: -inf - M stays -inf)
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -531,7 +570,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float p0 = exp2_fast(fmaf(s[k][8 * u + 2 * i], factor, -M)), p1 = exp2_fast(fmaf(s[k][8 * u + 2 * i + 1], factor, -M));
+          const float p0 = exp2_fast(fmaf(s[k][8 * u + 2 * i], f, -M)), p1 = exp2_fast(fmaf(s[k][8 * u + 2 * i + 1], f, -M));
           w[i] = __builtin_bit_cast(uint32_t, to_f16(p0, p1));
         }
         weights[2 * k + u] = f16x8_of(w[0], w[1], w[2], w[3]);
@@ -545,24 +584,14 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
 
   if (count > 0) {
     int mine = wave;   // the wave's tile of Meta
-    auto meta_next = [&](int e) {
-      meta_store(mine, ml, e);
+    auto meta_next = [&]() {
+      meta_store(mine, ml);
       mine += C::kWaves;
       ml = meta_load(mine, next_page);
       next_page = page_of(mine + C::kWaves);
     };
-    // the first ones come together and share an E
     static_assert(kMetaAhead <= C::kWaves, "");
-    if (wave < kMetaAhead) {
-      const int e_own = exponent_of(ml);
-      if (lane == 0) metas[kMetas - 1 - wave].e = e_own;
-    }
-    meet();
-    int e_first = kNoExponent;
-#pragma unroll
-    for (int i = 0; i < kMetaAhead; ++i) e_first = max(e_first, metas[kMetas - 1 - i].e);
-    meet();
-    if (wave < kMetaAhead) meta_next(e_first);
+    if (wave < kMetaAhead) meta_next();
     meet();
     // Tile t's codes are asked for two tiles before they are written to LDS, a tile before its turn.  Two tiles to a trip of the loop; those
     // past the last are like any other, with keys that nobody sees.
@@ -572,10 +601,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     c0 = codes_load(2);
     meet();
     auto meta_due = [&](int t) {
-      if (mine == t + kMetaAhead) {
-        const int before = __builtin_amdgcn_readfirstlane(metas[(t + kMetaAhead - 1) & (kMetas - 1)].e);
-        meta_next(max(before, exponent_of(ml)));
-      }
+      if (mine == t + kMetaAhead) meta_next();
     };
     f32x16v s[2];
     f16x8 weights[4];
@@ -632,12 +658,20 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     }
   }
   if (live) {
-    const float l = sum[0], unit = e == kNoExponent ? 0.f : ldexpf(1.f, e - 7);
+    // numerator and sum have powers of two of their own; what they differ by may be more than a float32 holds
+    const f32x2 kept = apart ? *own : f32x2{-1.f, 0.f};
+    const bool mine = !(kept[0] < 0.f);
+    const float l = mine ? kept[0] : sum[0], of = mine ? kept[1] : M;   // the sum, and what it is relative to
+    const int up = (int)fminf(fmaxf(M - of, -600.f), 600.f);
+    const float inv = l == 0.f ? 0.f : ldexpf(1.f / l, up / 2 - kValueLift), rest = ldexpf(1.f, up - up / 2);
+    auto output = [&](int n, int j) {
+      return f32x4{acc[n][4 * j] * inv * rest, acc[n][4 * j + 1] * inv * rest, acc[n][4 * j + 2] * inv * rest, acc[n][4 * j + 3] * inv * rest};
+    };
     if (!alone) {
       // (an item that begins here is the share's last, one that began before is its first)
       const int64_t slot_row = (int64_t)(2 * ((at + off) / each) + (off == 0)) * a.slot_rows + (row - row0);
       if (h == 0) {
-        a.ml[2 * slot_row] = m == kNoScore ? kNoScore : fmaxf(m * factor, kNoScore);
+        a.ml[2 * slot_row] = of;
         a.ml[2 * slot_row + 1] = l;
       }
 #pragma unroll
@@ -645,18 +679,16 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int d = 32 * n + 8 * j + 4 * h;
-          if (d < a.d)
-            *reinterpret_cast<f32x4*>(a.part + slot_row * a.d + d) =
-                f32x4{acc[n][4 * j] * unit, acc[n][4 * j + 1] * unit, acc[n][4 * j + 2] * unit, acc[n][4 * j + 3] * unit};
+          if (d < a.d) *reinterpret_cast<f32x4*>(a.part + slot_row * a.d + d) = output(n, j);
         }
     } else {
-      const float inv = l == 0.f ? 0.f : unit / l;
       uint16_t* O = a.O + token * a.o_token + qhead * a.o_head;
 #pragma unroll
       for (int n = 0; n < kOut; ++n)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float v[4] = {acc[n][4 * j] * inv, acc[n][4 * j + 1] * inv, acc[n][4 * j + 2] * inv, acc[n][4 * j + 3] * inv};
+          const f32x4 o = output(n, j);
+          const float v[4] = {o[0], o[1], o[2], o[3]};
           const int d = 32 * n + 8 * j + 4 * h;
           if (d < a.d) store_run<PTQ_BF16, 4, false>(O, d, a.d, v);
         }
@@ -674,7 +706,8 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   if (threadIdx.x == 0) *begun_at = begun;
 }
 
-// Joins what the shares have of an item that one of them begins: a thread has four channels of a row.
+// Joins what the shares have of an item that one of them begins, means of their keys' values and what those weigh: a thread has four channels
+// of a row.
 template <int DP>
 __global__ __launch_bounds__(256) void join_chunk_kernel(AttendArgs a) {
   using C = Chunk<DP>;
@@ -701,22 +734,24 @@ __global__ __launch_bounds__(256) void join_chunk_kernel(AttendArgs a) {
     }
 #pragma unroll
     for (int j = 0; j < n; ++j) t = fmaxf(t, ml[j][0]);
-    const float f = exp2_fast(top - t);
-    sum *= f;
-    o *= f;
+    const float before = exp2_fast(top - t) * sum;
+    float w[n], all = before;
 #pragma unroll
     for (int j = 0; j < n; ++j) {
-      const float w = p0 + j < parts ? exp2_fast(ml[j][0] - t) : 0.f;
-      sum += w * ml[j][1];
-      o += w * v[j];
+      w[j] = p0 + j < parts ? exp2_fast(ml[j][0] - t) * ml[j][1] : 0.f;
+      all += w[j];
     }
+    const float inv = all == 0.f ? 0.f : 1.f / all;   // a row that has seen nothing: zeros
+    o *= before * inv;
+#pragma unroll
+    for (int j = 0; j < n; ++j) o += (w[j] * inv) * v[j];
     top = t;
+    sum = all;
   };
   int p = 0;
   for (; parts - p > 4; p += 16) some(p, std::integral_constant<int, 16>{});
   if (p < parts) some(p, std::integral_constant<int, 4>{});
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that sees nothing: zeros
-  const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  const float v[4] = {o[0], o[1], o[2], o[3]};
   const int64_t token = q.first + row / a.group, qhead = head * a.group + row % a.group;
   store_run<PTQ_BF16, 4, false>(a.O + token * a.o_token + qhead * a.o_head, c, a.d, v);
 }
@@ -724,7 +759,7 @@ __global__ __launch_bounds__(256) void join_chunk_kernel(AttendArgs a) {
 template <int BITS, int DP>
 bool chunk_launch(const AttendArgs& a, hipStream_t s) {
   using C = Chunk<DP>;
-  constexpr int kBytes = C::kBuffers + C::kQueryBytes + kMetas * (int)sizeof(Meta);
+  constexpr int kBytes = C::kBuffers + C::kQueryBytes + C::kApartBytes + kMetas * (int)sizeof(Meta);
   if (!lds_opt_in<attend_chunk_kernel<BITS, DP>>(kBytes)) return false;
   const int tiles = (int)ceil_div((int64_t)a.max_q * a.group, C::kRows);
   const int64_t blocks = a.splits > 1 ? kShares : ceil_div((int64_t)a.b * a.c.heads, 8) * 8 * tiles;
