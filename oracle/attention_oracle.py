@@ -29,8 +29,9 @@ def rmsnorm_quantize(X, dtype="f32", residual=None, gamma=None, eps=1e-5, normal
             scales[i] = np.nan
             continue
         A = np.max(np.abs(u))
-        if A > 0:
-            codes[i] = np.rint(127.0 * u / A)
+        if A == 0:   # codes 0 and scale 0, whatever eps is
+            continue
+        codes[i] = np.rint(127.0 * u / A)
         scales[i] = A / 127.0
         if normalize:
             scales[i] /= np.sqrt(np.sum(y[i] ** 2) / n + eps)

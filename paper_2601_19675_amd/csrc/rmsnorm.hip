@@ -132,7 +132,7 @@ __global__ __launch_bounds__(ROW < 256 ? 256 : ROW) void rmsnorm_quantize_kernel
   }
   if (at == 0) {
     double s = (double)A / 127.0;
-    if (a.normalize) s /= sqrt(squares / (double)a.n + a.eps);
+    if (a.normalize && top != 0) s /= sqrt(squares / (double)a.n + a.eps);   // (a row of zeros has scale 0, also without an eps)
     a.S[row] = finite ? (float)s : __uint_as_float(0x7fc00000u);
   }
 }
