@@ -292,11 +292,12 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
     float top = kNoScore;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
-    // the maximum moves only when a score is 2^8 above it: until then weights stay small enough
+    // the maximum moves only when one of the row's own scores is 2^8 above it: until then weights stay small enough, and what other rows see does
+    // not change a bit of this one
     if (__any(top > m + 8.f)) {
       top = fmaxf(top, __shfl_xor(top, 16));
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = fmaxf(m, top), f = exp2_fast(m - next);
+      const float next = top > m + 8.f ? top : m, f = exp2_fast(m - next);
       m = next;
       l *= f;
 #pragma unroll
