@@ -30,8 +30,8 @@ struct AttendArgs {
   int least_share;                       // rows form: blocks of 128 keys that a workgroup takes at least
   int slot_rows;                         // chunk form: rows of a part
   // rows form: [part][token][head][...]; chunk form: [share][item it ends, item it begins][row][...]
-  float* part;                           // [...][d]: sums of weight times value
-  float* ml;                             // [...][2]: the maximum they are relative to, the sum of the weights
+  float* part;                           // [...][d]: the mean of the part's values
+  float* ml;                             // [...][2]: a maximum, the sum of the weights relative to it
   int* parts;                            // rows form: [token], how many there are; chunk form: [share][4], see there
 };
 

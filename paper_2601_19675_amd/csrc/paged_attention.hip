@@ -24,7 +24,8 @@
 //
 // The value's scale goes into the weight: with vs = mant 2^e, e enters the exponent that the running maximum is taken of, so
 // that the weights that are rounded to float16 are at most 2^8 whatever the scales are (rounding: 2^-11 of a weight, the
-// precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.
+// precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.  A row that sees a value's
+// scale beyond 2^-40 or 2^40, where that would leave float32's range, adds up its weights relative to a maximum of their own instead.
 #include <algorithm>
 
 #include "paged_attention.h"
@@ -35,12 +36,19 @@ namespace ptq {
 namespace {
 
 constexpr int kRows = 16, kBlock = 32, kWaves = 4, kShareBlock = kWaves * kBlock;
+constexpr int kFarExponent = 40;   // of a value's scale that the sum of the weights does not go through
 
 // blocks that a sequence counts for in the shares: one at least, if it has queries (somebody has to write their zeros)
 __device__ __forceinline__ int share_blocks(const AttendArgs& a, const Sequence& q) {
   return q.queries == 0 ? 0 : max(1, (q.end - q.begin + kShareBlock - 1) / kShareBlock);
 }
 struct __attribute__((packed, aligned(4))) Four { float e[4]; };
+// 2^-e, by its bits: those of 1, and -2^23 times e (which the compiler makes two instructions)
+__device__ __forceinline__ float power_below(int e) {
+  float f;
+  asm("v_mad_i32_i24 %0, %1, %2, 1.0" : "=v"(f) : "v"(e), "s"(-(1 << 23)));
+  return f;
+}
 
 template <int BITS, int DP>
 struct Shape {
@@ -70,7 +78,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
   constexpr int kCodeExp = BITS == 8 ? 24 : 20;   // a key's code c goes in as c 2^-kCodeExp
   extern __shared__ __attribute__((aligned(16))) float smem[];
   float (*lds_o)[kRows][DP + 4] = reinterpret_cast<float (*)[kRows][DP + 4]>(smem);
-  float (*lds_ml)[kRows][2] = reinterpret_cast<float (*)[kRows][2]>(smem + kWaves * kRows * (DP + 4));
+  f32x4 (*lds_ml)[kRows] = reinterpret_cast<f32x4 (*)[kRows]>(smem + kWaves * kRows * (DP + 4));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int head = blockIdx.y;
   // the workgroup's share: blocks [off, off + left) of sequence seq and on, `before` blocks before that sequence
@@ -259,10 +267,10 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
 #pragma unroll
   for (int i = 0; i < kOut; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = kNoScore, l = 0.f;
+  float furthest = 0.f;   // of the exponents of the value's scales that have been seen
 
-  auto compute = [&](int key0, const Pages& p, const Block& b) {
-    float x[8], mant[8];
-    int e[8];
+  // log2 of the weights, with the exponents of their value's scales in them, and the latter's mantissas and exponents
+  auto score = [&](int key0, const Pages& p, const Block& b, float (&x)[8], float (&mant)[8], int (&e)[8]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -287,11 +295,20 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
         const bool seen = (key >= lo) & (key < min(hi, to)) & ((HALVES ? p.key[i >> 2] : p.own[HALVES ? 0 : i]) >= 0);
         mant[i] = seen ? mant[i] : 0.f;
         x[i] = seen ? x[i] : -INFINITY;
+        e[i] = seen ? e[i] : 0;
       }
     }
+  };
+  auto compute = [&](int key0, const Pages& p, const Block& b) {
+    float x[8], mant[8];
+    int e[8];
+    score(key0, p, b, x, mant, e);
     float top = kNoScore;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i]);
+    for (int i = 0; i < 8; ++i) {
+      top = fmaxf(top, x[i]);
+      furthest = fmaxf(furthest, fabsf((float)e[i]));
+    }
     // the maximum moves only when one of the row's own scores is 2^8 above it: until then weights stay small enough, and what other rows see does
     // not change a bit of this one
     if (__any(top > m + 8.f)) {
@@ -309,7 +326,8 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       const float p0 = exp2_fast(x[i] - m), p1 = exp2_fast(x[i + 1] - m);
-      l += ldexpf(p0, -e[i]) + ldexpf(p1, -e[i + 1]);
+      l = fmaf(p0, power_below(e[i]), l);
+      l = fmaf(p1, power_below(e[i + 1]), l);
       w[i >> 1] = __builtin_bit_cast(uint32_t, to_f16(p0 * mant[i], p1 * mant[i + 1]));
     }
     const f16x8 weights = f16x8_of(w[0], w[1], w[2], w[3]);
@@ -375,6 +393,34 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
       });
     }
   }
+  float of = m;   // what the sum of the weights is relative to
+  if (__builtin_expect(__any(furthest > kFarExponent), 0)) {   // rows that see a scale out of range: the sum once more, relative to a maximum of its own
+    furthest = fmaxf(furthest, __shfl_xor(furthest, 16));
+    furthest = fmaxf(furthest, __shfl_xor(furthest, 32));
+    float sum = 0.f, top = kNoScore;
+    for (key0 = from + wave * kBlock; key0 < to; key0 += kWaves * kBlock) {
+      Block b;
+      const Pages p = pages_of(key0);
+      fetch(key0, p, b);
+      float x[8], mant[8], most = kNoScore;
+      int e[8];
+      score(key0, p, b, x, mant, e);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] -= (float)e[i];
+        most = fmaxf(most, x[i]);
+      }
+      most = fmaxf(most, __shfl_xor(most, 16));
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float next = fmaxf(top, most);
+      sum *= exp2_fast(top - next);
+      top = next;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += exp2_fast(x[i] - top);
+    }
+    l = furthest > kFarExponent ? sum : l;
+    of = furthest > kFarExponent ? top : m;
+  }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
 
@@ -390,23 +436,42 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
       else c = 8 * (s >> 1) + 2 * n + (s & 1);
       lds_o[wave][r][c] = BITS == 4 && (n & 1) ? (acc[n][i] - acc_z[BITS == 8 ? 0 : 1][i]) * 0x1p20f : (acc[n][i] - acc_z[0][i]) * 0x1p24f;
     }
-  if (g == 0) {
-    lds_ml[wave][r][0] = m;
-    lds_ml[wave][r][1] = l;
-  }
+  if (g == 0) lds_ml[wave][r] = f32x4{m, l, of, 0.f};
   __syncthreads();
   for (int i = threadIdx.x; i < rows * (DP / 4); i += kWaves * 64) {
     const int row = i / (DP / 4), c = i % (DP / 4) * 4;
     if (c >= a.d) continue;
     float top = kNoScore, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_ml[w][row][0]);
+    f32x4 ml[kWaves];
+    bool same = true;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = exp2_fast(lds_ml[w][row][0] - top);
-      sum += f * lds_ml[w][row][1];
+      ml[w] = lds_ml[w][row];
+      top = fmaxf(top, ml[w][0]);
+      same &= ml[w][2] == ml[w][0];
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = exp2_fast(ml[w][0] - top);
+      sum += f * ml[w][1];
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += f * lds_o[w][row][c + j];
+    }
+    if (!same) {   // numerator and sum have powers of two of their own; what they differ by may be more than a float32 holds
+      float top_l = kNoScore;
+      sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) top_l = fmaxf(top_l, ml[w][2]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) sum += exp2_fast(ml[w][2] - top_l) * ml[w][1];
+      const float half = exp2_fast(0.5f * (top - top_l)), inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * inv * half * half;
+      top = top_l;
+    } else {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that sees nothing: zeros
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] *= inv;
     }
     const int tok = q.first + row / a.group, h = head * a.group + row % a.group;
     if (!alone) {
@@ -417,9 +482,6 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
         a.ml[2 * at + 1] = sum;
       }
     } else {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that sees nothing: zeros
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] *= inv;
       store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, o);
     }
   }
@@ -436,7 +498,8 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
   }
 }
 
-// Adds the splits' parts of a (token, head): a lane looks at one part's maximum and sum, and has four channels of all parts.
+// Joins the splits' parts of a (token, head), means of their keys' values and what those weigh: a lane looks at one part's maximum and sum, and has
+// four channels of all parts.
 __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
   const int tok = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, c = lane * 4;
   int seq = 0;   // the sequence that the token belongs to
@@ -458,8 +521,15 @@ __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
   const float* part = a.part + first * a.d + (c < a.d ? c : 0);
   for (int s0 = 0; s0 < parts; s0 += 64) {
     const int s = min(s0 + lane, parts - 1);
-    const float f = s0 + lane < parts ? exp2_fast(a.ml[2 * (first + s * step)] - top) : 0.f;
-    sum += f * a.ml[2 * (first + s * step) + 1];
+    float f = s0 + lane < parts ? exp2_fast(a.ml[2 * (first + s * step)] - top) * a.ml[2 * (first + s * step) + 1] : 0.f;
+    float all = f;
+#pragma unroll
+    for (int n = 1; n < kWave; n <<= 1) all += __shfl_xor(all, n);
+    all += sum;
+    const float inv = all == 0.f ? 0.f : 1.f / all;   // a row that sees nothing: zeros
+    o *= sum * inv;
+    f *= inv;
+    sum = all;
     const int here = min(64, parts - s0);
     for (int i = 0; i < here; i += 8) {   // (f is 0 past the last part)
       f32x4 v[8];
@@ -469,11 +539,8 @@ __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
       for (int j = 0; j < 8; ++j) o += __shfl(f, i + j) * v[j];
     }
   }
-#pragma unroll
-  for (int n = 1; n < kWave; n <<= 1) sum += __shfl_xor(sum, n);
   if (c >= a.d) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  const float v[4] = {o[0], o[1], o[2], o[3]};
   store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, v);
 }
 
@@ -489,7 +556,7 @@ int64_t shares(int64_t hkv) { return std::max<int64_t>(1, kShares / hkv); }
 
 template <int BITS, int DP, bool HALVES, bool WHOLE>
 bool rows_form_launch(const AttendArgs& a, hipStream_t s) {
-  constexpr int kBytes = kWaves * kRows * (DP + 4 + 2) * (int)sizeof(float);
+  constexpr int kBytes = kWaves * kRows * (DP + 4 + 4) * (int)sizeof(float);
   if (!lds_opt_in<attend_rows_kernel<BITS, DP, HALVES, WHOLE>>(kBytes)) return false;
   const dim3 grid = a.splits > 1 ? dim3((unsigned)shares(a.c.heads), (unsigned)a.c.heads, 1) : dim3(1, (unsigned)a.c.heads, (unsigned)a.b);
   attend_rows_kernel<BITS, DP, HALVES, WHOLE><<<grid, kWaves * 64, kBytes, s>>>(a);
