@@ -37,7 +37,8 @@ struct AttendArgs {
 
 // a sequence's queries and keys
 struct Sequence {
-  int first, queries, length;            // first token, new tokens, keys
+  int first, queries, length;            // first token, new tokens, keys that the table and max_kv reach
+  int place;                             // of the first query, among all keys that the sequence is said to have
   int begin, end;                        // keys that some query sees lie in [begin, end), begin a multiple of 64
 };
 __device__ __forceinline__ Sequence sequence_of(const AttendArgs& a, int s) {
@@ -46,16 +47,18 @@ __device__ __forceinline__ Sequence sequence_of(const AttendArgs& a, int s) {
   q.first = (int)from;
   q.queries = from >= 0 && to <= a.t && to > from ? (int)(to - from) : 0;
   const int64_t most = min((int64_t)a.max_kv, a.ldt << a.c.page_shift);
-  q.length = max(0, (int)min((int64_t)a.kv_lens[s], most));
+  const int keys = max(0, a.kv_lens[s]);
+  q.place = keys - q.queries;
+  q.length = (int)min((int64_t)keys, most);
   q.end = q.length;
   q.begin = 0;
-  if (a.window > 0) q.begin = max(0, q.length - q.queries - a.window + 1) & ~63;
+  if (a.window > 0) q.begin = max(0, q.place - a.window + 1) & ~63;
   q.begin = min(q.begin, q.end);
   return q;
 }
 // keys [lo, hi) that query i of a sequence sees
 __device__ __forceinline__ void visible(const AttendArgs& a, const Sequence& q, int i, int& lo, int& hi) {
-  const int place = q.length - q.queries + i;
+  const int place = q.place + i;
   hi = a.causal ? max(0, min(q.length, place + 1)) : q.length;
   lo = a.window > 0 ? max(0, place - a.window + 1) : 0;
 }
