@@ -390,6 +390,7 @@ ptq_status ptq_paged_attention(const void* Q, ptq_dtype qdt, int64_t q_token, in
   if (t < 0 || t > (1 << 24) || hq <= 0 || hq > 65535 || hq % hkv != 0 || b < 0 || b > 65535 || max_q < 0 || max_q > t || ldt < 0 ||
       max_kv < 0 || max_kv > INT32_MAX / 4 || q_token < 0 || q_head < 0 || o_token < 0 || o_head < 0)
     return PTQ_ERR_SHAPE;
+  if (max_q * (hq / hkv) > (1 << 27)) return PTQ_ERR_SHAPE;   // a key head's rows, counted in 32 bits and by the workgroup of a launch
   if (t == 0 || b == 0 || max_q == 0) return PTQ_OK;
   if (pages == 0) return PTQ_ERR_SHAPE;
   if (!Q || !O || Q == O || !cu_q || !codes || !scales || !zeros || !table || !kv_lens || misaligned(codes, 16)) return PTQ_ERR_ARG;
