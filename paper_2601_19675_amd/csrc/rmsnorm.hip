@@ -11,6 +11,8 @@
 //
 // 16384 rows of 4096 bfloat16 with the residual's way in and out (470 MB): 80.7 us, 5.8 TB/s; 4096 rows of 11008 float32 (225 MB) 42 us,
 // 5.4 TB/s; four rows of 4096 3.6 us, of which the launch is the most.
+#include <algorithm>
+
 #include "stored_rows.h"
 
 namespace ptq {
@@ -160,10 +162,17 @@ int64_t rmsnorm_max_columns() { return 8 * 4 * 1024; }
 ptq_status rmsnorm_quantize_launch(const void* X, ptq_dtype dt, int64_t ldx, int64_t t, int64_t n, const void* residual,
                                    int64_t ldr, void* residual_out, int64_t ldo, const void* gamma, double eps, int normalize,
                                    int8_t* codes, int64_t ldc, float* scales, hipStream_t s) {
-  const NormArgs a{X, residual, residual_out, gamma, codes, scales, ldx, ldr, ldo, ldc, (int)t, (int)n, eps, normalize};
-  if (dt == PTQ_BF16) n % 8 ? launch<PTQ_BF16, true>(a, s) : launch<PTQ_BF16, false>(a, s);
-  else n % 8 ? launch<PTQ_F32, true>(a, s) : launch<PTQ_F32, false>(a, s);
-  PTQ_HIP_CHECK_LAUNCH();
+  // a launch has fewer than 2^32 threads, and a row up to 1024 of them
+  constexpr int64_t kRows = 1 << 21;
+  const int64_t size = dt == PTQ_BF16 ? 2 : 4;
+  for (int64_t first = 0; first < t; first += kRows) {
+    auto from = [&](const void* p, int64_t ld) { return p ? static_cast<const char*>(p) + first * ld * size : nullptr; };
+    const NormArgs a{from(X, ldx), from(residual, ldr), const_cast<char*>(from(residual_out, ldo)), gamma, codes + first * ldc, scales + first,
+                     ldx, ldr, ldo, ldc, (int)std::min(kRows, t - first), (int)n, eps, normalize};
+    if (dt == PTQ_BF16) n % 8 ? launch<PTQ_BF16, true>(a, s) : launch<PTQ_BF16, false>(a, s);
+    else n % 8 ? launch<PTQ_F32, true>(a, s) : launch<PTQ_F32, false>(a, s);
+    PTQ_HIP_CHECK_LAUNCH();
+  }
   return PTQ_OK;
 }
 

@@ -20,3 +20,24 @@ def test_query_rows_of_a_key_head():
              attention(2 ** 24, 8, 1, 2 ** 24), attention(2 ** 24, 128, 1, 2 ** 20)]
     got = [rc for rc, _ in record([("ptq_paged_attention", a) for a in calls])]
     assert got == [SHAPE, SHAPE, SHAPE, WORKSPACE, WORKSPACE]
+
+
+def one(name, args, read):
+    (rc, launches), = record([(name, args)], read=read)
+    assert rc == OK and launches
+    return launches
+
+
+@pytest.mark.parametrize("t,n,dt,threads", [(2 ** 25 + 5, 4096, 1, 256), (2 ** 27 + 1, 64, 0, 256), (2 ** 22 + 3, 32768, 1, 1024), (1000, 4096, 1, 256)])
+def test_norm_of_many_rows(t, n, dt, threads):
+    size = 2 if dt == 1 else 4
+    args = [PTR, dt, n, t, n, 2 * PTR, n + 8, 3 * PTR, n + 16, PTR, 1e-5, 1, 4 * PTR, n + 32, 5 * PTR, 0]
+    fields = dict(X=(0, "q", 0), R=(0, "q", 8), Y=(0, "q", 16), C=(0, "q", 32), S=(0, "q", 40), t=(0, "i", 80))
+    done = 0
+    for k in one("ptq_rmsnorm_quantize", args, {"rmsnorm_quantize_kernel": fields}):
+        assert 0 < k["grid"][0] * threads < THREADS and k["grid"][1:] == [1, 1]
+        assert k["grid"][0] >= (k["t"] if n > 2048 else -(-k["t"] // 4))
+        assert (k["X"], k["R"], k["Y"]) == (PTR + done * n * size, 2 * PTR + done * (n + 8) * size, 3 * PTR + done * (n + 16) * size)
+        assert (k["C"], k["S"]) == (4 * PTR + done * (n + 32), 5 * PTR + 4 * done)
+        done += k["t"]
+    assert done == t
