@@ -9,6 +9,8 @@
 //
 // Four prompts of up to 8192 tokens, 32 heads of 128 channels, bfloat16 into 4 bits: 893 MB both ways in 217 us (write 124, read 96), 4.1
 // TB/s; a large copy has 4.7.
+#include <algorithm>
+
 #include "kv_cache.h"
 #include "static_for.h"
 #include "stored_rows.h"
@@ -159,7 +161,7 @@ struct ReadArgs {
   int64_t ldt;
   const int32_t* cu;
   int64_t rows, max_kv;
-  int d;
+  int d, first_tile;               // of places, in this launch
   KvCache c;
 };
 
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(ReadArgs a) {
   constexpr int kGroups = 256 / LANES;
   using ST = typename StoredType<DT>::type;
   const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, seq = blockIdx.z, which = blockIdx.y;
-  const int tile = blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads, c = lane * 8;
+  const int tile = a.first_tile + blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads, c = lane * 8;
   const int64_t begin = a.cu[seq], end = a.cu[seq + 1];
   if (begin < 0 || end > a.rows) return;
   const int64_t length = min(end - begin, a.max_kv);
@@ -217,21 +219,37 @@ KvCache cache_of(uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, i
   return KvCache{codes, scales, zeros, pages, hkv, __builtin_ctz((unsigned)page), d * bits / 8};
 }
 
+// tokens or places of a workgroup, and such tiles in a launch, which has fewer than 2^32 threads
+int tile_rows(int d) { return kRowsPerLane * (256 / (d <= 64 ? 8 : d <= 128 ? 16 : 32)); }
+int64_t launch_tiles(int heads) { return (1 << 23) / heads; }
+
 template <int DT, int BITS>
-void write_lanes(const WriteArgs& a, hipStream_t s) {
-  auto grid = [&](int lanes) { return dim3((unsigned)(ceil_div(a.t, kRowsPerLane * (256 / lanes)) * a.c.heads), 2); };
-  if (a.d <= 64) kv_write_kernel<DT, BITS, 8><<<grid(8), 256, 0, s>>>(a);
-  else if (a.d <= 128) kv_write_kernel<DT, BITS, 16><<<grid(16), 256, 0, s>>>(a);
-  else kv_write_kernel<DT, BITS, 32><<<grid(32), 256, 0, s>>>(a);
+void write_lanes(const WriteArgs& all, hipStream_t s) {
+  const int rows = tile_rows(all.d);
+  const int64_t step = launch_tiles(all.c.heads) * rows;
+  for (int64_t first = 0; first < all.t; first += step) {
+    WriteArgs a = all;
+    for (int i = 0; i < 2; ++i) a.X[i] = static_cast<const typename StoredType<DT>::type*>(all.X[i]) + first * all.token[i];
+    a.slots += first;
+    a.t = (int)std::min(step, all.t - first);
+    const dim3 grid((unsigned)(ceil_div(a.t, rows) * a.c.heads), 2);
+    if (a.d <= 64) kv_write_kernel<DT, BITS, 8><<<grid, 256, 0, s>>>(a);
+    else if (a.d <= 128) kv_write_kernel<DT, BITS, 16><<<grid, 256, 0, s>>>(a);
+    else kv_write_kernel<DT, BITS, 32><<<grid, 256, 0, s>>>(a);
+  }
 }
 template <int DT, int BITS>
-void read_lanes(const ReadArgs& a, int b, hipStream_t s) {
-  auto grid = [&](int lanes) {
-    return dim3((unsigned)(ceil_div(a.max_kv, kRowsPerLane * (256 / lanes)) * a.c.heads), 2, (unsigned)b);
-  };
-  if (a.d <= 64) kv_read_kernel<DT, BITS, 8><<<grid(8), 256, 0, s>>>(a);
-  else if (a.d <= 128) kv_read_kernel<DT, BITS, 16><<<grid(16), 256, 0, s>>>(a);
-  else kv_read_kernel<DT, BITS, 32><<<grid(32), 256, 0, s>>>(a);
+void read_lanes(const ReadArgs& all, int b, hipStream_t s) {
+  // no sequence has more places than there are rows, whatever max_kv allows
+  const int64_t tiles = ceil_div(std::min(all.max_kv, all.rows), tile_rows(all.d)), step = launch_tiles(all.c.heads);
+  for (int64_t first = 0; first < tiles; first += step) {
+    ReadArgs a = all;
+    a.first_tile = (int)first;
+    const dim3 grid((unsigned)(std::min(step, tiles - first) * a.c.heads), 2, (unsigned)b);
+    if (a.d <= 64) kv_read_kernel<DT, BITS, 8><<<grid, 256, 0, s>>>(a);
+    else if (a.d <= 128) kv_read_kernel<DT, BITS, 16><<<grid, 256, 0, s>>>(a);
+    else kv_read_kernel<DT, BITS, 32><<<grid, 256, 0, s>>>(a);
+  }
 }
 
 }  // namespace
@@ -251,7 +269,7 @@ ptq_status kv_cache_read_launch(const uint8_t* codes, const float* scales, const
                                 int hkv, int d, int bits, const int32_t* table, int64_t ldt, int64_t b, const int32_t* cu_kv,
                                 int64_t rows, int64_t max_kv, void* K, int64_t k_token, int64_t k_head, void* V,
                                 int64_t v_token, int64_t v_head, ptq_dtype dt, hipStream_t s) {
-  const ReadArgs a{{K, V}, {k_token, v_token}, {k_head, v_head}, table, ldt, cu_kv, rows, max_kv, d,
+  const ReadArgs a{{K, V}, {k_token, v_token}, {k_head, v_head}, table, ldt, cu_kv, rows, max_kv, d, 0,
                    cache_of(const_cast<uint8_t*>(codes), const_cast<float*>(scales), const_cast<uint8_t*>(zeros), pages, page, hkv, d, bits)};
   if (dt == PTQ_BF16) bits == 8 ? read_lanes<PTQ_BF16, 8>(a, (int)b, s) : read_lanes<PTQ_BF16, 4>(a, (int)b, s);
   else bits == 8 ? read_lanes<PTQ_F32, 8>(a, (int)b, s) : read_lanes<PTQ_F32, 4>(a, (int)b, s);

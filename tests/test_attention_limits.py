@@ -41,3 +41,29 @@ def test_norm_of_many_rows(t, n, dt, threads):
         assert (k["C"], k["S"]) == (4 * PTR + done * (n + 32), 5 * PTR + 4 * done)
         done += k["t"]
     assert done == t
+
+
+@pytest.mark.parametrize("t,hkv,d", [(2 ** 26 + 9, 32, 128), (2 ** 25, 32767, 16), (1000, 8, 128), (2 ** 30 - 1, 64, 256)])
+def test_cache_write_of_many_tokens(t, hkv, d):
+    args = [PTR, hkv * d, d, 2 * PTR, hkv * d + 16, d, 1, t, hkv, d, 3 * PTR, 8, PTR, PTR, PTR, 8, 16, 0]
+    fields = dict(K=(0, "q", 0), V=(0, "q", 8), slots=(0, "q", 48), t=(0, "i", 56))
+    per = 4 * 256 // (8 if d <= 64 else 16 if d <= 128 else 32)
+    done = 0
+    for k in one("ptq_kv_cache_write", args, {"kv_write_kernel": fields}):
+        assert 0 < k["grid"][0] * 256 < THREADS and k["grid"][1:] == [2, 1] and k["grid"][0] == -(-k["t"] // per) * hkv
+        assert (k["K"], k["V"], k["slots"]) == (PTR + 2 * done * hkv * d, 2 * PTR + 2 * done * (hkv * d + 16), 3 * PTR + 4 * done)
+        done += k["t"]
+    assert done == t
+
+
+@pytest.mark.parametrize("max_kv,rows,hkv,d", [(2 ** 30 - 1, 2 ** 29, 32, 64), (2 ** 30 - 1, 2 ** 30, 32767, 16), (2 ** 30 - 1, 1000, 8, 128), (700, 5000, 8, 128),
+                                               (2 ** 30 - 1, 1, 32767, 256)])
+def test_cache_read_of_long_sequences(max_kv, rows, hkv, d):
+    args = [PTR, PTR, PTR, 8, 16, hkv, d, 8, PTR, 4, 3, PTR, rows, max_kv, PTR, hkv * d, d, PTR, hkv * d, d, 1, 0]
+    per = 4 * 256 // (8 if d <= 64 else 16 if d <= 128 else 32)
+    done = 0   # tiles of places of a sequence
+    for k in one("ptq_kv_cache_read", args, {"kv_read_kernel": dict(first=(0, "i", 92))}):
+        assert 0 < k["grid"][0] * 256 < THREADS and k["grid"][1:] == [2, 3] and k["grid"][0] % hkv == 0 and k["first"] == done
+        done += k["grid"][0] // hkv
+    # max_kv is a bound: no sequence has more places than there are rows
+    assert done == -(-min(max_kv, rows) // per)
