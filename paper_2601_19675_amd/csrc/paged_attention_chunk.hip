@@ -105,7 +105,7 @@ __device__ __forceinline__ int item_work(const AttendArgs& a, int seq, int tile)
 }
 
 template <int BITS, int DP>
-__global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(AttendArgs a, int tiles) {
+__global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(AttendArgs a, int tiles, int first_group) {
   using C = Chunk<DP>;
   constexpr int kSteps = DP / 16, kOut = DP / 32;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   } else {
     // groups (sequence, key head) go round the dies, so that a group's row tiles share its codes in one L2; the last rows, which
     // see most, first
-    const int die = blockIdx.x & 7, idx = blockIdx.x >> 3, group = idx / tiles * 8 + die;
+    const int die = blockIdx.x & 7, idx = blockIdx.x >> 3, group = first_group + idx / tiles * 8 + die;
     if (group >= a.b * a.c.heads) return;
     seq = group / a.c.heads, head = group % a.c.heads, tile = tiles - 1 - idx % tiles;
   }
@@ -762,10 +762,15 @@ bool chunk_launch(const AttendArgs& a, hipStream_t s) {
   constexpr int kBytes = C::kBuffers + C::kQueryBytes + C::kApartBytes + kMetas * (int)sizeof(Meta);
   if (!lds_opt_in<attend_chunk_kernel<BITS, DP>>(kBytes)) return false;
   const int tiles = (int)ceil_div((int64_t)a.max_q * a.group, C::kRows);
-  const int64_t blocks = a.splits > 1 ? kShares : ceil_div((int64_t)a.b * a.c.heads, 8) * 8 * tiles;
-  if (blocks > INT32_MAX) return false;
-  attend_chunk_kernel<BITS, DP><<<(unsigned)blocks, C::kThreads, kBytes, s>>>(a, tiles);
-  if (a.splits > 1) join_chunk_kernel<DP><<<dim3(kShares, C::kRows * (DP / 4) / 256), 256, 0, s>>>(a);
+  if (a.splits > 1) {
+    attend_chunk_kernel<BITS, DP><<<kShares, C::kThreads, kBytes, s>>>(a, tiles, 0);
+    join_chunk_kernel<DP><<<dim3(kShares, C::kRows * (DP / 4) / 256), 256, 0, s>>>(a);
+    return true;
+  }
+  // A launch has fewer than 2^32 threads; eight groups of up to 2^27 rows, two threads to a row, fit one.
+  const int64_t eights = ceil_div((int64_t)a.b * a.c.heads, 8), step = std::max<int64_t>(1, (1 << 19) / tiles);
+  for (int64_t first = 0; first < eights; first += step)
+    attend_chunk_kernel<BITS, DP><<<(unsigned)(std::min(step, eights - first) * 8 * tiles), C::kThreads, kBytes, s>>>(a, tiles, (int)(8 * first));
   return true;
 }
 

@@ -67,3 +67,18 @@ def test_cache_read_of_long_sequences(max_kv, rows, hkv, d):
         done += k["grid"][0] // hkv
     # max_kv is a bound: no sequence has more places than there are rows
     assert done == -(-min(max_kv, rows) // per)
+
+
+@pytest.mark.parametrize("b,hq,hkv,max_q,d", [(4096, 32, 32, 2 ** 17, 64), (65535, 8, 8, 300, 64), (3, 8, 1, 2 ** 24, 64), (9, 8, 2, 300, 256), (65535, 32767, 32767, 17, 16)])
+def test_chunks_of_many_sequences(b, hq, hkv, max_q, d):
+    t = 2 ** 24
+    args = attention(t, hq, hkv, max_q, b=b, max_kv=1000, ws=PTR)
+    args[6] = d
+    threads, rows = (256, 128) if d > 128 else (512, 256)
+    tiles = -(-max_q * (hq // hkv) // rows)
+    done = 0   # groups: a sequence and a key head each, eight side by side
+    for k in one("ptq_paged_attention", args, {"attend_chunk_kernel": dict(tiles=(1, "i"), first=(2, "i"))}):
+        assert 0 < k["grid"][0] * threads < THREADS and k["grid"][1:] == [1, 1]
+        assert k["tiles"] == tiles and k["first"] == done and k["grid"][0] % (8 * tiles) == 0
+        done += k["grid"][0] // tiles
+    assert b * hkv <= done < b * hkv + 8
