@@ -530,7 +530,8 @@ ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const ui
  *           max_kv or the table's ldt pages are not there.
  * max_q, max_kv   no sequence has more queries or keys (rows of queries from max_q on are left out).     b <= 65535.
  * table     b x ldt int32; a number outside [0, pages) is a page that is not there.
- * hq        a multiple of hkv, at most 65535; t <= 2^24, max_q hq / hkv <= 2^27.     softmax_scale  finite.     window  >= 0.     The rest as above.
+ * hq        a multiple of hkv, at most 65535; t <= 2^24, max_q hq / hkv <= 2^27.
+ * softmax_scale  up to 2e38 either way.     window  >= 0.     The rest as above.
  * Workspace: PTQ_OP_PAGED_ATTENTION with m = hq, n = d, t and block = max_kv.  Results do not depend on what it holds.
  * Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE, PTQ_ERR_WORKSPACE.
  */

@@ -386,7 +386,7 @@ ptq_status ptq_paged_attention(const void* Q, ptq_dtype qdt, int64_t q_token, in
   if (qdt != PTQ_BF16) return PTQ_ERR_DTYPE;
   const ptq_status bad = kv_cache_bad(hkv, d, bits, pages, page);
   if (bad != PTQ_OK) return bad;
-  if (!std::isfinite(softmax_scale) || window < 0) return PTQ_ERR_ARG;
+  if (!(std::fabs(softmax_scale) <= 2e38) || window < 0) return PTQ_ERR_ARG;   // (times log2(e) it is a float32)
   if (t < 0 || t > (1 << 24) || hq <= 0 || hq > 65535 || hq % hkv != 0 || b < 0 || b > 65535 || max_q < 0 || max_q > t || ldt < 0 ||
       max_kv < 0 || max_kv > INT32_MAX / 4 || q_token < 0 || q_head < 0 || o_token < 0 || o_head < 0)
     return PTQ_ERR_SHAPE;

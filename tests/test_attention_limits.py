@@ -82,3 +82,11 @@ def test_chunks_of_many_sequences(b, hq, hkv, max_q, d):
         assert k["tiles"] == tiles and k["first"] == done and k["grid"][0] % (8 * tiles) == 0
         done += k["grid"][0] // tiles
     assert b * hkv <= done < b * hkv + 8
+
+
+@pytest.mark.parametrize("scale,status", [(1e39, 1), (-1e300, 1), (2.4e38, 1), (3e37, WORKSPACE), (0.0, WORKSPACE)])
+def test_softmax_scales_that_float32_does_not_hold(scale, status):
+    args = attention(4, 8, 2, 3)
+    args[21] = scale
+    (rc, launches), = record([("ptq_paged_attention", args)])
+    assert rc == status and not launches
