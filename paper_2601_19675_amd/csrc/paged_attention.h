@@ -118,7 +118,9 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 constexpr int kChunkShares = 256, kChunkRows = 256;   // workgroups that have shares; query rows of a workgroup at most
 constexpr int kSharedChunkKeys = 2048;                 // shorter contexts are not shared out
-int64_t paged_attention_chunk_items(const AttendArgs& a);   // tiles of rows, at most
+// tiles of rows of all sequences and key heads: by max_q, and those of them that can hold a row of the tokens there are
+struct ChunkItems { int64_t tiles, busy; };
+ChunkItems paged_attention_chunk_items(const AttendArgs& a);
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s);
 
 }  // namespace ptq

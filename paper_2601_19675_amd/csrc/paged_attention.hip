@@ -550,7 +550,7 @@ int64_t most_splits(int64_t rows, int64_t max_kv) {
   return std::max<int64_t>(1, std::min<int64_t>(ceil_div(max_kv, 256), kPartRows / std::max<int64_t>(rows, 1)));
 }
 
-constexpr int64_t kLongKeys = 8192;
+constexpr int64_t kLongKeys = 4096, kMostSharedTiles = 4096;
 constexpr int kShares = 512;          // workgroups that share the contexts: two to a compute unit
 int64_t shares(int64_t hkv) { return std::max<int64_t>(1, kShares / hkv); }
 
@@ -605,15 +605,18 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
     // on no difference), and a sequence's parts fit the workspace
     a.least_share = a.splits > 1 ? (int)std::max<int64_t>(2, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
   } else {
-    const int64_t items = paged_attention_chunk_items(a);
     // Workgroups run in rounds, one to a compute unit, and the host does not know how much each has to do.  Shares cost each workgroup
-    // a second item's queries and half done outputs, and a second kernel: they are taken where the last round would leave a fifth of
-    // the compute units idle or more (us, whole | in shares, 128 channels: 8 items of 2048 keys 81 | 47, 128 of up to 1024 52 | 60, 256 of
-    // up to 4096 164 | 175; 64 channels: 324 of 2500 161 | 133, 576 of 5000 434 | 394), and for any number where contexts are long, which
-    // are seldom the same (768 items of 8192: 906 | 961; 320 of 16384: 1236 | 905; two sequences of 16384 and 8283: 914 | 836).
-    const int64_t rounds = ceil_div(items, kChunkShares), idle = rounds * kChunkShares - items;
-    const bool shared = keys >= kLongKeys || (keys >= kSharedChunkKeys && 5 * idle >= rounds * kChunkShares);
-    a.splits = !shared || items >= 4 * kChunkShares || items * ceil_div(max_kv, 64) > INT32_MAX / 4 ? 1 : 2;
+    // a second item's queries and half done outputs, and a second kernel: they are taken where the last round would leave a fifth of the
+    // compute units idle or more, and for a single round of long contexts, which are seldom the same.  us, whole | in shares, contexts of one length (of
+    // different ones, down to a fifth), 128 channels: 8 items of 2048 keys 78 | 45, 256 of 2048 84 | 97 (84 | 91), of 4096 162 | 174 (159 | 143), of
+    // 16384 643 | 656 (598 | 430); 400 of 16384 (849 | 813); 512 of 16384 1208 | 1248 (774 | 846); 768 of 8192 874 | 912; 64 channels: 212 of 5000
+    // (154 | 118), 324 of 2500 161 | 131, 576 of 5000 431 | 390; a chunk of 512 beside 15 single tokens, all of 32768: 192 of the 1024 tiles that max_q
+    // alone would say, 3000 | 945.
+    const ChunkItems items = paged_attention_chunk_items(a);
+    const int64_t rounds = ceil_div(items.busy, kChunkShares), idle = rounds * kChunkShares - items.busy;
+    const bool shared = keys >= kSharedChunkKeys && (5 * idle >= rounds * kChunkShares || (rounds == 1 && keys >= kLongKeys));
+    // (every workgroup looks through all tiles for its share, and counts work in 32 bits)
+    a.splits = !shared || items.tiles / hkv > kMostSharedTiles || items.tiles * ceil_div(max_kv, 64) > INT32_MAX / 4 ? 1 : 2;
     a.slot_rows = (int)std::min<int64_t>(kChunkRows, hq * t);
   }
   const int64_t part_rows = rows_form ? a.splits * t * hq : 2 * kChunkShares * a.slot_rows;

@@ -776,10 +776,11 @@ bool chunk_launch(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t paged_attention_chunk_items(const AttendArgs& a) {
+ChunkItems paged_attention_chunk_items(const AttendArgs& a) {
   const int64_t rows = a.d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows;
   static_assert(Chunk<128>::kRows <= kChunkRows && Chunk<64>::kRows == Chunk<128>::kRows, "");
-  return (int64_t)a.b * a.c.heads * ceil_div((int64_t)a.max_q * a.group, rows);
+  const int64_t tiles = (int64_t)a.b * ceil_div((int64_t)a.max_q * a.group, rows), busy = (int64_t)a.t * a.group / rows + a.b;
+  return ChunkItems{tiles * a.c.heads, std::min(tiles, busy) * a.c.heads};
 }
 
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s) {
