@@ -522,8 +522,9 @@ ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const ui
  * Keys and values stand for scale (code - zero) exactly; scores, running maxima and sums are float32.  Weights are rounded to
  * float16 (2^-11, or 2^-24 of the largest where that is more) before they meet the values; in chunks of queries (more than 16 rows,
  * tokens times group, to a key head) the values are too, and the sum is of the rounded weights.  With fewer rows the matrix unit adds the products of
- * 4-bit values to within 2^-17 of the largest.  A key that is not seen has no effect, whatever its scales hold; one that is seen
- * and whose scales are NaN makes the row NaN.
+ * 4-bit values to within 2^-17 of the largest.  The largest is that of the keys that the row sees: a key that is not seen has no effect, not in
+ * one bit, whatever its scales hold; one that is seen and whose scales are NaN makes the row NaN.  Values may be of any size; scales outside
+ * 2^-18 to 2^4 (4 bits: 2^8) in chunks, and outside 2^-40 to 2^40 otherwise, take up to twice the time.
  *
  * Q, O      token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_BF16.  O is not Q.
  * cu_q, kv_lens   b + 1 and b int32 on the device.  A sequence that would begin before token 0 or end past t is left out; keys past

@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kSkinnyWaves * 64) void skinny_kernel(LinearArgs a)
 // If n is not a multiple of 128 the stage that holds the rest comes first, with its lanes past n sent out of the buffer's range
 // (zeros): the main loop does not have to know about it.
 //
-// 8192 tokens x 11008 x 4096: 348 us, 2.1 POP/s, the rate of a large library product.  333 tokens x 4096 x 11008: 27.3 us, 1.1 POP/s: 192 tiles of
+// 8192 tokens x 11008 x 4096: 353 us, 2.1 POP/s, the rate of a large library product.  333 tokens x 4096 x 11008: 27.7 us, 1.1 POP/s: 192 tiles of
 // 86 stages that take 0.26 us each, of which the products are 0.11.
 
 __device__ __forceinline__ int turn(int r) { return (r & 7) ^ ((r >> 3) & 1); }

@@ -15,14 +15,17 @@
 // bfloat16 outputs see nothing; the sum of the weights is of the rounded ones, a channel of ones beside the values', so that the rounding of a
 // weight drops out where the values are alike.  All sums are float32.
 //
-// A value's scale outside that range is brought to its nearer end by a power of two 2^x, which goes into the weights instead: a row that sees such a key
-// takes 2^(y f + x - A) with a running maximum A of its own for the numerator, 2^(y f - M) for the sum, and joins them at its end.  This is
-// decided by row, and nothing that the other rows see enters into it: a key that a row does not see leaves its result as it is, bit by bit.
+// A value's scale outside that range is brought to its nearer end by a power of two 2^x, which goes into the weights instead: from the first such key
+// that a row sees on, M is the maximum of y f + x and the numerator's weights are 2^(y f + x - M), while the sum is that of 2^(y f - m), m a
+// maximum of its own; the row joins them at its end.  This is decided by row, and nothing that other rows see enters into it: a key that a row does
+// not see leaves its result as it is, bit by bit.  (Such a row, or a tile with such a key, nearly doubles its wave's turn: the case below takes 1470 us
+// with all scales out of range.)
 //
 // Bound: a turn of one half of the workgroup, softmax (a score takes about eleven instruction slots, four of them the power of two) and the codes'
-// way to float16, while the other half has the matrix unit (16 d flops a score): vector instructions are issued 43 % of the time, the
-// matrix unit is busy 39 %.  Chunks of 2048 and 1035 tokens against 16384 and 8283 keys, 32 heads of 128 channels over 8: 823 us,
-// 785 TFLOP/s of float16 products.
+// way to float16, while the other half has the matrix unit (16 d flops a score).  At d = 128 a turn takes 2600 cycles, of which the matrix
+// instructions are 1150; vector instructions are issued 44 % of the time, the matrix unit is busy 40 %: neither is full, a wave to a SIMD waits for
+// its own results.  Chunks of 2048 and 1035 tokens against 16384 and 8283 keys, 32 heads of 128 channels over 8: 808 to 835 us by the card,
+// 775 to 800 TFLOP/s of float16 products.
 //
 // Tiles of rows differ in how many keys they see.  Where that would leave compute units idle, all tiles of keys of all tiles of rows are laid
 // end to end and dealt out in equal shares, and a second kernel joins what several workgroups have of a tile of rows.
@@ -39,7 +42,7 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16v;
 
 constexpr int kTile = 64;   // keys
 // Workgroups that share the work, one to a compute unit.  It is counted in tiles of keys, and what comes before and after an item's
-// tiles (queries, first codes, outputs: 13000 cycles, a tile 3200 to 5900) as kStart of them.
+// tiles (queries and first codes 13000 cycles, outputs 8000, a tile 3200 to 5900) as kStart of them.
 constexpr int kShares = kChunkShares, kStart = 4, kLeastShare = 2 * kStart;
 constexpr int kValueLift = 4;         // V' = 2^kValueLift vs (code - zero)
 constexpr int kMetas = 8, kMetaAhead = 4;   // tiles whose Meta is in LDS, and how far before its turn it is brought there
