@@ -543,6 +543,62 @@ ptq_status ptq_paged_attention(const void* Q, ptq_dtype qdt, int64_t q_token, in
                                int64_t window, void* O, int64_t o_token, int64_t o_head, void* ws, size_t ws_bytes,
                                ptq_stream stream);
 
+/*
+ * Rotary positions.  Pairs (a, b) of the first rot channels of a head are turned by angle = positions[i] freq[j]:
+ *   y_a = scale (x_a cos - x_b sin),   y_b = scale (x_a sin + x_b cos),   rounded to float32 and then to the storage type;
+ * pair j < rot / 2 is channels (j, j + rot / 2), with interleaved != 0 channels (2 j, 2 j + 1).  The other channels are copied.  Angles, cosines,
+ * sines and products are float64.  (With -freq the call turns back, and gives the gradient of x from that of y.)
+ *
+ * X, Y      token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_F32 / PTQ_BF16.  Y may be X
+ *           with the same strides; otherwise they do not overlap.  Rows of Y do not overlap each other.
+ * positions t int32.     freq  rot / 2 float64, |positions freq| below 2^50 (beyond, angles are not right any more).
+ * rot       even, 2 <= rot <= d.      d <= 65536.     scale  finite.
+ * No workspace.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE.
+ */
+ptq_status ptq_rotary(const void* X, int64_t x_token, int64_t x_head, ptq_dtype dt, int64_t t, int64_t heads, int64_t d,
+                      const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved, void* Y,
+                      int64_t y_token, int64_t y_head, ptq_stream stream);
+
+/*
+ * Frequencies for ptq_rotary, host arithmetic only (freq is a HOST pointer to rot / 2 values): f_j = base^(-2 j / rot), and for contexts
+ * `factor` times as long as the ones a layer has learnt from
+ *   PTQ_ROTARY_LINEAR   f_j / factor: as if positions were divided by it
+ *   PTQ_ROTARY_BASE     base factor^(rot / (rot - 2)) in place of base: the first pair stays, the last one has f / factor  (rot > 2)
+ *   PTQ_ROTARY_TURNS    f_j (k + (1 - k) / factor), k = clamp((turns_j - slow) / (fast - slow), 0, 1), turns_j = context f_j / (2 pi): pairs that
+ *                       turn more than `fast` times over `context` tokens stay, those that turn less than `slow` times have f / factor
+ * PTQ_ROTARY_PLAIN leaves them, and ignores what follows it.  (The magnitude that some of these go with is ptq_rotary's scale.)
+ * rot even, >= 2; base > 0; factor > 0; with TURNS context > 0, fast > slow; all finite.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE.
+ */
+typedef enum { PTQ_ROTARY_PLAIN = 0, PTQ_ROTARY_LINEAR = 1, PTQ_ROTARY_BASE = 2, PTQ_ROTARY_TURNS = 3 } ptq_rotary_scaling;
+ptq_status ptq_rotary_frequencies(double* freq, int64_t rot, double base, ptq_rotary_scaling scaling, double factor, double context,
+                                  double slow, double fast);
+
+/*
+ * ptq_rotary of queries (Q to Q_out, which may be Q) and keys, and ptq_kv_cache_write of the turned keys and of V, in one launch and with the
+ * same results, bit by bit.  Arguments as there, but d and rot are multiples of 16, d <= 256, and hq is 1 to 65535.  K and V are only
+ * read; Q_out overlaps neither.
+ * Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE.
+ */
+ptq_status ptq_rotary_kv_cache_write(const void* Q, int64_t q_token, int64_t q_head, int64_t hq, const void* K, int64_t k_token,
+                                     int64_t k_head, const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hkv,
+                                     int64_t d, const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved,
+                                     const int32_t* slots, int bits, uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages,
+                                     int64_t page, void* Q_out, int64_t o_token, int64_t o_head, ptq_stream stream);
+
+/*
+ * Copies pages from[i] of one cache (from_*) to pages to[i] of another, or of the same one, 0 <= i < n: keys and values of all heads, codes,
+ * scales and zeros as they are.  What a fork needs for the page in which its sequence goes on (full pages are shared by naming them in both
+ * tables), a compaction for the pages it moves.
+ *
+ * row_bytes  d bits / 8 of both caches, a multiple of 8, at most 256; hkv and page are those of both too.
+ * from, to   n int32 on the device.  Where either is no page of its cache, nothing is copied.  Pages in `to` are different from each other and, within
+ *            one cache, none of them is another's `from` (which of the two would come first is not defined).
+ * Two different caches do not overlap.  No workspace.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE.
+ */
+ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_scales, const uint8_t* from_zeros, int64_t from_pages,
+                                   uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv,
+                                   int64_t row_bytes, const int32_t* from, const int32_t* to, int64_t n, ptq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -147,3 +147,17 @@ def attention(Q, cu_q, codes, scales, zeros, bits: int, table, kv_lens, softmax_
                     r = abs(softmax_scale) * (np.abs(Q[a + rows, h]) @ np.abs(np.where(np.isnan(k), 0.0, k)).T)
                     reach[a + rows, h] = np.where(sees[rows], r, 0).max(1)
     return (O, size, reach) if spread else O
+
+
+def rotary(X, positions, freq, scale=1.0, interleaved=False, dtype="f32"):
+    """X (tokens x heads x d) with its first 2 len(freq) channels turned pair by pair; angles in extended precision (64 bits of fraction)."""
+    X = np.asarray(X, dtype=np.float64)
+    half = len(freq)
+    angle = np.outer(np.asarray(positions).astype(np.longdouble), np.asarray(freq, dtype=np.float64).astype(np.longdouble))
+    cos, sin = (scale * np.cos(angle)).astype(np.float64), (scale * np.sin(angle)).astype(np.float64)
+    Y = X.copy()
+    for j in range(half):
+        a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + half)
+        Y[:, :, a] = X[:, :, a] * cos[:, j, None] - X[:, :, b] * sin[:, j, None]
+        Y[:, :, b] = X[:, :, a] * sin[:, j, None] + X[:, :, b] * cos[:, j, None]
+    return store(Y, dtype)

@@ -21,6 +21,7 @@ OP_HESSIAN, OP_CHOLESKY_INV, OP_QUANTIZE, OP_LAYER_ERROR = 0, 1, 2, 3
 OP_LOPRO_ORDER, OP_LOPRO_ROTATE_HESSIAN = 4, 5
 OP_ACTIVATION_ABS_SUM, OP_SCALED_R1SVD, OP_LINEAR_FORWARD = 6, 7, 8
 OP_INT8_LINEAR, OP_PAGED_ATTENTION = 10, 11
+PTQ_ROTARY_PLAIN, PTQ_ROTARY_LINEAR, PTQ_ROTARY_BASE, PTQ_ROTARY_TURNS = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -105,6 +106,15 @@ def load_library() -> ctypes.CDLL:
     lib.ptq_paged_attention.restype = c.c_int
     lib.ptq_paged_attention.argtypes = [vp, c.c_int, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, i64, i64, i64, c.c_int, vp,
                                         i64, vp, i64, c.c_double, c.c_int, i64, vp, i64, i64, vp, sz, vp]
+    lib.ptq_rotary.restype = c.c_int
+    lib.ptq_rotary.argtypes = [vp, i64, i64, c.c_int, i64, i64, i64, vp, vp, i64, c.c_double, c.c_int, vp, i64, i64, vp]
+    lib.ptq_rotary_frequencies.restype = c.c_int
+    lib.ptq_rotary_frequencies.argtypes = [vp, i64, c.c_double, c.c_int, c.c_double, c.c_double, c.c_double, c.c_double]
+    lib.ptq_rotary_kv_cache_write.restype = c.c_int
+    lib.ptq_rotary_kv_cache_write.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, i64, c.c_int, i64, i64, i64, vp, vp, i64, c.c_double,
+                                              c.c_int, vp, c.c_int, vp, vp, vp, i64, i64, vp, i64, i64, vp]
+    lib.ptq_kv_cache_copy_pages.restype = c.c_int
+    lib.ptq_kv_cache_copy_pages.argtypes = [vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, vp, vp, i64, vp]
     _LIB = lib
     return lib
 
@@ -501,3 +511,39 @@ def ptq_paged_attention(Q: torch.Tensor, cu_q: torch.Tensor, max_q: int, codes: 
                                                 causal, window, ws)
     if rc:
         raise PtqError(rc, "ptq_paged_attention")
+
+
+def ptq_rotary(X: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, Y: torch.Tensor, scale: float = 1.0,
+               interleaved: bool = False) -> None:
+    """Y (t x heads x d, bfloat16 or float32, may be X) <- X with its first 2 len(freq) channels turned by positions (int32 t) times freq
+    (float64, one per pair of channels) and multiplied by scale."""
+    rc = (_TOKENS or _tokens()).rotary(X, positions, freq, Y, scale, interleaved)
+    if rc:
+        raise PtqError(rc, "ptq_rotary")
+
+
+def ptq_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = PTQ_ROTARY_PLAIN, factor: float = 1.0, context: float = 0.0,
+                           slow: float = 1.0, fast: float = 4.0) -> torch.Tensor:
+    """The rot / 2 frequencies of a rotation (float64, on the host; host arithmetic): see PTQ_ROTARY_LINEAR, _BASE and _TURNS in include/ptq.h."""
+    freq = torch.empty(max(0, rot // 2), dtype=torch.float64)
+    rc = load_library().ptq_rotary_frequencies(freq.data_ptr(), rot, base, scaling, factor, context, slow, fast)
+    if rc:
+        raise PtqError(rc, "ptq_rotary_frequencies")
+    return freq
+
+
+def ptq_rotary_kv_cache_write(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor,
+                              slots: torch.Tensor, bits: int, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
+                              Q_out: torch.Tensor, scale: float = 1.0, interleaved: bool = False) -> None:
+    """Q_out (may be Q) <- ptq_rotary of Q, and ptq_kv_cache_write of ptq_rotary of K and of V, in one launch."""
+    rc = (_TOKENS or _tokens()).rotary_kv_cache_write(Q, K, V, positions, freq, slots, bits, codes, scales, zeros, Q_out, scale, interleaved)
+    if rc:
+        raise PtqError(rc, "ptq_rotary_kv_cache_write")
+
+
+def ptq_kv_cache_copy_pages(from_codes: torch.Tensor, from_scales: torch.Tensor, from_zeros: torch.Tensor, source: torch.Tensor,
+                            codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor, target: torch.Tensor) -> None:
+    """Pages target (int32) of the cache codes, scales, zeros <- pages source (int32) of the cache from_*, which may be the same one."""
+    rc = (_TOKENS or _tokens()).kv_cache_copy_pages(from_codes, from_scales, from_zeros, source, codes, scales, zeros, target)
+    if rc:
+        raise PtqError(rc, "ptq_kv_cache_copy_pages")

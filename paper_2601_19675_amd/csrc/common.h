@@ -184,5 +184,17 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
                                   const int32_t* table, int64_t ldt, const int32_t* kv_lens, int64_t max_kv,
                                   double softmax_scale, int causal, int64_t window, void* O, int64_t o_token, int64_t o_head,
                                   void* ws, hipStream_t s);
+void rotary_frequencies(double* freq, int64_t rot, double base, ptq_rotary_scaling scaling, double factor, double context, double slow, double fast);
+ptq_status rotary_launch(const void* X, int64_t x_token, int64_t x_head, ptq_dtype dt, int64_t t, int64_t heads, int64_t d,
+                         const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved, void* Y,
+                         int64_t y_token, int64_t y_head, hipStream_t s);
+ptq_status rotary_kv_cache_write_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t hq, const void* K, int64_t k_token,
+                                        int64_t k_head, const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hkv,
+                                        int64_t d, const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved,
+                                        const int32_t* slots, int bits, uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages,
+                                        int64_t page, void* Q_out, int64_t o_token, int64_t o_head, hipStream_t s);
+ptq_status kv_cache_copy_pages_launch(const uint8_t* from_codes, const float* from_scales, const uint8_t* from_zeros, int64_t from_pages,
+                                      uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv,
+                                      int64_t row_bytes, const int32_t* from, const int32_t* to, int64_t n, hipStream_t s);
 
 }  // namespace ptq

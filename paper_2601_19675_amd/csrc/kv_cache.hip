@@ -11,9 +11,8 @@
 // TB/s; a large copy has 4.7.
 #include <algorithm>
 
-#include "kv_cache.h"
+#include "kv_grid.h"
 #include "static_for.h"
-#include "stored_rows.h"
 
 namespace ptq {
 namespace {
@@ -28,36 +27,12 @@ struct WriteArgs {
   KvCache c;
 };
 
-// the largest over the LANES lanes of a row
-template <int LANES, class T>
-__device__ __forceinline__ T row_max(T v) {
-  v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppSwapPairs, 0xf, 0xf, true));
-  v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppSwapHalfQuads, 0xf, 0xf, true));
-  v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppHalfMirror, 0xf, 0xf, true));
-  if constexpr (LANES >= 16) v = max(v, (T)__builtin_amdgcn_update_dpp(0, (int)v, kDppMirror, 0xf, 0xf, true));
-  if constexpr (LANES >= 32) v = max(v, (T)__shfl_xor((int)v, 16));
-  return v;
-}
-
-// what lane I of every four lanes has
-template <int I>
-__device__ __forceinline__ float of_four(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x55 * I, 0xf, 0xf, true));
-}
-
-// the quotient of d by a small whole number, correctly rounded: r = d - q by is exact, its share is added once
-__device__ __forceinline__ double divided(double d, double by, double inv) {
-  const double q = d * inv;
-  return fma(fma(-q, by, d), inv, q);
-}
-
 // LANES lanes to a row; consecutive groups take consecutive tokens of one head, whose rows lie side by side in a page.  Consecutive
 // workgroups take the heads of the same tokens: a head's rows alone, 8 KB apart in a projection's output, would fall on few of the
 // memory's channels (20000 tokens x 32 heads x 128 into 4 bits that way: 155 us).
 template <int DT, int BITS, int LANES>
 __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
   constexpr int kGroups = 256 / LANES;
-  constexpr double kTop = (1 << BITS) - 1;
   using ST = typename StoredType<DT>::type;
   const int group = threadIdx.x / LANES, lane = threadIdx.x % LANES, which = blockIdx.y;
   const int tile = blockIdx.x / a.c.heads, head = blockIdx.x % a.c.heads;
@@ -74,82 +49,41 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     slot[i] = token < a.t ? a.slots[safe] : -1;
     x[i] = load_run<DT, 8, false>(X + safe * stride, c, a.d);
   }
-  // Bits tell a row's extremes, and whether all of it is finite: as signed numbers those of the largest value come last, as
-  // unsigned ones those of the value furthest below 0, if one is.
-  int hi_bits = 0;
-  uint32_t lo_bits = 0;
+  RowExtremes most;
 #pragma unroll
   for (int i = 0; i < kRowsPerLane; ++i) {
     float v[8];
     run_to_f32<DT, 8>(x[i], c, a.d, v);
-    int hi = 0;
-    uint32_t lo = 0;
+    RowExtremes row;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      hi = max(hi, __float_as_int(v[e]));
-      lo = max(lo, __float_as_uint(v[e]));
-    }
-    hi = row_max<LANES>(hi);
-    lo = row_max<LANES>(lo);
+    for (int e = 0; e < 8; ++e) row.take(v[e]);
+    row.hi = row_max<LANES>(row.hi);
+    row.lo = row_max<LANES>(row.lo);
     // the grids of the group's four rows are worked out side by side: lane i of every four has row i
-    if ((lane & 3) == i) {
-      hi_bits = hi;
-      lo_bits = lo;
-    }
+    if ((lane & 3) == i) most = row;
   }
-  // a row with an infinity or a NaN: its scale becomes NaN, and so does whatever reads it; its codes 0 (x inv is NaN or 0)
-  const bool finite = hi_bits < 0x7f800000 && lo_bits < 0xff800000u;
-  const float hi = __int_as_float(hi_bits);
-  float lo = lo_bits > 0x80000000u ? __uint_as_float(lo_bits) : 0.f;
-  float scale = finite ? (float)divided((double)hi - (double)lo, kTop, 1.0 / kTop) : 1.f;
-  if (scale == 0.f) {   // nothing but zeros (or less than float32 can divide)
-    lo = -1.f;
-    scale = (float)(2.0 / kTop);
-  }
-  const float below[1] = {finite ? -lo : 0.f};
-  float inv = __builtin_amdgcn_rcpf(scale), z[1];
-  whole_codes<1>(below, inv, 1.f, scale, z);
-  // both ends rounded away from 0 (the only codes past the grid), or no float32 reciprocal: by the quotient, and clamped
-  const bool odd_grid = __any((scale < 0x1p-110f) | (scale > 0x1p110f) | (finite && rintf(hi * inv) + z[0] > (float)kTop));
-  inv = finite ? inv : 0.f;
+  const RowGrid grid = row_grid<BITS>(most);
   {
     int mine = slot[0];
 #pragma unroll
     for (int i = 1; i < kRowsPerLane; ++i) mine = (lane & 3) == i ? slot[i] : mine;
     if (lane < kRowsPerLane && (uint32_t)mine < places) {
       const int64_t row = kv_row(rows, (uint32_t)mine >> a.c.page_shift, mine & ((1 << a.c.page_shift) - 1));
-      a.c.scales[row] = finite ? scale : __uint_as_float(0x7fc00000u);
-      a.c.zeros[row] = (uint8_t)z[0];
+      a.c.scales[row] = grid.finite ? grid.scale : __uint_as_float(0x7fc00000u);
+      a.c.zeros[row] = (uint8_t)grid.zero;
     }
   }
   static_for<kRowsPerLane>([&](auto i_) {
     constexpr int i = decltype(i_)::value;
-    const float inv_i = of_four<i>(inv), z_i = of_four<i>(z[0]);
     float v[8];
     run_to_f32<DT, 8>(x[i], c, a.d, v);
-    // 1.5 2^23 + a whole number has that number in its low bits, and adding it rounds there: code = rne(x inv + zero), which is rne(x / scale) + zero
-    // as long as x inv + zero, off by less than 2^-14 (see whole_codes; the sum adds 2^-17), is not that close to a middle
-    constexpr float kWhole = 12582912.f;
-    const float from = z_i + kWhole;
-    float u[8], far = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      u[e] = fmaf(v[e], inv_i, from);
-      far = fmaxf(far, fabsf(fmaf(v[e], inv_i, from - u[e])));
-    }
-    if (__any(far > 0.5f - 0x1p-14f) | odd_grid) {
-      const float s = of_four<i>(scale), good = of_four<i>(finite ? 1.f : 0.f);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        u[e] = kWhole + (good != 0.f ? fminf((float)rint((double)v[e] / (double)s) + z_i, (float)kTop) : 0.f);
-    }
-    auto byte_pair = [&](int e0, int e1) { return __builtin_amdgcn_perm(__float_as_uint(u[e1]), __float_as_uint(u[e0]), 0x0c0c0400u); };
-    auto bytes = [&](int e0, int e1, int e2, int e3) { return __builtin_amdgcn_perm(byte_pair(e2, e3), byte_pair(e0, e1), 0x05040100u); };
+    uint32_t w[BITS / 4];
+    row_codes_of<BITS, i>(v, grid, w);
     if ((uint32_t)slot[i] < places && c < a.d) {
       const int64_t row = kv_row(rows, (uint32_t)slot[i] >> a.c.page_shift, slot[i] & ((1 << a.c.page_shift) - 1));
       uint8_t* out = a.c.codes + row * a.c.row_bytes + lane * BITS;
-      if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out) = uint2{bytes(0, 1, 2, 3), bytes(4, 5, 6, 7)};
-      else *reinterpret_cast<uint32_t*>(out) = bytes(0, 4, 1, 5) | (bytes(2, 6, 3, 7) << 4);
+      if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out) = uint2{w[0], w[1]};
+      else *reinterpret_cast<uint32_t*>(out) = w[0];
     }
   });
 }

@@ -400,4 +400,66 @@ ptq_status ptq_paged_attention(const void* Q, ptq_dtype qdt, int64_t q_token, in
                                 static_cast<hipStream_t>(stream));
 }
 
+ptq_status ptq_rotary(const void* X, int64_t x_token, int64_t x_head, ptq_dtype dt, int64_t t, int64_t heads, int64_t d,
+                      const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved, void* Y,
+                      int64_t y_token, int64_t y_head, ptq_stream stream) {
+  if (dt != PTQ_F32 && dt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  if (!std::isfinite(scale)) return PTQ_ERR_ARG;
+  if (t < 0 || t > INT32_MAX / 2 || heads < 0 || heads > 65535 || rot < 2 || rot % 2 != 0 || rot > d || d > 65536 || x_token < 0 || x_head < 0 ||
+      y_token < 0 || y_head < 0)
+    return PTQ_ERR_SHAPE;
+  if (t == 0 || heads == 0) return PTQ_OK;
+  if (!X || !Y || !positions || !freq || (X == Y && (x_token != y_token || x_head != y_head))) return PTQ_ERR_ARG;
+  return rotary_launch(X, x_token, x_head, dt, t, heads, d, positions, freq, rot, scale, interleaved, Y, y_token, y_head,
+                       static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_rotary_frequencies(double* freq, int64_t rot, double base, ptq_rotary_scaling scaling, double factor, double context,
+                                  double slow, double fast) {
+  if (rot < 2 || rot % 2 != 0 || rot > 65536) return PTQ_ERR_SHAPE;
+  if (!freq || !(base > 0.0) || !std::isfinite(base) || scaling < PTQ_ROTARY_PLAIN || scaling > PTQ_ROTARY_TURNS) return PTQ_ERR_ARG;
+  if (scaling != PTQ_ROTARY_PLAIN && (!(factor > 0.0) || !std::isfinite(factor))) return PTQ_ERR_ARG;
+  if (scaling == PTQ_ROTARY_BASE && rot == 2) return PTQ_ERR_SHAPE;
+  if (scaling == PTQ_ROTARY_TURNS && (!(context > 0.0) || !std::isfinite(context) || !std::isfinite(slow) || !std::isfinite(fast) || !(fast > slow)))
+    return PTQ_ERR_ARG;
+  rotary_frequencies(freq, rot, base, scaling, factor, context, slow, fast);
+  return PTQ_OK;
+}
+
+ptq_status ptq_rotary_kv_cache_write(const void* Q, int64_t q_token, int64_t q_head, int64_t hq, const void* K, int64_t k_token,
+                                     int64_t k_head, const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hkv,
+                                     int64_t d, const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved,
+                                     const int32_t* slots, int bits, uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages,
+                                     int64_t page, void* Q_out, int64_t o_token, int64_t o_head, ptq_stream stream) {
+  if (dt != PTQ_F32 && dt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  const ptq_status bad = kv_cache_bad(hkv, d, bits, pages, page);
+  if (bad != PTQ_OK) return bad;
+  if (!std::isfinite(scale)) return PTQ_ERR_ARG;
+  if (t < 0 || t > INT32_MAX / 2 || hq <= 0 || hq > 65535 || rot < 16 || rot % 16 != 0 || rot > d || q_token < 0 || q_head < 0 || k_token < 0 ||
+      k_head < 0 || v_token < 0 || v_head < 0 || o_token < 0 || o_head < 0)
+    return PTQ_ERR_SHAPE;
+  if (t == 0) return PTQ_OK;
+  if (!Q || !K || !V || !positions || !freq || !slots || !codes || !scales || !zeros || !Q_out || misaligned(codes, 16) ||
+      (Q == Q_out && (q_token != o_token || q_head != o_head)) || Q_out == K || Q_out == V)
+    return PTQ_ERR_ARG;
+  return rotary_kv_cache_write_launch(Q, q_token, q_head, hq, K, k_token, k_head, V, v_token, v_head, dt, t, hkv, d, positions, freq, rot, scale,
+                                      interleaved, slots, bits, codes, scales, zeros, pages, page, Q_out, o_token, o_head,
+                                      static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_scales, const uint8_t* from_zeros, int64_t from_pages,
+                                   uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv,
+                                   int64_t row_bytes, const int32_t* from, const int32_t* to, int64_t n, ptq_stream stream) {
+  if (row_bytes <= 0 || row_bytes > 256 || row_bytes % 8 != 0 || n < 0 || n > INT32_MAX) return PTQ_ERR_SHAPE;
+  for (const int64_t p : {from_pages, pages}) {
+    const ptq_status bad = kv_cache_bad(hkv, 16, 8, p, page);
+    if (bad != PTQ_OK) return bad;
+  }
+  if (n == 0 || from_pages == 0 || pages == 0) return PTQ_OK;
+  if (!from_codes || !from_scales || !from_zeros || !codes || !scales || !zeros || !from || !to) return PTQ_ERR_ARG;
+  if (misaligned(from_codes, 16) || misaligned(codes, 16)) return PTQ_ERR_ARG;
+  return kv_cache_copy_pages_launch(from_codes, from_scales, from_zeros, from_pages, codes, scales, zeros, pages, page, hkv, row_bytes, from,
+                                    to, n, static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

@@ -1,0 +1,342 @@
+// Rotary positions: pairs of channels of a head, seen as points of a plane, are turned by the token's position times the pair's
+// frequency,
+//   y_a = scale (x_a cos - x_b sin),   y_b = scale (x_a sin + x_b cos),
+// alone (Y may be X), or with the keys going on into the paged cache in the same launch.
+//
+// Bound: bytes, each channel once in and out.  A thread has the same eight pairs of several heads of a token, so that cosines and sines are
+// worked out once for all of them and stay in registers; consecutive threads have a head's row side by side, and consecutive workgroups
+// the heads of the same tokens.  All of it is float64, which runs at float32's rate here and hides behind the memory: what
+// is rounded to a key's type, and decides its codes, is the exact value but for 2^-50.
+#include <algorithm>
+#include <cmath>
+
+#include "kv_grid.h"
+#include "rotary.h"
+#include "static_for.h"
+
+namespace ptq {
+namespace {
+
+constexpr int kHeadsAhead = 4;   // heads whose channels are on their way together
+
+struct RotaryArgs {
+  const void* X; void* Y;
+  int64_t x_token, x_head, y_token, y_head;
+  const int32_t* positions; const double* freq;
+  int t, heads, d, rot, interleaved;
+  int slices, per;                 // workgroups to a tile of tokens, and heads of each
+  double scale;
+};
+
+// Which two runs of eight channels a lane has, and whether they are pairs that turn (eight frequencies from 8 lane on; rot % 16 == 0).
+struct LaneRuns { int a, b; bool turns; };
+__device__ __forceinline__ LaneRuns lane_runs(int lane, int rot, int interleaved) {
+  if (interleaved) return LaneRuns{16 * lane, 16 * lane + 8, 16 * lane < rot};
+  if (16 * lane < rot) return LaneRuns{8 * lane, 8 * lane + rot / 2, true};
+  return LaneRuns{16 * lane, 16 * lane + 8, false};
+}
+// cosines and sines of the lane's pairs; those of a lane without are not used
+__device__ __forceinline__ void lane_angles(const LaneRuns& runs, int lane, int position, const double* freq, double scale, CosSin (&t)[8]) {
+  double f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = freq[runs.turns ? 8 * lane + e : 0];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) t[e] = cos_sin(position, f[e], scale);
+}
+__device__ __forceinline__ void turn_runs(float (&u)[8], float (&v)[8], const LaneRuns& runs, int interleaved, const CosSin (&t)[8]) {
+  if (!runs.turns) return;
+  if (interleaved) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      turn(u[2 * e], u[2 * e + 1], t[e]);
+      turn(v[2 * e], v[2 * e + 1], t[4 + e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) turn(u[e], v[e], t[e]);
+  }
+}
+
+// LANES lanes to a row of up to 16 LANES channels (d % 16 == 0, rot % 16 == 0); workgroup (tile, slice)
+template <int DT, int LANES>
+__device__ __forceinline__ void rotary_rows(const RotaryArgs& a, int tile, int slice) {
+  constexpr int kTokens = 256 / LANES;
+  using ST = typename StoredType<DT>::type;
+  const int lane = threadIdx.x % LANES, token = tile * kTokens + threadIdx.x / LANES, safe = min(token, a.t - 1);
+  const LaneRuns runs = lane_runs(lane, a.rot, a.interleaved);
+  const int first = slice * a.per, last = min(a.heads, first + a.per);
+  const ST* X = static_cast<const ST*>(a.X) + safe * a.x_token;
+  ST* Y = static_cast<ST*>(a.Y) + safe * a.y_token;
+  const int position = a.positions[safe];
+  CosSin angles[8];
+  bool ready = false;
+  for (int h0 = first; h0 < last; h0 += kHeadsAhead) {
+    Run<DT, 8> x[kHeadsAhead][2];
+#pragma unroll
+    for (int i = 0; i < kHeadsAhead; ++i) {
+      const ST* row = X + min(h0 + i, last - 1) * a.x_head;
+      x[i][0] = load_run<DT, 8, false>(row, runs.a, a.d);
+      x[i][1] = load_run<DT, 8, false>(row, runs.b, a.d);
+    }
+    if (!ready) lane_angles(runs, lane, position, a.freq, a.scale, angles);
+    ready = true;
+#pragma unroll
+    for (int i = 0; i < kHeadsAhead; ++i) {
+      float u[8], v[8];
+      run_to_f32<DT, 8>(x[i][0], runs.a, a.d, u);
+      run_to_f32<DT, 8>(x[i][1], runs.b, a.d, v);
+      turn_runs(u, v, runs, a.interleaved, angles);
+      if (token < a.t && h0 + i < last) {
+        store_run<DT, 8, false>(Y + (h0 + i) * a.y_head, runs.a, a.d, u);
+        store_run<DT, 8, false>(Y + (h0 + i) * a.y_head, runs.b, a.d, v);
+      }
+    }
+  }
+}
+
+template <int DT, int LANES>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
+  rotary_rows<DT, LANES>(a, blockIdx.x / a.slices, blockIdx.x % a.slices);
+}
+
+// Any widths: a thread has one pair, or two channels that stay as they are, of a token's heads.
+template <int DT>
+__global__ __launch_bounds__(256) void rotary_any_kernel(RotaryArgs a, int64_t first_tile) {
+  using ST = typename StoredType<DT>::type;
+  const int slice = blockIdx.x % a.slices, pairs = (a.d + 1) / 2;
+  const int64_t i = (first_tile + blockIdx.x / a.slices) * 256 + threadIdx.x, token = i / pairs;
+  if (token >= a.t) return;
+  const int p = (int)(i - token * pairs);
+  const bool turns = 2 * p < a.rot;
+  const int ca = turns && !a.interleaved ? p : 2 * p, cb = turns && !a.interleaved ? p + a.rot / 2 : 2 * p + 1;
+  const bool both = cb < a.d;
+  const int last = min(a.heads, (slice + 1) * a.per);
+  const ST* X = static_cast<const ST*>(a.X) + token * a.x_token;
+  ST* Y = static_cast<ST*>(a.Y) + token * a.y_token;
+  CosSin angle{1.0, 0.0};
+  if (turns) angle = cos_sin(a.positions[token], a.freq[p], a.scale);
+  for (int h0 = slice * a.per; h0 < last; h0 += kHeadsAhead) {
+    ST x[kHeadsAhead][2];
+#pragma unroll
+    for (int k = 0; k < kHeadsAhead; ++k) {
+      const ST* row = X + min(h0 + k, last - 1) * a.x_head;
+      x[k][0] = row[ca];
+      x[k][1] = row[both ? cb : ca];
+    }
+#pragma unroll
+    for (int k = 0; k < kHeadsAhead; ++k) {
+      if (h0 + k >= last) break;
+      ST* row = Y + (h0 + k) * a.y_head;
+      if (turns) {
+        float u = (float)stored_to_f64<DT>(x[k][0]), v = (float)stored_to_f64<DT>(x[k][1]);
+        turn(u, v, angle);
+        if constexpr (DT == PTQ_BF16) {
+          row[ca] = f32_to_bf16_bits(u);
+          row[cb] = f32_to_bf16_bits(v);
+        } else {
+          row[ca] = u;
+          row[cb] = v;
+        }
+      } else {
+        row[ca] = x[k][0];
+        if (both) row[cb] = x[k][1];
+      }
+    }
+  }
+}
+
+struct RotaryCacheArgs {
+  RotaryArgs q;                    // .t, .d, .rot, .positions ... are the keys' too
+  const void* X[2];                // keys, values
+  int64_t token[2], head[2];
+  const int32_t* slots;
+  int slices, per;                 // of the keys, and of the values
+  KvCache c;
+};
+
+// Keys (turned) or values of a tile of tokens and a slice of heads into the cache: kv_cache.hip's rows, with the lanes' two runs.
+template <int DT, int BITS, int LANES>
+__device__ __forceinline__ void cache_rows(const RotaryCacheArgs& a, int tile, int slice, int which) {
+  constexpr int kTokens = 256 / LANES;
+  using ST = typename StoredType<DT>::type;
+  const int lane = threadIdx.x % LANES, token = tile * kTokens + threadIdx.x / LANES, safe = min(token, a.q.t - 1);
+  LaneRuns runs = lane_runs(lane, a.q.rot, a.q.interleaved);
+  if (which) runs.turns = false;
+  const int first = slice * a.per, last = min(a.c.heads, first + a.per);
+  const ST* X = static_cast<const ST*>(which ? a.X[1] : a.X[0]) + safe * (which ? a.token[1] : a.token[0]);
+  const int64_t stride = which ? a.head[1] : a.head[0];
+  const int position = a.q.positions[safe], slot = token < a.q.t ? a.slots[safe] : -1;
+  const bool there = (uint32_t)slot < (uint32_t)(a.c.pages << a.c.page_shift);
+  const int place = there ? slot : 0;
+  const uint32_t page = (uint32_t)place >> a.c.page_shift, offset = place & ((1 << a.c.page_shift) - 1);
+  CosSin angles[8];
+  bool ready = which != 0;
+  for (int h0 = first; h0 < last; h0 += kHeadsAhead) {
+    Run<DT, 8> x[kHeadsAhead][2];
+#pragma unroll
+    for (int i = 0; i < kHeadsAhead; ++i) {
+      const ST* row = X + min(h0 + i, last - 1) * stride;
+      x[i][0] = load_run<DT, 8, false>(row, runs.a, a.q.d);
+      x[i][1] = load_run<DT, 8, false>(row, runs.b, a.q.d);
+    }
+    if (!ready) lane_angles(runs, lane, position, a.q.freq, a.q.scale, angles);
+    ready = true;
+    float v[kHeadsAhead][2][8];
+    RowExtremes most;
+#pragma unroll
+    for (int i = 0; i < kHeadsAhead; ++i) {
+      run_to_f32<DT, 8>(x[i][0], runs.a, a.q.d, v[i][0]);
+      run_to_f32<DT, 8>(x[i][1], runs.b, a.q.d, v[i][1]);
+      turn_runs(v[i][0], v[i][1], runs, a.q.interleaved, angles);
+      RowExtremes row;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[i][k][e] = as_stored<DT>(v[i][k][e]);
+          row.take(v[i][k][e]);
+        }
+      row.hi = row_max<LANES>(row.hi);
+      row.lo = row_max<LANES>(row.lo);
+      if ((lane & 3) == i) most = row;
+    }
+    const RowGrid grid = row_grid<BITS>(most);
+    auto row_at = [&](int head) { return kv_row(kv_rows(a.c, which, head), page, offset); };
+    if (lane < kHeadsAhead && there && h0 + lane < last) {
+      const int64_t row = row_at(h0 + lane);
+      a.c.scales[row] = grid.finite ? grid.scale : __uint_as_float(0x7fc00000u);
+      a.c.zeros[row] = (uint8_t)grid.zero;
+    }
+    static_for<kHeadsAhead>([&](auto i_) {
+      constexpr int i = decltype(i_)::value;
+      uint32_t w[2][BITS / 4];
+      row_codes_of<BITS, i>(v[i][0], grid, w[0]);
+      row_codes_of<BITS, i>(v[i][1], grid, w[1]);
+      if (there && h0 + i < last && runs.a < a.q.d) {   // (d % 16 == 0: a lane has both of its runs or neither)
+        uint8_t* out = a.c.codes + row_at(h0 + i) * a.c.row_bytes;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint8_t* at = out + (k ? runs.b : runs.a) / 8 * BITS;
+          if constexpr (BITS == 8) *reinterpret_cast<uint2*>(at) = uint2{w[k][0], w[k][1]};
+          else *reinterpret_cast<uint32_t*>(at) = w[k][0];
+        }
+      }
+    });
+  }
+}
+
+template <int DT, int BITS, int LANES>
+__global__ __launch_bounds__(256) void rotary_cache_kernel(RotaryCacheArgs a) {
+  const int all = a.q.slices + 2 * a.slices, tile = blockIdx.x / all, part = blockIdx.x % all;
+  if (part < a.q.slices) rotary_rows<DT, LANES>(a.q, tile, part);
+  else cache_rows<DT, BITS, LANES>(a, tile, (part - a.q.slices) % a.slices, (part - a.q.slices) / a.slices);
+}
+
+int lanes_of(int64_t d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+
+// Heads of a workgroup: as many as leave the device 2048 workgroups (eight to a compute unit), between one round of loads and eight of them.
+// (The angles of a round's heads take as long as turning one head.)
+int heads_per(int64_t tiles, int64_t heads) {
+  const int64_t most = std::max<int64_t>(1, tiles * heads / 2048);
+  return (int)std::min<int64_t>(heads, std::min<int64_t>(8 * kHeadsAhead, ceil_div(most, kHeadsAhead) * kHeadsAhead));
+}
+// tiles of a launch, which has fewer than 2^32 threads
+int64_t launch_tiles(int64_t slices) { return std::max<int64_t>(1, (1 << 23) / slices); }
+
+template <int DT>
+void rotary_typed(const RotaryArgs& all, hipStream_t s) {
+  using ST = typename StoredType<DT>::type;
+  RotaryArgs a = all;
+  const bool runs = all.d % 16 == 0 && all.d <= 256 && all.rot % 16 == 0;
+  const int lanes = lanes_of(all.d), tokens = 256 / lanes;
+  const int64_t tiles = runs ? ceil_div(all.t, tokens) : ceil_div((int64_t)all.t * ((all.d + 1) / 2), 256);
+  a.per = heads_per(tiles, all.heads);
+  a.slices = (int)ceil_div(all.heads, a.per);
+  const int64_t step = launch_tiles(a.slices);
+  for (int64_t first = 0; first < tiles; first += step) {
+    const int64_t n = std::min(step, tiles - first);
+    const unsigned grid = (unsigned)(n * a.slices);
+    if (!runs) {
+      rotary_any_kernel<DT><<<grid, 256, 0, s>>>(a, first);
+      continue;
+    }
+    a.X = static_cast<const ST*>(all.X) + first * tokens * a.x_token;
+    a.Y = static_cast<ST*>(all.Y) + first * tokens * a.y_token;
+    a.positions = all.positions + first * tokens;
+    a.t = (int)std::min<int64_t>(n * tokens, all.t - first * tokens);
+    if (lanes == 4) rotary_kernel<DT, 4><<<grid, 256, 0, s>>>(a);
+    else if (lanes == 8) rotary_kernel<DT, 8><<<grid, 256, 0, s>>>(a);
+    else rotary_kernel<DT, 16><<<grid, 256, 0, s>>>(a);
+  }
+}
+
+template <int DT, int BITS>
+void rotary_cache_typed(const RotaryCacheArgs& all, hipStream_t s) {
+  using ST = typename StoredType<DT>::type;
+  RotaryCacheArgs a = all;
+  const int lanes = lanes_of(all.q.d), tokens = 256 / lanes;
+  const int64_t tiles = ceil_div(all.q.t, tokens);
+  const int64_t heads = all.q.heads + 2 * all.c.heads;
+  a.q.per = std::min(all.q.heads, heads_per(tiles, heads));
+  a.q.slices = (int)ceil_div(all.q.heads, a.q.per);
+  a.per = std::min(all.c.heads, heads_per(tiles, heads));
+  a.slices = (int)ceil_div(all.c.heads, a.per);
+  const int64_t each = a.q.slices + 2 * a.slices, step = launch_tiles(each);
+  for (int64_t first = 0; first < tiles; first += step) {
+    const int64_t n = std::min(step, tiles - first), at = first * tokens;
+    a.q.X = static_cast<const ST*>(all.q.X) + at * a.q.x_token;
+    a.q.Y = static_cast<ST*>(all.q.Y) + at * a.q.y_token;
+    a.q.positions = all.q.positions + at;
+    a.slots = all.slots + at;
+    for (int i = 0; i < 2; ++i) a.X[i] = static_cast<const ST*>(all.X[i]) + at * a.token[i];
+    a.q.t = (int)std::min<int64_t>(n * tokens, all.q.t - at);
+    const unsigned grid = (unsigned)(n * each);
+    if (lanes == 4) rotary_cache_kernel<DT, BITS, 4><<<grid, 256, 0, s>>>(a);
+    else if (lanes == 8) rotary_cache_kernel<DT, BITS, 8><<<grid, 256, 0, s>>>(a);
+    else rotary_cache_kernel<DT, BITS, 16><<<grid, 256, 0, s>>>(a);
+  }
+}
+
+}  // namespace
+
+void rotary_frequencies(double* freq, int64_t rot, double base, ptq_rotary_scaling scaling, double factor, double context, double slow, double fast) {
+  const double pi = 3.14159265358979323846;
+  if (scaling == PTQ_ROTARY_BASE && rot > 2) base *= std::pow(factor, (double)rot / (double)(rot - 2));
+  for (int64_t i = 0; i < rot / 2; ++i) {
+    double f = std::pow(base, -2.0 * (double)i / (double)rot);
+    if (scaling == PTQ_ROTARY_LINEAR) f /= factor;
+    if (scaling == PTQ_ROTARY_TURNS) {
+      const double turns = context * f / (2.0 * pi), kept = std::min(1.0, std::max(0.0, (turns - slow) / (fast - slow)));
+      f *= kept + (1.0 - kept) / factor;
+    }
+    freq[i] = f;
+  }
+}
+
+ptq_status rotary_launch(const void* X, int64_t x_token, int64_t x_head, ptq_dtype dt, int64_t t, int64_t heads, int64_t d,
+                         const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved, void* Y,
+                         int64_t y_token, int64_t y_head, hipStream_t s) {
+  const RotaryArgs a{X, Y, x_token, x_head, y_token, y_head, positions, freq, (int)t, (int)heads, (int)d, (int)rot, interleaved, 1, 1, scale};
+  dt == PTQ_BF16 ? rotary_typed<PTQ_BF16>(a, s) : rotary_typed<PTQ_F32>(a, s);
+  PTQ_HIP_CHECK_LAUNCH();
+  return PTQ_OK;
+}
+
+ptq_status rotary_kv_cache_write_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t hq, const void* K, int64_t k_token,
+                                        int64_t k_head, const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hkv,
+                                        int64_t d, const int32_t* positions, const double* freq, int64_t rot, double scale, int interleaved,
+                                        const int32_t* slots, int bits, uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages,
+                                        int64_t page, void* Q_out, int64_t o_token, int64_t o_head, hipStream_t s) {
+  RotaryCacheArgs a{};
+  a.q = RotaryArgs{Q, Q_out, q_token, q_head, o_token, o_head, positions, freq, (int)t, (int)hq, (int)d, (int)rot, interleaved, 1, 1, scale};
+  a.X[0] = K, a.X[1] = V;
+  a.token[0] = k_token, a.token[1] = v_token, a.head[0] = k_head, a.head[1] = v_head;
+  a.slots = slots;
+  a.c = KvCache{codes, scales, zeros, pages, (int)hkv, __builtin_ctz((unsigned)page), (int)(d * bits / 8)};
+  if (dt == PTQ_BF16) bits == 8 ? rotary_cache_typed<PTQ_BF16, 8>(a, s) : rotary_cache_typed<PTQ_BF16, 4>(a, s);
+  else bits == 8 ? rotary_cache_typed<PTQ_F32, 8>(a, s) : rotary_cache_typed<PTQ_F32, 4>(a, s);
+  PTQ_HIP_CHECK_LAUNCH();
+  return PTQ_OK;
+}
+
+}  // namespace ptq

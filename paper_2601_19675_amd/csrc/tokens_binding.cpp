@@ -249,9 +249,81 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
+// X and Y of a rotation, positions and frequencies
+void rotary_ok(const Tensor& X, const Tensor& Y, const Tensor& positions, const Tensor& freq) {
+  PTQ_CHECK(X.dim() == 3 && X.stride(2) == 1 && Y.sizes() == X.sizes() && Y.stride(2) == 1 && Y.scalar_type() == X.scalar_type());
+  PTQ_CHECK(whole_numbers(positions, X.size(0)));
+  PTQ_CHECK(freq.scalar_type() == at::kDouble && freq.is_contiguous() && freq.dim() == 1);
+}
+
+// X, positions, freq, Y, scale, interleaved
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (!count_is(count, 6)) return nullptr;
+  return status_of([&]() -> ptq_status {
+    const Tensor &X = tensor(a[0]), &positions = tensor(a[1]), &freq = tensor(a[2]), &Y = tensor(a[3]);
+    const double scale = number(a[4]);
+    const int interleaved = truth(a[5]);
+    rotary_ok(X, Y, positions, freq);
+    ptq_dtype dt;
+    if (!dtype_of(X, dt)) return PTQ_ERR_DTYPE;
+    const ptq_stream s = stream();
+    return released([&] {
+      return ptq_rotary(ptr(X), X.stride(0), X.stride(1), dt, X.size(0), X.size(1), X.size(2), as<int32_t>(positions), as<double>(freq), 2 * freq.numel(),
+                        scale, interleaved, ptr(Y), Y.stride(0), Y.stride(1), s);
+    });
+  });
+}
+
+// Q, K, V, positions, freq, slots, bits, codes, scales, zeros, Q_out, scale, interleaved
+PyObject* rotary_kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (!count_is(count, 13)) return nullptr;
+  return status_of([&]() -> ptq_status {
+    const Tensor &Q = tensor(a[0]), &K = tensor(a[1]), &V = tensor(a[2]), &positions = tensor(a[3]), &freq = tensor(a[4]), &slots = tensor(a[5]),
+                 &codes = tensor(a[7]), &scales = tensor(a[8]), &zeros = tensor(a[9]), &O = tensor(a[10]);
+    const int64_t bits = whole(a[6]);
+    const double scale = number(a[11]);
+    const int interleaved = truth(a[12]);
+    rotary_ok(Q, O, positions, freq);
+    PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.sizes() == K.sizes() && V.stride(2) == 1 && K.scalar_type() == Q.scalar_type() && V.scalar_type() == Q.scalar_type());
+    const int64_t t = K.size(0), heads = K.size(1), d = K.size(2);
+    PTQ_CHECK(Q.size(0) == t && Q.size(2) == d);
+    const Cache c = cache_of(codes, scales, zeros, bits, d);
+    PTQ_CHECK(c.heads == heads);
+    PTQ_CHECK(whole_numbers(slots, t));
+    ptq_dtype dt;
+    if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
+    const ptq_stream s = stream();
+    return released([&] {
+      return ptq_rotary_kv_cache_write(ptr(Q), Q.stride(0), Q.stride(1), Q.size(1), ptr(K), K.stride(0), K.stride(1), ptr(V), V.stride(0), V.stride(1), dt,
+                                       t, heads, d, as<int32_t>(positions), as<double>(freq), 2 * freq.numel(), scale, interleaved, as<int32_t>(slots),
+                                       (int)bits, as<uint8_t>(codes), as<float>(scales), as<uint8_t>(zeros), c.pages, c.page, ptr(O), O.stride(0),
+                                       O.stride(1), s);
+    });
+  });
+}
+
+// from_codes, from_scales, from_zeros, source, codes, scales, zeros, target
+PyObject* kv_cache_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (!count_is(count, 8)) return nullptr;
+  return status_of([&]() -> ptq_status {
+    const Tensor &fc = tensor(a[0]), &fs = tensor(a[1]), &fz = tensor(a[2]), &source = tensor(a[3]), &codes = tensor(a[4]), &scales = tensor(a[5]),
+                 &zeros = tensor(a[6]), &target = tensor(a[7]);
+    PTQ_CHECK(fc.dim() == 5 && codes.dim() == 5 && fc.size(4) == codes.size(4));
+    const Cache from = cache_of(fc, fs, fz, 8, fc.size(4)), to = cache_of(codes, scales, zeros, 8, codes.size(4));
+    PTQ_CHECK(from.heads == to.heads && from.page == to.page);
+    const int64_t n = source.numel();
+    PTQ_CHECK(whole_numbers(source, n) && whole_numbers(target, n));
+    const ptq_stream s = stream();
+    return released([&] {
+      return ptq_kv_cache_copy_pages(as<uint8_t>(fc), as<float>(fs), as<uint8_t>(fz), from.pages, as<uint8_t>(codes), as<float>(scales), as<uint8_t>(zeros),
+                                     to.pages, to.page, to.heads, codes.size(4), as<int32_t>(source), as<int32_t>(target), n, s);
+    });
+  });
+}
+
 #define PTQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PTQ_METHOD(rmsnorm_quantize), PTQ_METHOD(int8_linear), PTQ_METHOD(kv_cache_write), PTQ_METHOD(kv_cache_read),
-                         PTQ_METHOD(paged_attention), {nullptr, nullptr, 0, nullptr}};
+                         PTQ_METHOD(paged_attention), PTQ_METHOD(rotary), PTQ_METHOD(rotary_kv_cache_write), PTQ_METHOD(kv_cache_copy_pages), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tokens", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
