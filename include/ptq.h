@@ -599,6 +599,31 @@ ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_
                                    uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv,
                                    int64_t row_bytes, const int32_t* from, const int32_t* to, int64_t n, ptq_stream stream);
 
+/*
+ * Softmax attention of whole prompts, before their keys and values are quantized (or without a cache: calibration): prompt s is the tokens
+ * cu[s] .. cu[s + 1] of Q, K, V and O.  Token i of a prompt sees its token j if, with causal != 0, j <= i and, with window > 0, j > i - window.
+ * Query head h reads key head h / (hq / hkv):
+ *
+ *   O = sum_j p_j v_j / sum_j p_j,   p_j = exp(softmax_scale q . k_j - max)
+ *
+ * Scores, running maxima and sums are float32; weights are rounded to bfloat16 (2^-8 of each), and the sum is of the rounded ones.  A token that is not
+ * seen has no effect, whatever it holds; one that is seen and is not finite makes what it reaches not finite.  Scores are float32: |softmax_scale
+ * q . k| beyond 1e38 makes the row NaN or leaves keys out.
+ *
+ * Q, K, V, O  token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_BF16.  O may be Q with the same
+ *           strides; otherwise it overlaps none of the others.  K and V whose bases lie on 16 bytes and whose strides are multiples
+ *           of 8 and below 2^24 take the shorter way.
+ * cu        b + 1 int32 on the device.  A prompt that would begin before token 0 or end past t is left out, and so are tokens from max_n of a prompt on.
+ * max_n     no prompt is longer.     b <= 65535; t <= 2^24; max_n hq / hkv <= 2^27.
+ * hq        a multiple of hkv, at most 65535.     d  a multiple of 16, at most 256.
+ * softmax_scale  up to 2e38 either way.     window  >= 0.
+ * No workspace.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE.
+ */
+ptq_status ptq_prompt_attention(const void* Q, int64_t q_token, int64_t q_head, const void* K, int64_t k_token, int64_t k_head,
+                                const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hq, int64_t hkv, int64_t d,
+                                const int32_t* cu, int64_t b, int64_t max_n, double softmax_scale, int causal, int64_t window, void* O,
+                                int64_t o_token, int64_t o_head, ptq_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

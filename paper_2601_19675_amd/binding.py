@@ -115,6 +115,9 @@ def load_library() -> ctypes.CDLL:
                                               c.c_int, vp, c.c_int, vp, vp, vp, i64, i64, vp, i64, i64, vp]
     lib.ptq_kv_cache_copy_pages.restype = c.c_int
     lib.ptq_kv_cache_copy_pages.argtypes = [vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, vp, vp, i64, vp]
+    lib.ptq_prompt_attention.restype = c.c_int
+    lib.ptq_prompt_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, c.c_int, i64, i64, i64, i64, vp, i64, i64, c.c_double, c.c_int,
+                                         i64, vp, i64, i64, vp]
     _LIB = lib
     return lib
 
@@ -547,3 +550,12 @@ def ptq_kv_cache_copy_pages(from_codes: torch.Tensor, from_scales: torch.Tensor,
     rc = (_TOKENS or _tokens()).kv_cache_copy_pages(from_codes, from_scales, from_zeros, source, codes, scales, zeros, target)
     if rc:
         raise PtqError(rc, "ptq_kv_cache_copy_pages")
+
+
+def ptq_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu: torch.Tensor, max_n: int, softmax_scale: float,
+                         O: torch.Tensor, causal: bool = True, window: int = 0) -> None:
+    """O <- attention of whole prompts, Q (bfloat16 t x heads x d) against K and V (t x key heads x d); prompt s is the tokens
+    cu[s] .. cu[s + 1] (int32, on the device), no more than max_n."""
+    rc = (_TOKENS or _tokens()).prompt_attention(Q, K, V, cu, max_n, softmax_scale, O, causal, window)
+    if rc:
+        raise PtqError(rc, "ptq_prompt_attention")

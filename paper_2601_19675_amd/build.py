@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libptq.so")
 PROBE_LIB = os.path.join(HERE, "libptq_probe.so")   # diagnostics for bench.py --mfma-control, not part of the product
 TOKENS_LIB = os.path.join(HERE, "_tokens.so")       # from torch tensors to the calls of the 8-bit attention path
-SOURCES = ["ptq_api.hip", "hessian.hip", "hessian_f32.hip", "cholesky.hip", "quantize.hip", "vq.hip", "layer_error.hip", "lopro.hip", "r1svd.hip", "r1svd_bf16.hip", "artifact.hip", "rmsnorm.hip", "kv_cache.hip", "kv_pages.hip", "rotary.hip", "int8_linear.hip", "paged_attention.hip", "paged_attention_chunk.hip"]
+SOURCES = ["ptq_api.hip", "hessian.hip", "hessian_f32.hip", "cholesky.hip", "quantize.hip", "vq.hip", "layer_error.hip", "lopro.hip", "r1svd.hip", "r1svd_bf16.hip", "artifact.hip", "rmsnorm.hip", "kv_cache.hip", "kv_pages.hip", "rotary.hip", "int8_linear.hip", "paged_attention.hip", "paged_attention_chunk.hip", "prompt_attention.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result",
     # packed-FP32 instructions are kept out of every kernel
@@ -130,6 +130,7 @@ ASSEMBLY_CHECKS = {
     "layer_error.hip": check_lds_dma_wait_states,
     "artifact.hip": check_lds_dma_wait_states,
     "int8_linear.hip": check_lds_dma_wait_states,
+    "prompt_attention.hip": check_lds_dma_wait_states,
 }
 
 

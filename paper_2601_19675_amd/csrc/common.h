@@ -197,4 +197,9 @@ ptq_status kv_cache_copy_pages_launch(const uint8_t* from_codes, const float* fr
                                       uint8_t* codes, float* scales, uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv,
                                       int64_t row_bytes, const int32_t* from, const int32_t* to, int64_t n, hipStream_t s);
 
+ptq_status prompt_attention_launch(const void* Q, int64_t q_token, int64_t q_head, const void* K, int64_t k_token, int64_t k_head,
+                                   const void* V, int64_t v_token, int64_t v_head, int64_t t, int64_t hq, int64_t hkv, int64_t d,
+                                   const int32_t* cu, int64_t b, int64_t max_n, double softmax_scale, int causal, int64_t window, void* O,
+                                   int64_t o_token, int64_t o_head, hipStream_t s);
+
 }  // namespace ptq

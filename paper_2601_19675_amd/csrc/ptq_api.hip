@@ -462,4 +462,21 @@ ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_
                                     to, n, static_cast<hipStream_t>(stream));
 }
 
+ptq_status ptq_prompt_attention(const void* Q, int64_t q_token, int64_t q_head, const void* K, int64_t k_token, int64_t k_head,
+                                const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hq, int64_t hkv, int64_t d,
+                                const int32_t* cu, int64_t b, int64_t max_n, double softmax_scale, int causal, int64_t window, void* O,
+                                int64_t o_token, int64_t o_head, ptq_stream stream) {
+  if (dt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  if (!(std::fabs(softmax_scale) <= 2e38) || window < 0) return PTQ_ERR_ARG;   // (times log2(e) it is a float32)
+  if (hkv <= 0 || hkv > 32767 || d <= 0 || d > 256 || d % 16 != 0) return PTQ_ERR_SHAPE;
+  if (t < 0 || t > (1 << 24) || hq <= 0 || hq > 65535 || hq % hkv != 0 || b < 0 || b > 65535 || max_n < 0 || max_n > t || q_token < 0 || q_head < 0 ||
+      k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0 || o_token < 0 || o_head < 0)
+    return PTQ_ERR_SHAPE;
+  if (max_n * (hq / hkv) > (1 << 27)) return PTQ_ERR_SHAPE;   // a key head's rows, counted in 32 bits
+  if (t == 0 || b == 0 || max_n == 0) return PTQ_OK;
+  if (!Q || !K || !V || !O || !cu || O == K || O == V || (O == Q && (o_token != q_token || o_head != q_head))) return PTQ_ERR_ARG;
+  return prompt_attention_launch(Q, q_token, q_head, K, k_token, k_head, V, v_token, v_head, t, hq, hkv, d, cu, b, max_n, softmax_scale, causal,
+                                 window, O, o_token, o_head, static_cast<hipStream_t>(stream));
+}
+
 }  // extern "C"

@@ -321,9 +321,33 @@ PyObject* kv_cache_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
+// Q, K, V, cu, max_n, softmax_scale, O, causal, window
+PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (!count_is(count, 9)) return nullptr;
+  return status_of([&]() -> ptq_status {
+    const Tensor &Q = tensor(a[0]), &K = tensor(a[1]), &V = tensor(a[2]), &cu = tensor(a[3]), &O = tensor(a[6]);
+    const int64_t max_n = whole(a[4]), window = whole(a[8]);
+    const double scale = number(a[5]);
+    const int causal = truth(a[7]);
+    PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
+    PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && K.scalar_type() == Q.scalar_type() &&
+              V.scalar_type() == Q.scalar_type());
+    PTQ_CHECK(K.size(0) == Q.size(0) && K.size(2) == Q.size(2));
+    PTQ_CHECK(cu.scalar_type() == at::kInt && cu.is_contiguous() && cu.numel() >= 1);
+    ptq_dtype dt;
+    if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
+    const ptq_stream s = stream();
+    return released([&] {
+      return ptq_prompt_attention(ptr(Q), Q.stride(0), Q.stride(1), ptr(K), K.stride(0), K.stride(1), ptr(V), V.stride(0), V.stride(1), dt, Q.size(0),
+                                  Q.size(1), K.size(1), Q.size(2), as<int32_t>(cu), cu.numel() - 1, max_n, scale, causal, window, ptr(O), O.stride(0),
+                                  O.stride(1), s);
+    });
+  });
+}
+
 #define PTQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PTQ_METHOD(rmsnorm_quantize), PTQ_METHOD(int8_linear), PTQ_METHOD(kv_cache_write), PTQ_METHOD(kv_cache_read),
-                         PTQ_METHOD(paged_attention), PTQ_METHOD(rotary), PTQ_METHOD(rotary_kv_cache_write), PTQ_METHOD(kv_cache_copy_pages), {nullptr, nullptr, 0, nullptr}};
+                         PTQ_METHOD(paged_attention), PTQ_METHOD(rotary), PTQ_METHOD(rotary_kv_cache_write), PTQ_METHOD(kv_cache_copy_pages), PTQ_METHOD(prompt_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tokens", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
