@@ -60,7 +60,8 @@ typedef enum {
   PTQ_OP_SCALED_R1SVD = 7,
   PTQ_OP_LINEAR_FORWARD = 8, /* t = tokens, block = rank r */
   PTQ_OP_INT8_LINEAR = 10,    /* t = tokens (9 is no operation) */
-  PTQ_OP_PAGED_ATTENTION = 11 /* m = query heads, n = d, t = tokens, block = max_kv */
+  PTQ_OP_PAGED_ATTENTION = 11, /* m = query heads, n = d, t = tokens, block = max_kv */
+  PTQ_OP_SHARED_ATTENTION = 12 /* the same */
 } ptq_op;
 
 typedef void* ptq_stream; /* hipStream_t */
@@ -623,6 +624,27 @@ ptq_status ptq_prompt_attention(const void* Q, int64_t q_token, int64_t q_head, 
                                 const void* V, int64_t v_token, int64_t v_head, ptq_dtype dt, int64_t t, int64_t hq, int64_t hkv, int64_t d,
                                 const int32_t* cu, int64_t b, int64_t max_n, double softmax_scale, int causal, int64_t window, void* O,
                                 int64_t o_token, int64_t o_head, ptq_stream stream);
+
+/*
+ * ptq_paged_attention for sequences that share prefixes (forks of a sequence, requests behind one long text): the keys of a prefix are read and
+ * multiplied once for all queries behind it.  The result is ptq_paged_attention's with the same arguments and window 0, but for how it is rounded: a
+ * prefix is gone through as chunks are, with their roundings, where more than one sequence has it and no key head has more than 16 rows (tokens
+ * times group) of a sequence; otherwise the call does what ptq_paged_attention does.
+ *
+ * cu_groups  groups + 1 int32 on the device, never falling: sequences cu_groups[j] .. cu_groups[j + 1] share a prefix.  Sequences of no group, and groups
+ *            that begin before sequence 0 or end past b, share nothing.
+ * shared     groups int32 on the device: a prefix's keys.  The sequences' tables name the same pages for them, or pages that hold the same; the first
+ *            sequence's are read.  Whole blocks of 64 keys are shared, each sequence reads the rest of a prefix for itself.
+ * max_shared no prefix is longer (keys from there on are each sequence's own).     groups <= 65535; t hq / hkv <= 2^27.
+ * Workspace: PTQ_OP_SHARED_ATTENTION with m = hq, n = d, t and block = max_kv.  Results do not depend on what it holds.
+ * Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE, PTQ_ERR_WORKSPACE.
+ */
+ptq_status ptq_paged_attention_shared(const void* Q, ptq_dtype qdt, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                                      const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                                      const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits, const int32_t* table,
+                                      int64_t ldt, const int32_t* kv_lens, int64_t max_kv, const int32_t* cu_groups, const int32_t* shared,
+                                      int64_t groups, int64_t max_shared, double softmax_scale, int causal, void* O, int64_t o_token,
+                                      int64_t o_head, void* ws, size_t ws_bytes, ptq_stream stream);
 
 #ifdef __cplusplus
 }

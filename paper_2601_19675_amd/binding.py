@@ -20,7 +20,7 @@ PTQ_F32, PTQ_BF16, PTQ_F64 = 0, 1, 2
 OP_HESSIAN, OP_CHOLESKY_INV, OP_QUANTIZE, OP_LAYER_ERROR = 0, 1, 2, 3
 OP_LOPRO_ORDER, OP_LOPRO_ROTATE_HESSIAN = 4, 5
 OP_ACTIVATION_ABS_SUM, OP_SCALED_R1SVD, OP_LINEAR_FORWARD = 6, 7, 8
-OP_INT8_LINEAR, OP_PAGED_ATTENTION = 10, 11
+OP_INT8_LINEAR, OP_PAGED_ATTENTION, OP_SHARED_ATTENTION = 10, 11, 12
 PTQ_ROTARY_PLAIN, PTQ_ROTARY_LINEAR, PTQ_ROTARY_BASE, PTQ_ROTARY_TURNS = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -118,6 +118,9 @@ def load_library() -> ctypes.CDLL:
     lib.ptq_prompt_attention.restype = c.c_int
     lib.ptq_prompt_attention.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, i64, c.c_int, i64, i64, i64, i64, vp, i64, i64, c.c_double, c.c_int,
                                          i64, vp, i64, i64, vp]
+    lib.ptq_paged_attention_shared.restype = c.c_int
+    lib.ptq_paged_attention_shared.argtypes = [vp, c.c_int, i64, i64, i64, i64, i64, vp, i64, i64, vp, vp, vp, i64, i64, i64, c.c_int, vp, i64, vp,
+                                               i64, vp, vp, i64, i64, c.c_double, c.c_int, vp, i64, i64, vp, sz, vp]
     _LIB = lib
     return lib
 
@@ -559,3 +562,14 @@ def ptq_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, cu: 
     rc = (_TOKENS or _tokens()).prompt_attention(Q, K, V, cu, max_n, softmax_scale, O, causal, window)
     if rc:
         raise PtqError(rc, "ptq_prompt_attention")
+
+
+def ptq_paged_attention_shared(Q: torch.Tensor, cu_q: torch.Tensor, max_q: int, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor,
+                               bits: int, table: torch.Tensor, kv_lens: torch.Tensor, max_kv: int, cu_groups: torch.Tensor, shared: torch.Tensor,
+                               max_shared: int, softmax_scale: float, O: torch.Tensor, causal: bool = True, ws: torch.Tensor | None = None) -> None:
+    """ptq_paged_attention of sequences that share prefixes: sequences cu_groups[j] .. cu_groups[j + 1] (int32, on the device) have their first
+    shared[j] keys (int32, on the device, no more than max_shared) in common."""
+    rc = (_TOKENS or _tokens()).paged_attention_shared(Q, cu_q, max_q, codes, scales, zeros, bits, table, kv_lens, max_kv, cu_groups, shared, max_shared,
+                                                       softmax_scale, O, causal, ws)
+    if rc:
+        raise PtqError(rc, "ptq_paged_attention_shared")

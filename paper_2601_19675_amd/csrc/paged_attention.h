@@ -33,6 +33,12 @@ struct AttendArgs {
   float* part;                           // [...][d]: the mean of the part's values
   float* ml;                             // [...][2]: a maximum, the sum of the weights relative to it
   int* parts;                            // rows form: [token], how many there are; chunk form: [share][4], see there
+  // of sequences that share prefixes (see shared_of): the chunk form goes through the prefixes, a group of sequences in a sequence's place, the rows form
+  // through what is behind them
+  const int32_t *cu_groups, *shared;
+  int groups, max_shared;
+  float *alone, *alone_ml;               // [token][head][d] and [2]: parts of tiles of rows that a share has all of
+  int2* where;                           // [token][head]: the row of part and ml that has the first part (-1: alone has it), and how many there are
 };
 
 // a sequence's queries and keys
@@ -61,6 +67,36 @@ __device__ __forceinline__ void visible(const AttendArgs& a, const Sequence& q, 
   const int place = q.place + i;
   hi = a.causal ? max(0, min(q.length, place + 1)) : q.length;
   lo = a.window > 0 ? max(0, place - a.window + 1) : 0;
+}
+
+// Sequences cu_groups[j] .. cu_groups[j + 1] have the first shared[j] keys in common, and their queries lie side by side: all of them, seen as
+// one sequence of `length` keys.  It is that many whole blocks of 64; the keys from there on are each sequence's own.  No queries where nothing is shared.
+__device__ __forceinline__ Sequence group_of(const AttendArgs& a, int j) {
+  Sequence q{0, 0, 0, 0, 0, 0};
+  const int from = a.cu_groups[j], to = a.cu_groups[j + 1];
+  if (from < 0 || to > a.b || to - (int64_t)from < 2) return q;
+  const int64_t first = a.cu_q[from], last = a.cu_q[to], most = min((int64_t)min(a.max_shared, a.max_kv), a.ldt << a.c.page_shift);
+  q.length = (int)min((int64_t)max(0, a.shared[j]), most) & ~63;
+  q.first = (int)first;
+  q.queries = first >= 0 && last <= a.t && last > first && q.length > 0 ? (int)(last - first) : 0;
+  q.end = q.length;
+  return q;
+}
+// the last i in [from, to) with at[i] <= x, or from
+__device__ __forceinline__ int last_not_above(const int32_t* at, int from, int to, int x) {
+  for (int n = to - from; n > 1;) {
+    const int half = n >> 1;
+    if (at[from + half] <= x) from += half;
+    n -= half;
+  }
+  return from;
+}
+// how many keys of a sequence its group has in common
+__device__ __forceinline__ int shared_of(const AttendArgs& a, int s) {
+  const int j = last_not_above(a.cu_groups, 0, a.groups, s);
+  if (s < a.cu_groups[j] || s >= a.cu_groups[j + 1]) return 0;
+  const Sequence g = group_of(a, j);
+  return g.queries > 0 ? g.length : 0;
 }
 
 __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel) { return __builtin_amdgcn_perm(hi, lo, sel); }
@@ -122,5 +158,8 @@ constexpr int kSharedChunkKeys = 2048;                 // shorter contexts are n
 struct ChunkItems { int64_t tiles, busy; };
 ChunkItems paged_attention_chunk_items(const AttendArgs& a);
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s);
+// the prefixes that groups share, in shares; parts are left in part, ml, alone, alone_ml and where
+int64_t paged_attention_prefix_tiles(const AttendArgs& a);   // tiles of rows of all groups, at most
+ptq_status paged_attention_prefix_launch(const AttendArgs& a, int bits, hipStream_t s);
 
 }  // namespace ptq

@@ -43,6 +43,13 @@ constexpr int kFarExponent = 40;   // of a value's scale that the sum of the wei
 __device__ __forceinline__ int share_blocks(const AttendArgs& a, const Sequence& q) {
   return q.queries == 0 ? 0 : max(1, (q.end - q.begin + kShareBlock - 1) / kShareBlock);
 }
+// a sequence, of one that shares a prefix what is behind it
+template <bool SHARED>
+__device__ __forceinline__ Sequence own_of(const AttendArgs& a, int s) {
+  Sequence q = sequence_of(a, s);
+  if constexpr (SHARED) q.begin = min(max(q.begin, shared_of(a, s)), q.end);
+  return q;
+}
 struct __attribute__((packed, aligned(4))) Four { float e[4]; };
 // 2^-e, by its bits: those of 1, and -2^23 times e (which the compiler makes two instructions)
 __device__ __forceinline__ float power_below(int e) {
@@ -71,7 +78,7 @@ __device__ __forceinline__ f16x8 key_codes(const uint32_t* w) {
 
 // HALVES: pages of 16 tokens and more, so that each half of a block lies in one page, whose number is the wave's (addresses are scalar
 // work); WHOLE: d == DP
-template <int BITS, int DP, bool HALVES, bool WHOLE>
+template <int BITS, int DP, bool HALVES, bool WHOLE, bool SHARED>
 __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   using S = Shape<BITS, DP>;
   constexpr int kSteps = DP / 32;      // matrix instructions to a score
@@ -87,7 +94,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
   int before = 0, share = 1, left = INT32_MAX;
   if (a.splits > 1) {
     int total = 0;
-    for (int s0 = 0; s0 < a.b; s0 += kWave) total += s0 + lane < a.b ? share_blocks(a, sequence_of(a, s0 + lane)) : 0;
+    for (int s0 = 0; s0 < a.b; s0 += kWave) total += s0 + lane < a.b ? share_blocks(a, own_of<SHARED>(a, s0 + lane)) : 0;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o);
     total = __builtin_amdgcn_readfirstlane(total);
@@ -96,7 +103,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
     if (mine >= total) return;
     left = min(share, total - (int)mine);
     for (int s0 = 0;; s0 += kWave) {   // the first sequence that reaches past `mine`
-      const int n = s0 + lane < a.b ? share_blocks(a, sequence_of(a, s0 + lane)) : 0;
+      const int n = s0 + lane < a.b ? share_blocks(a, own_of<SHARED>(a, s0 + lane)) : 0;
       int upto = n;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
@@ -117,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
 
   for (;; ++seq) {
   if (seq >= a.b) return;
-  const Sequence q = sequence_of(a, seq);
+  const Sequence q = own_of<SHARED>(a, seq);
   const int queries = min(q.queries, a.max_q), rows = queries * a.group;
   if (rows == 0) {
     if (a.splits == 1) return;
@@ -475,7 +482,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
       for (int j = 0; j < 4; ++j) o[j] *= inv;
     }
     const int tok = q.first + row / a.group, h = head * a.group + row % a.group;
-    if (!alone) {
+    if (SHARED || !alone) {
       const int64_t at = ((int64_t)part * a.t + tok) * a.hq + h;
       *reinterpret_cast<f32x4*>(a.part + at * a.d + c) = f32x4{o[0], o[1], o[2], o[3]};
       if (c == 0) {
@@ -545,6 +552,58 @@ __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
   store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, v);
 }
 
+// Joins the parts of a (token, head) that shares a prefix: those of the prefix, then those of what is behind it.  As above.
+__global__ __launch_bounds__(64) void shared_join_kernel(AttendArgs pre, AttendArgs a) {
+  const int tok = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, c = lane * 4;
+  const int seq = last_not_above(a.cu_q, 0, a.b, tok);
+  const Sequence q = sequence_of(a, seq);
+  if (tok < q.first || tok - q.first >= min(q.queries, a.max_q)) return;
+  const int64_t first = (int64_t)tok * a.hq + h, step = (int64_t)a.t * a.hq;
+  int2 where = shared_of(a, seq) > 0 ? pre.where[first] : int2{0, 0};
+  // (where sequences do not lie one after the other, nobody may have written it: whatever it holds, what is read is part of the workspace)
+  const int most = 2 * kChunkShares * pre.slot_rows;
+  where = int2{min(max(where.x, -1), most - 1), min(max(where.y, 0), kChunkShares)};
+  const int of_prefix = where.y, parts = of_prefix + (a.splits > 1 ? a.parts[tok] : 1);
+  // the row of part p, and whose
+  auto row_of = [&](int p) { return p >= of_prefix ? first + (p - of_prefix) * step : where.x < 0 ? first : (int64_t)min(where.x + (p > 0 ? 2 * p - 1 : 0) * pre.slot_rows, most - 1); };
+  auto ml_of = [&](int p) {
+    return *reinterpret_cast<const f32x2*>((p >= of_prefix ? a.ml : where.x < 0 ? pre.alone_ml : pre.ml) + 2 * row_of(p));
+  };
+  const int cc = c < a.d ? c : 0;
+  auto part_of = [&](int p) {
+    return *reinterpret_cast<const f32x4*>((p >= of_prefix ? a.part : where.x < 0 ? pre.alone : pre.part) + row_of(p) * a.d + cc);
+  };
+  float top = kNoScore, sum = 0.f;
+  for (int s = lane; s < parts; s += 64) top = fmaxf(top, ml_of(s)[0]);
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < parts; s0 += 64) {
+    const int s = min(s0 + lane, parts - 1);
+    const f32x2 ml = ml_of(s);
+    float f = s0 + lane < parts ? exp2_fast(ml[0] - top) * ml[1] : 0.f;
+    float all = f;
+#pragma unroll
+    for (int n = 1; n < kWave; n <<= 1) all += __shfl_xor(all, n);
+    all += sum;
+    const float inv = all == 0.f ? 0.f : 1.f / all;   // a row that sees nothing: zeros
+    o *= sum * inv;
+    f *= inv;
+    sum = all;
+    const int here = min(64, parts - s0);
+    for (int i = 0; i < here; i += 8) {   // (f is 0 past the last part)
+      f32x4 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = part_of(s0 + min(i + j, here - 1));
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o += __shfl(f, i + j) * v[j];
+    }
+  }
+  if (c >= a.d) return;
+  const float v[4] = {o[0], o[1], o[2], o[3]};
+  store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, v);
+}
+
 constexpr int64_t kPartRows = 65536;   // rows times splits at most: what the workspace holds
 
 int64_t most_splits(int64_t rows, int64_t max_kv) {
@@ -555,18 +614,23 @@ constexpr int64_t kLongKeys = 4096, kMostSharedTiles = 4096;
 constexpr int kShares = 512;          // workgroups that share the contexts: two to a compute unit
 int64_t shares(int64_t hkv) { return std::max<int64_t>(1, kShares / hkv); }
 
-template <int BITS, int DP, bool HALVES, bool WHOLE>
+template <int BITS, int DP, bool HALVES, bool WHOLE, bool SHARED>
 bool rows_form_launch(const AttendArgs& a, hipStream_t s) {
   constexpr int kBytes = kWaves * kRows * (DP + 4 + 4) * (int)sizeof(float);
-  if (!lds_opt_in<attend_rows_kernel<BITS, DP, HALVES, WHOLE>>(kBytes)) return false;
+  if (!lds_opt_in<attend_rows_kernel<BITS, DP, HALVES, WHOLE, SHARED>>(kBytes)) return false;
   const dim3 grid = a.splits > 1 ? dim3((unsigned)shares(a.c.heads), (unsigned)a.c.heads, 1) : dim3(1, (unsigned)a.c.heads, (unsigned)a.b);
-  attend_rows_kernel<BITS, DP, HALVES, WHOLE><<<grid, kWaves * 64, kBytes, s>>>(a);
+  attend_rows_kernel<BITS, DP, HALVES, WHOLE, SHARED><<<grid, kWaves * 64, kBytes, s>>>(a);
   return true;
 }
-template <int BITS, int DP>
+template <int BITS, int DP, bool SHARED>
 bool rows_launch(const AttendArgs& a, hipStream_t s) {
-  if (a.c.page_shift < 4) return rows_form_launch<BITS, DP, false, false>(a, s);
-  return a.d == DP ? rows_form_launch<BITS, DP, true, true>(a, s) : rows_form_launch<BITS, DP, true, false>(a, s);
+  if (a.c.page_shift < 4) return rows_form_launch<BITS, DP, false, false, SHARED>(a, s);
+  return a.d == DP ? rows_form_launch<BITS, DP, true, true, SHARED>(a, s) : rows_form_launch<BITS, DP, true, false, SHARED>(a, s);
+}
+template <bool SHARED>
+bool rows_launch_any(const AttendArgs& a, int bits, hipStream_t s) {
+  return bits == 8 ? (a.d <= 64 ? rows_launch<8, 64, SHARED>(a, s) : a.d <= 128 ? rows_launch<8, 128, SHARED>(a, s) : rows_launch<8, 256, SHARED>(a, s))
+                   : (a.d <= 64 ? rows_launch<4, 64, SHARED>(a, s) : a.d <= 128 ? rows_launch<4, 128, SHARED>(a, s) : rows_launch<4, 256, SHARED>(a, s));
 }
 
 }  // namespace
@@ -579,12 +643,11 @@ size_t paged_attention_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t
   return align_up((size_t)std::max(rows_form, chunk_form) * sizeof(float), 256);
 }
 
-ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
-                                  const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
-                                  const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits,
-                                  const int32_t* table, int64_t ldt, const int32_t* kv_lens, int64_t max_kv,
-                                  double softmax_scale, int causal, int64_t window, void* O, int64_t o_token, int64_t o_head,
-                                  void* ws, hipStream_t s) {
+namespace {
+AttendArgs attend_args(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d, const int32_t* cu_q, int64_t b,
+                       int64_t max_q, const uint8_t* codes, const float* scales, const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv,
+                       int bits, const int32_t* table, int64_t ldt, const int32_t* kv_lens, int64_t max_kv, double softmax_scale, int causal,
+                       int64_t window, void* O, int64_t o_token, int64_t o_head) {
   AttendArgs a{};
   a.Q = static_cast<const uint16_t*>(Q);
   a.O = static_cast<uint16_t*>(O);
@@ -595,6 +658,18 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
   a.scale = (float)(softmax_scale * 1.4426950408889634);
   a.t = (int)t, a.b = (int)b, a.hq = (int)hq, a.group = (int)(hq / hkv), a.d = (int)d, a.max_q = (int)max_q, a.max_kv = (int)max_kv;
   a.causal = causal, a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
+  return a;
+}
+}  // namespace
+
+ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                                  const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                                  const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits,
+                                  const int32_t* table, int64_t ldt, const int32_t* kv_lens, int64_t max_kv,
+                                  double softmax_scale, int causal, int64_t window, void* O, int64_t o_token, int64_t o_head,
+                                  void* ws, hipStream_t s) {
+  AttendArgs a = attend_args(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt, kv_lens, max_kv,
+                             softmax_scale, causal, window, O, o_token, o_head);
   const bool rows_form = max_q * a.group <= kRows;
   // the keys a split has to get through: those in the window, if there is one
   const int64_t keys = window > 0 ? std::min<int64_t>(max_kv, (int64_t)a.window + max_q + 63) : max_kv;
@@ -625,14 +700,69 @@ ptq_status paged_attention_launch(const void* Q, int64_t q_token, int64_t q_head
   a.ml = a.part + part_rows * d;
   a.parts = reinterpret_cast<int*>(a.ml + part_rows * 2);
   if (rows_form) {
-    const bool launched = bits == 8 ? (d <= 64 ? rows_launch<8, 64>(a, s) : d <= 128 ? rows_launch<8, 128>(a, s) : rows_launch<8, 256>(a, s))
-                                    : (d <= 64 ? rows_launch<4, 64>(a, s) : d <= 128 ? rows_launch<4, 128>(a, s) : rows_launch<4, 256>(a, s));
-    if (!launched) return PTQ_ERR_HIP;
+    if (!rows_launch_any<false>(a, bits, s)) return PTQ_ERR_HIP;
   } else {
     const ptq_status rc = paged_attention_chunk_launch(a, bits, s);
     if (rc != PTQ_OK) return rc;
   }
   if (rows_form && a.splits > 1) attend_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(a);
+  PTQ_HIP_CHECK_LAUNCH();
+  return PTQ_OK;
+}
+
+// parts of what is behind the prefixes, of the prefixes (shares', and tiles of rows that a share has alone), what begins in a share, the parts'
+// maxima and sums, where a row's first part is, how many a token has; or what the call without prefixes needs
+namespace {
+struct SharedPlan { int64_t splits, own_rows, prefix_rows, slot_rows, floats; };
+SharedPlan shared_plan(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
+  SharedPlan p;
+  const int64_t rows = hq * t;
+  p.splits = most_splits(rows, max_kv);
+  p.own_rows = p.splits * rows;
+  p.slot_rows = std::min<int64_t>(kChunkRows, rows);
+  p.prefix_rows = 2 * kChunkShares * p.slot_rows;
+  p.floats = (p.own_rows + p.prefix_rows + rows) * (d + 2) + 2 * rows + t + 4 * kChunkShares;
+  return p;
+}
+}  // namespace
+size_t paged_attention_shared_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
+  return std::max(align_up((size_t)shared_plan(hq, d, t, max_kv).floats * sizeof(float), 256), paged_attention_workspace_bytes(hq, d, t, max_kv));
+}
+
+ptq_status paged_attention_shared_launch(const void* Q, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                                         const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                                         const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits, const int32_t* table,
+                                         int64_t ldt, const int32_t* kv_lens, int64_t max_kv, const int32_t* cu_groups, const int32_t* shared,
+                                         int64_t groups, int64_t max_shared, double softmax_scale, int causal, void* O, int64_t o_token,
+                                         int64_t o_head, void* ws, hipStream_t s) {
+  AttendArgs a = attend_args(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt, kv_lens, max_kv,
+                             softmax_scale, causal, 0, O, o_token, o_head);
+  a.cu_groups = cu_groups, a.shared = shared, a.groups = (int)groups, a.max_shared = (int)std::min(max_shared, max_kv);
+  // Chunks of tokens are bound by their products, which are no fewer with a prefix in common, and prefixes of less than a block are not gone
+  // through apart.
+  if (max_q * a.group > kRows || a.max_shared < 64 || groups == 0 || paged_attention_prefix_tiles(a) > kMostSharedTiles)
+    return paged_attention_launch(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt, kv_lens,
+                                  max_kv, softmax_scale, causal, 0, O, o_token, o_head, ws, s);
+  const SharedPlan p = shared_plan(hq, d, t, max_kv);
+  const int64_t rows = hq * t;
+  AttendArgs pre = a;
+  a.part = static_cast<float*>(ws);
+  pre.part = a.part + p.own_rows * d;
+  pre.alone = pre.part + p.prefix_rows * d;
+  pre.parts = reinterpret_cast<int*>(pre.alone + rows * d);
+  a.ml = pre.alone + rows * d + 4 * kChunkShares;
+  pre.ml = a.ml + 2 * p.own_rows;
+  pre.alone_ml = pre.ml + 2 * p.prefix_rows;
+  pre.where = reinterpret_cast<int2*>(pre.alone_ml + 2 * rows);
+  a.parts = reinterpret_cast<int*>(pre.where + rows);
+  pre.splits = 2;
+  pre.slot_rows = (int)p.slot_rows;
+  a.splits = max_kv < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)p.splits;
+  a.least_share = a.splits > 1 ? (int)std::max<int64_t>(2, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
+  const ptq_status rc = paged_attention_prefix_launch(pre, bits, s);
+  if (rc != PTQ_OK) return rc;
+  if (!rows_launch_any<true>(a, bits, s)) return PTQ_ERR_HIP;
+  shared_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(pre, a);
   PTQ_HIP_CHECK_LAUNCH();
   return PTQ_OK;
 }

@@ -87,9 +87,25 @@ struct Meta {
   int odd;                // whether an x is not 0
 };
 
+// A tile of rows is of a sequence, or of a group of sequences and the prefix that they share (SHARED), whose rows all see it but for what each
+// row's own place leaves out.
+template <bool SHARED>
+__device__ __forceinline__ Sequence item_of(const AttendArgs& a, int seq) {
+  if constexpr (SHARED) return group_of(a, seq);
+  else return sequence_of(a, seq);
+}
+template <bool SHARED>
+__device__ __forceinline__ int rows_of(const AttendArgs& a, const Sequence& q) {
+  return (SHARED ? q.queries : min(q.queries, a.max_q)) * a.group;
+}
 // the keys that some row of a tile of rows sees
-template <int ROWS>
+template <int ROWS, bool SHARED>
 __device__ __forceinline__ void span_of(const AttendArgs& a, const Sequence& q, int tile, int& begin, int& end) {
+  if constexpr (SHARED) {
+    begin = 0;
+    end = q.end;
+    return;
+  }
   const int rows = min(q.queries, a.max_q) * a.group;
   int unused;
   visible(a, q, tile * ROWS / a.group, begin, unused);
@@ -98,16 +114,16 @@ __device__ __forceinline__ void span_of(const AttendArgs& a, const Sequence& q, 
   end = min(end, q.end);
 }
 // what a tile of rows counts for
-template <int ROWS>
+template <int ROWS, bool SHARED>
 __device__ __forceinline__ int item_work(const AttendArgs& a, int seq, int tile) {
-  const Sequence q = sequence_of(a, seq);
-  if (tile * ROWS >= min(q.queries, a.max_q) * a.group) return 0;
+  const Sequence q = item_of<SHARED>(a, seq);
+  if (tile * ROWS >= rows_of<SHARED>(a, q)) return 0;
   int begin, end;
-  span_of<ROWS>(a, q, tile, begin, end);
+  span_of<ROWS, SHARED>(a, q, tile, begin, end);
   return kStart + max(0, end - begin + kTile - 1) / kTile;
 }
 
-template <int BITS, int DP>
+template <int BITS, int DP, bool SHARED>
 __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(AttendArgs a, int tiles, int first_group) {
   using C = Chunk<DP>;
   constexpr int kSteps = DP / 16, kOut = DP / 32;
@@ -121,9 +137,9 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   int4* const begun_at = reinterpret_cast<int4*>(a.parts) + (blockIdx.x & 7) * (kShares / 8) + (blockIdx.x >> 3);
   if (a.splits > 1) {
     // consecutive shares on one die, where they find each other's codes in the L2
-    const int pairs = a.b * tiles, lane = threadIdx.x & 63;
+    const int sequences = SHARED ? a.groups : a.b, pairs = sequences * tiles, lane = threadIdx.x & 63;
     int total = 0;   // of one key head
-    for (int p0 = 0; p0 < pairs; p0 += kWave) total += p0 + lane < pairs ? item_work<C::kRows>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+    for (int p0 = 0; p0 < pairs; p0 += kWave) total += p0 + lane < pairs ? item_work<C::kRows, SHARED>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o);
     total = __builtin_amdgcn_readfirstlane(total);
@@ -139,7 +155,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     const int within = (int)mine % total;
     int before = 0;
     for (int p0 = 0;; p0 += kWave) {   // the first item that reaches past `within`
-      const int n = p0 + lane < pairs ? item_work<C::kRows>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+      const int n = p0 + lane < pairs ? item_work<C::kRows, SHARED>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
       int upto = n;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
@@ -169,12 +185,12 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   for (;;) {
   // (opaque: what follows from it is not kept in registers from one item to the next)
   const int tid = opaque(threadIdx.x), lane = tid & 63, r = lane & 31, h = lane >> 5;
-  const Sequence q = sequence_of(a, seq);
-  const int rows = min(q.queries, a.max_q) * a.group, row0 = tile * C::kRows;
+  const Sequence q = item_of<SHARED>(a, seq);
+  const int rows = rows_of<SHARED>(a, q), row0 = tile * C::kRows;
   if (row0 >= rows) {   // (a share has something to do yet)
     if (a.splits == 1) return;
     tile = 0;
-    if (++seq == a.b) {
+    if (++seq == (SHARED ? a.groups : a.b)) {
       seq = 0;
       ++head;
     }
@@ -183,7 +199,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
 
   // the keys that some row of the workgroup sees, and those of them in this share
   int lo, hi, lo_a, hi_a, lo_b, hi_b, begin, end;
-  span_of<C::kRows>(a, q, tile, begin, end);
+  span_of<C::kRows, SHARED>(a, q, tile, begin, end);
   const int whole = kStart + max(0, end - begin + kTile - 1) / kTile, take = min(whole - off, left);
   const bool alone = take == whole;
   end = min(end, begin + max(0, off + take - kStart) * kTile);
@@ -192,14 +208,14 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   // ... and those that the wave's rows see: some of them [lo_a, hi_b), all of them [lo_b, hi_a)
   const int wrow = row0 + 32 * wave;
   const bool working = wrow < rows;
-  if (working) {
+  if (working && !SHARED) {
     visible(a, q, wrow / a.group, lo_a, hi_a);
     visible(a, q, (min(wrow + 32, rows) - 1) / a.group, lo_b, hi_b);
   }
 
   const int64_t plane = (a.c.pages * a.c.heads) << a.c.page_shift;
   const uint8_t* VC = a.c.codes + plane * a.c.row_bytes;
-  const int32_t* table = a.table + seq * a.ldt;
+  const int32_t* table = a.table + (SHARED ? a.cu_groups[seq] : seq) * a.ldt;
   const int inside = (1 << a.c.page_shift) - 1;
 
   // ---- what comes before the codes: a wave's tiles are every kWaves-th, a lane per key, so that it has that many tiles' time for its
@@ -240,8 +256,26 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   };
 
   const int row = wrow + r, token = q.first + row / a.group, qhead = head * a.group + row % a.group;
-  const bool live = row < rows;
-  visible(a, q, live ? row / a.group : 0, lo, hi);
+  bool live = row < rows;
+  if constexpr (SHARED) {
+    // the row's own sequence says what of the prefix it sees
+    lo = 0, hi = 0;
+    if (live) {
+      const int own = last_not_above(a.cu_q, a.cu_groups[seq], a.cu_groups[seq + 1], token);
+      const Sequence o = sequence_of(a, own);
+      int unused;
+      visible(a, o, token - o.first, unused, hi);
+      hi = min(hi, q.length);
+      live = token >= o.first && token - o.first < min(o.queries, a.max_q);
+    }
+    lo_b = 0;
+    hi_a = live ? hi : INT32_MAX;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) hi_a = min(hi_a, __shfl_xor(hi_a, o));
+    hi_a = __builtin_amdgcn_readfirstlane(hi_a);
+  } else {
+    visible(a, q, live ? row / a.group : 0, lo, hi);
+  }
   if (!live) hi = 0;
   constexpr int kHeld = kSteps - C::kQuerySteps;   // steps of d of the queries in registers
   f16x8 fq[kHeld];
@@ -670,19 +704,29 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     auto output = [&](int n, int j) {
       return f32x4{acc[n][4 * j] * inv * rest, acc[n][4 * j + 1] * inv * rest, acc[n][4 * j + 2] * inv * rest, acc[n][4 * j + 3] * inv * rest};
     };
-    if (!alone) {
+    if (SHARED || !alone) {
       // (an item that begins here is the share's last, one that began before is its first)
-      const int64_t slot_row = (int64_t)(2 * ((at + off) / each) + (off == 0)) * a.slot_rows + (row - row0);
+      int64_t slot_row = (int64_t)(2 * ((at + off) / each) + (off == 0)) * a.slot_rows + (row - row0);
+      float *part = a.part, *ml = a.ml;
+      if constexpr (SHARED) {
+        const int64_t mine = (int64_t)token * a.hq + qhead;
+        if (off == 0 && h == 0) a.where[mine] = int2{alone ? -1 : (int)slot_row, (at + whole - 1) / each - at / each + 1};
+        if (alone) {
+          slot_row = mine;
+          part = a.alone;
+          ml = a.alone_ml;
+        }
+      }
       if (h == 0) {
-        a.ml[2 * slot_row] = of;
-        a.ml[2 * slot_row + 1] = l;
+        ml[2 * slot_row] = of;
+        ml[2 * slot_row + 1] = l;
       }
 #pragma unroll
       for (int n = 0; n < kOut; ++n)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int d = 32 * n + 8 * j + 4 * h;
-          if (d < a.d) *reinterpret_cast<f32x4*>(a.part + slot_row * a.d + d) = output(n, j);
+          if (d < a.d) *reinterpret_cast<f32x4*>(part + slot_row * a.d + d) = output(n, j);
         }
     } else {
       uint16_t* O = a.O + token * a.o_token + qhead * a.o_head;
@@ -763,21 +807,42 @@ template <int BITS, int DP>
 bool chunk_launch(const AttendArgs& a, hipStream_t s) {
   using C = Chunk<DP>;
   constexpr int kBytes = C::kBuffers + C::kQueryBytes + C::kApartBytes + kMetas * (int)sizeof(Meta);
-  if (!lds_opt_in<attend_chunk_kernel<BITS, DP>>(kBytes)) return false;
+  if (!lds_opt_in<attend_chunk_kernel<BITS, DP, false>>(kBytes)) return false;
   const int tiles = (int)ceil_div((int64_t)a.max_q * a.group, C::kRows);
   if (a.splits > 1) {
-    attend_chunk_kernel<BITS, DP><<<kShares, C::kThreads, kBytes, s>>>(a, tiles, 0);
+    attend_chunk_kernel<BITS, DP, false><<<kShares, C::kThreads, kBytes, s>>>(a, tiles, 0);
     join_chunk_kernel<DP><<<dim3(kShares, C::kRows * (DP / 4) / 256), 256, 0, s>>>(a);
     return true;
   }
   // A launch has fewer than 2^32 threads; eight groups of up to 2^27 rows, two threads to a row, fit one.
   const int64_t eights = ceil_div((int64_t)a.b * a.c.heads, 8), step = std::max<int64_t>(1, (1 << 19) / tiles);
   for (int64_t first = 0; first < eights; first += step)
-    attend_chunk_kernel<BITS, DP><<<(unsigned)(std::min(step, eights - first) * 8 * tiles), C::kThreads, kBytes, s>>>(a, tiles, (int)(8 * first));
+    attend_chunk_kernel<BITS, DP, false><<<(unsigned)(std::min(step, eights - first) * 8 * tiles), C::kThreads, kBytes, s>>>(a, tiles, (int)(8 * first));
+  return true;
+}
+
+template <int BITS, int DP>
+bool prefix_launch(const AttendArgs& a, hipStream_t s) {
+  using C = Chunk<DP>;
+  constexpr int kBytes = C::kBuffers + C::kQueryBytes + C::kApartBytes + kMetas * (int)sizeof(Meta);
+  if (!lds_opt_in<attend_chunk_kernel<BITS, DP, true>>(kBytes)) return false;
+  attend_chunk_kernel<BITS, DP, true><<<kShares, C::kThreads, kBytes, s>>>(a, (int)ceil_div((int64_t)a.t * a.group, C::kRows), 0);
   return true;
 }
 
 }  // namespace
+
+int64_t paged_attention_prefix_tiles(const AttendArgs& a) {
+  return (int64_t)a.groups * ceil_div((int64_t)a.t * a.group, a.d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows);
+}
+
+ptq_status paged_attention_prefix_launch(const AttendArgs& a, int bits, hipStream_t s) {
+  const bool launched = bits == 8 ? (a.d <= 64 ? prefix_launch<8, 64>(a, s) : a.d <= 96 ? prefix_launch<8, 96>(a, s)
+                                     : a.d <= 128 ? prefix_launch<8, 128>(a, s) : prefix_launch<8, 256>(a, s))
+                                  : (a.d <= 64 ? prefix_launch<4, 64>(a, s) : a.d <= 96 ? prefix_launch<4, 96>(a, s)
+                                     : a.d <= 128 ? prefix_launch<4, 128>(a, s) : prefix_launch<4, 256>(a, s));
+  return launched ? PTQ_OK : PTQ_ERR_HIP;
+}
 
 ChunkItems paged_attention_chunk_items(const AttendArgs& a) {
   const int64_t rows = a.d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows;

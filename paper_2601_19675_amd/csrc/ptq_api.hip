@@ -56,6 +56,7 @@ ptq_status ptq_workspace_bytes(ptq_op op, int64_t m, int64_t n, int64_t t, int64
     case PTQ_OP_LINEAR_FORWARD: *bytes = linear_forward_workspace_bytes(t, m, n, block); return PTQ_OK;
     case PTQ_OP_INT8_LINEAR: *bytes = int8_linear_workspace_bytes(m, n, t); return PTQ_OK;
     case PTQ_OP_PAGED_ATTENTION: *bytes = paged_attention_workspace_bytes(m, n, t, block); return PTQ_OK;
+    case PTQ_OP_SHARED_ATTENTION: *bytes = paged_attention_shared_workspace_bytes(m, n, t, block); return PTQ_OK;
   }
   return PTQ_ERR_ARG;
 }
@@ -477,6 +478,30 @@ ptq_status ptq_prompt_attention(const void* Q, int64_t q_token, int64_t q_head, 
   if (!Q || !K || !V || !O || !cu || O == K || O == V || (O == Q && (o_token != q_token || o_head != q_head))) return PTQ_ERR_ARG;
   return prompt_attention_launch(Q, q_token, q_head, K, k_token, k_head, V, v_token, v_head, t, hq, hkv, d, cu, b, max_n, softmax_scale, causal,
                                  window, O, o_token, o_head, static_cast<hipStream_t>(stream));
+}
+
+ptq_status ptq_paged_attention_shared(const void* Q, ptq_dtype qdt, int64_t q_token, int64_t q_head, int64_t t, int64_t hq, int64_t d,
+                                      const int32_t* cu_q, int64_t b, int64_t max_q, const uint8_t* codes, const float* scales,
+                                      const uint8_t* zeros, int64_t pages, int64_t page, int64_t hkv, int bits, const int32_t* table,
+                                      int64_t ldt, const int32_t* kv_lens, int64_t max_kv, const int32_t* cu_groups, const int32_t* shared,
+                                      int64_t groups, int64_t max_shared, double softmax_scale, int causal, void* O, int64_t o_token,
+                                      int64_t o_head, void* ws, size_t ws_bytes, ptq_stream stream) {
+  if (qdt != PTQ_BF16) return PTQ_ERR_DTYPE;
+  const ptq_status bad = kv_cache_bad(hkv, d, bits, pages, page);
+  if (bad != PTQ_OK) return bad;
+  if (!(std::fabs(softmax_scale) <= 2e38)) return PTQ_ERR_ARG;   // (times log2(e) it is a float32)
+  if (t < 0 || t > (1 << 24) || hq <= 0 || hq > 65535 || hq % hkv != 0 || b < 0 || b > 65535 || max_q < 0 || max_q > t || ldt < 0 ||
+      max_kv < 0 || max_kv > INT32_MAX / 4 || q_token < 0 || q_head < 0 || o_token < 0 || o_head < 0 || groups < 0 || groups > 65535 || max_shared < 0)
+    return PTQ_ERR_SHAPE;
+  if (max_q * (hq / hkv) > (1 << 27) || t * (hq / hkv) > (1 << 27)) return PTQ_ERR_SHAPE;   // a key head's rows, counted in 32 bits
+  if (t == 0 || b == 0 || max_q == 0) return PTQ_OK;
+  if (pages == 0) return PTQ_ERR_SHAPE;
+  if (!Q || !O || Q == O || !cu_q || !codes || !scales || !zeros || !table || !kv_lens || misaligned(codes, 16)) return PTQ_ERR_ARG;
+  if (groups > 0 && (!cu_groups || !shared)) return PTQ_ERR_ARG;
+  if (ws_bad(ws, ws_bytes, paged_attention_shared_workspace_bytes(hq, d, t, max_kv))) return PTQ_ERR_WORKSPACE;
+  return paged_attention_shared_launch(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt,
+                                       kv_lens, max_kv, cu_groups, shared, groups, max_shared, softmax_scale, causal, O, o_token, o_head, ws,
+                                       static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -345,9 +345,41 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
+// Q, cu_q, max_q, codes, scales, zeros, bits, table, kv_lens, max_kv, cu_groups, shared, max_shared, softmax_scale, O, causal, ws
+PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  if (!count_is(count, 17)) return nullptr;
+  return status_of([&]() -> ptq_status {
+    const Tensor &Q = tensor(a[0]), &cu = tensor(a[1]), &codes = tensor(a[3]), &scales = tensor(a[4]), &zeros = tensor(a[5]), &table = tensor(a[7]),
+                 &lens = tensor(a[8]), &cu_groups = tensor(a[10]), &shared = tensor(a[11]), &O = tensor(a[14]);
+    const Tensor* ws = optional(a[16]);
+    const int64_t max_q = whole(a[2]), bits = whole(a[6]), max_kv = whole(a[9]), max_shared = whole(a[12]);
+    const double scale = number(a[13]);
+    const int causal = truth(a[15]);
+    PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
+    const int64_t t = Q.size(0), hq = Q.size(1), d = Q.size(2);
+    const Cache c = cache_of(codes, scales, zeros, bits, d);
+    PTQ_CHECK(table_ok(table));
+    const int64_t b = table.size(0), groups = shared.numel();
+    PTQ_CHECK(whole_numbers(cu, b + 1));
+    PTQ_CHECK(whole_numbers(lens, b));
+    PTQ_CHECK(whole_numbers(cu_groups, groups + 1) && whole_numbers(shared, groups));
+    PTQ_CHECK(!ws || ws->is_contiguous());
+    ptq_dtype dt;
+    if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
+    const Workspace w(ws, Q, PTQ_OP_SHARED_ATTENTION, hq, d, t, max_kv);
+    const ptq_stream s = stream();
+    return released([&] {
+      return ptq_paged_attention_shared(ptr(Q), dt, Q.stride(0), Q.stride(1), t, hq, d, as<int32_t>(cu), b, max_q, as<uint8_t>(codes), as<float>(scales),
+                                        as<uint8_t>(zeros), c.pages, c.page, c.heads, (int)bits, as<int32_t>(table), table.size(1), as<int32_t>(lens),
+                                        max_kv, as<int32_t>(cu_groups), as<int32_t>(shared), groups, max_shared, scale, causal, ptr(O), O.stride(0),
+                                        O.stride(1), w.at, w.bytes, s);
+    });
+  });
+}
+
 #define PTQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PTQ_METHOD(rmsnorm_quantize), PTQ_METHOD(int8_linear), PTQ_METHOD(kv_cache_write), PTQ_METHOD(kv_cache_read),
-                         PTQ_METHOD(paged_attention), PTQ_METHOD(rotary), PTQ_METHOD(rotary_kv_cache_write), PTQ_METHOD(kv_cache_copy_pages), PTQ_METHOD(prompt_attention), {nullptr, nullptr, 0, nullptr}};
+                         PTQ_METHOD(paged_attention), PTQ_METHOD(rotary), PTQ_METHOD(rotary_kv_cache_write), PTQ_METHOD(kv_cache_copy_pages), PTQ_METHOD(prompt_attention), PTQ_METHOD(paged_attention_shared), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tokens", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
