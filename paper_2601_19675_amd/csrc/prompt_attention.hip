@@ -11,8 +11,9 @@
 // maximum M, a whole number, moves only when one of the row's scores is 2^8 above it; weights are rounded to bfloat16 (2^-8 of each), and the sum of
 // the weights is of the rounded ones, so that the rounding drops out where the values are alike.  Scores, maxima and sums are float32.
 //
-// A key that a row does not see leaves it as it is, whatever it holds: its score is replaced, and in the tiles of keys of which some row
-// does not see all, values that are not finite are taken out of the product (0 times them is not 0) and added for the rows that see them.
+// A key that a row does not see leaves it as it is, whatever it holds: its score is replaced.  A value that is not finite would meet a weight of 0
+// all the same (0 times it is not 0): a workgroup that ends with anything not finite starts over, takes such values out of the tiles that it
+// reads, and adds them at the end for the rows that see them.
 #include <algorithm>
 
 #include "lds_dma.h"
@@ -73,9 +74,11 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
 
-  // the last rows, which see most, first
-  const int64_t groups = (int64_t)a.b * a.hkv, item = first_item + blockIdx.x;
-  const int tile = a.tiles - 1 - (int)(item / groups), seq = (int)(item % groups / a.hkv), head = (int)(item % groups % a.hkv);
+  // Groups (prompt, key head) go round the dies, so that a group's row tiles share its keys and values in one L2; the last rows, which see
+  // most, first.  (Consecutive workgroups of a die go to its shader engines in turn, however busy those are: they have to be alike.)
+  const int64_t block = first_item + blockIdx.x, idx = block >> 3, group = idx / a.tiles * 8 + (block & 7);
+  if (group >= (int64_t)a.b * a.hkv) return;
+  const int tile = a.tiles - 1 - (int)(idx % a.tiles), seq = (int)(group / a.hkv), head = (int)(group % a.hkv);
   const int64_t from64 = a.cu[seq], to64 = a.cu[seq + 1];
   if (from64 < 0 || to64 > a.t || to64 <= from64) return;
   const int first = (int)from64, n = min((int)(to64 - from64), a.max_n), rows = n * a.group, row0 = tile * C::kRows;
@@ -91,13 +94,15 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
   sees((min(row0 + C::kRows, rows) - 1) / a.group, unused, end);
   begin &= ~(kTile - 1);
   const int count = (end - begin + kTile - 1) / kTile;      // a row sees itself: at least one
-  // of the wave's rows: all of them see [lo_b, hi_a), none sees anything outside [lo_a, hi_b)
   const int wrow = row0 + 32 * wave;
-  const bool working = wrow < rows;
-  int lo_a = 0, hi_a = 0, lo_b = 0, hi_b = 0;
-  if (working) {
-    sees(wrow / a.group, lo_a, hi_a);
-    sees((min(wrow + 32, rows) - 1) / a.group, lo_b, hi_b);
+  // tiles [plain0, plain1) are those of which every row of the workgroup sees all keys
+  int plain0, plain1;
+  {
+    int lo_b, hi_a;
+    sees(row0 / a.group, unused, hi_a);
+    sees((min(row0 + C::kRows, rows) - 1) / a.group, lo_b, unused);
+    plain0 = max(0, lo_b - begin + kTile - 1) / kTile;
+    plain1 = max(0, hi_a - begin) / kTile;
   }
 
   // ---- keys and values of a tile, into LDS
@@ -143,14 +148,6 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     asm volatile("" ::: "memory");
   };
 
-  // asked for in the order K0, V0, K1, V1, ...
-  bring_keys(0);
-#pragma unroll
-  for (int t = 0; t < kRing - 2; ++t) {
-    bring_vals(t);
-    bring_keys(t + 1);
-  }
-
   // ---- the wave's queries
   const int row = wrow + r, token = first + row / a.group, qhead = head * a.group + row % a.group;
   const bool live = row < rows;
@@ -171,11 +168,7 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
   const float factor = fmaxf(fabsf(a.scale), 0x1p-126f);   // positive: a score that is not there is -inf times it
 
   f32x16v acc[kOut];
-#pragma unroll
-  for (int k = 0; k < kOut; ++k)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[k][i] = 0.f;
-  float M = kNoScore, sum = 0.f;   // of the weights of the lane's keys
+  float M, sum;   // the sum is of the weights of the lane's keys
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3f803f80u);
 
   // a lane's place in a tile of keys: row r, chunk h; of values: keys 4 h + j of 16, channels 4 (lane & 3) of 16 (lane >> 4 & 1) on
@@ -190,50 +183,45 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     const uint2 u = __builtin_bit_cast(uint2, x), w = __builtin_bit_cast(uint2, y);
     return bf16x8_of(u.x, u.y, w.x, w.y);
   };
-  // Some row of the wave does not see all keys of tile t: values that are not finite must not meet a weight of 0.  Whether there are any.
-  auto odd_values = [&](int t) {
-    const int at = opaque(val_slot(t) + val_at);
-    u16x2 top = {0, 0};
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int k = 0; k < kOut; ++k) {
-        const u32x4 v = __builtin_bit_cast(u32x4, value(at, g, k));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, (uint32_t)(v[i] & 0x7fff7fffu)));
-      }
-    return __any((top[0] >= 0x7f80) | (top[1] >= 0x7f80)) != 0;
-  };
-  // ... their product without them, and they themselves for the rows that see them (a weight is positive: an infinity stays what it is)
-  auto multiply_odd = [&](int t, const bf16x8 (&weights)[4]) {
-    const int at = opaque(val_slot(t) + val_at);
+  // values of tile t that are not finite become 0
+  auto clean = [&](int t) {
 #pragma unroll 1
-    for (int g = 0; g < 4; ++g) {
-      const bf16x8 w = g == 0 ? weights[0] : g == 1 ? weights[1] : g == 2 ? weights[2] : weights[3];
+    for (int at = threadIdx.x * 16; at < C::kBytes; at += C::kThreads * 16) {
+      u32x4 v = *reinterpret_cast<u32x4*>(smem + val_slot(t) + at);
 #pragma unroll
-      for (int k = 0; k < kOut; ++k) {
-        u32x4 v = __builtin_bit_cast(u32x4, value(at, g, k));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
-          if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
-        }
-        acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), w, acc[k], 0, 0, 0);
+      for (int i = 0; i < 4; ++i) {
+        if ((v[i] & 0x7f80u) == 0x7f80u) v[i] &= 0xffff0000u;
+        if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0xffffu;
       }
+      *reinterpret_cast<u32x4*>(smem + val_slot(t) + at) = v;
     }
-    const int from = lo - (begin + t * kTile), to = hi - (begin + t * kTile);
+    meet();
+  };
+  // ... and are added here for the wave's rows that see them (a weight is positive: an infinity stays what it is)
+  auto add_cleaned = [&]() {
 #pragma unroll 1
-    for (int key = max(0, from); key < min(kTile, to); ++key) {
-      const char* row = smem + val_slot(t) + key * C::kPitch;
+    for (int key0 = begin; key0 < end; key0 += kTile) {
+      int odd = 0;
+#pragma unroll 1
+      for (int i = lane; i < kTile * (a.d / 8); i += kWave) {
+        const int key = min(key0 + i / (a.d / 8), n - 1), c = i % (a.d / 8) * 8;
+        const Run<PTQ_BF16, 8> v = load_run<PTQ_BF16, 8, false>(a.V + (int64_t)(first + key) * a.v_token + head * a.v_head, c, a.d);
 #pragma unroll
-      for (int k = 0; k < kOut; ++k)
+        for (int e = 0; e < 4; ++e) odd |= ((v.w[e] & 0x7f80u) == 0x7f80u) | ((v.w[e] & 0x7f800000u) == 0x7f800000u);
+      }
+      if (!__any(odd)) continue;
+#pragma unroll 1
+      for (int key = max(key0, lo); key < min(min(key0 + kTile, end), hi); ++key) {
+        const uint16_t* V = a.V + (int64_t)(first + key) * a.v_token + head * a.v_head;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {   // channels 32 k + 8 q + 4 h ..
-          const uint2 v = *reinterpret_cast<const uint2*>(row + (((4 * k + q) ^ val_turn<DP>(key)) * 16) + 8 * h);
-          const uint32_t e[4] = {v.x << 16, v.x & 0xffff0000u, v.y << 16, v.y & 0xffff0000u};
+        for (int k = 0; k < kOut; ++k)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[k][4 * q + i] += (e[i] & 0x7f800000u) == 0x7f800000u ? __uint_as_float(e[i]) : 0.f;
-        }
+          for (int i = 0; i < 16; ++i) {
+            const int c = 32 * k + 8 * (i >> 2) + 4 * h + (i & 3);
+            const float v = c < a.d ? bf16_bits_to_f32(V[c]) : 0.f;
+            acc[k][i] += fabsf(v) < INFINITY ? 0.f : v;
+          }
+      }
     }
   };
 
@@ -241,16 +229,8 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
   // missing.  Groups of instructions -- the channels' blocks of 16 keys; two steps of d of both halves of the keys -- whose operands are
   // read from LDS a group before.
   constexpr int kGroups = 4 + kSteps / 2, kPer = kOut > 4 ? kOut : 4;
-  bool whole = true;   // every row of the wave sees all of tile t - 1
   auto multiply = [&](auto had_, auto has_, int t, const bf16x8 (&weights)[4], f32x16v (&s)[2]) {
     constexpr int kFirst = decltype(had_)::value ? 0 : 4, kLast = decltype(has_)::value ? kGroups : 4;
-    bool values = true;
-    if constexpr (decltype(had_)::value) {
-      if (!whole && odd_values(t - 1)) {
-        multiply_odd(t - 1, weights);
-        values = false;
-      }
-    }
     const int key_base = opaque(key_slot(t) + key_at), val_base = opaque(val_slot(t + kRing - 1) + val_at);
     bf16x8 f[2][kPer];
     auto read = [&](auto g_) {
@@ -272,10 +252,8 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (g + 1 < kLast) read(std::integral_constant<int, g + 1>{});
       if constexpr (g < 4) {
-        if (values) {
 #pragma unroll
-          for (int k = 0; k < kOut; ++k) acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at][k], weights[g], acc[k], 0, 0, 0);
-        }
+        for (int k = 0; k < kOut; ++k) acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at][k], weights[g], acc[k], 0, 0, 0);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -288,10 +266,9 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     __builtin_amdgcn_sched_barrier(0);
   };
   // the weights of tile t; what has been summed so far is brought to their maximum
-  auto soften = [&](int t, f32x16v (&s)[2], bf16x8 (&weights)[4]) {
-    const int key0 = begin + t * kTile;
-    whole = key0 >= lo_b && key0 + kTile <= hi_a;
-    if (!whole) {
+  auto soften = [&](auto mask_, int t, f32x16v (&s)[2], bf16x8 (&weights)[4]) {
+    if constexpr (decltype(mask_)::value) {
+      const int key0 = begin + t * kTile;
       // counted from the half wave's first key: what is left are constants
       const int from_ = opaque(lo - key0 - 4 * h), to_ = opaque(hi - key0 - 4 * h);
 #pragma unroll
@@ -330,49 +307,95 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
       }
   };
 
-  f32x16v s[2];
-  bf16x8 weights[4];
   constexpr std::true_type yes;
   constexpr std::false_type no;
-  if constexpr (TURNS) {
-    // Phases: the first half of the waves multiplies in the even ones -- values of tile t - 1 and keys of tile t in phase 2 t -- and works
-    // out weights in the odd ones; the second half is a phase behind.  Slots of tiles that both have read are filled again in the latter.
-    const bool second = wave >= C::kWaves / 2;
-    arrived(std::integral_constant<int, 2 * kRing - 4>{});
-    meet();
-    if (second) meet();
-    if (working) multiply(no, yes, 0, weights, s);
-    for (int t = 0;; ++t) {
-      if (second) arrived(std::integral_constant<int, 2 * kRing - 6>{});
-      meet();
-      bring_vals(t + kRing - 2);
-      bring_keys(t + kRing - 1);
-      if (working) soften(t, s, weights);
-      if (!second) arrived(std::integral_constant<int, 2 * kRing - 4>{});
-      meet();
-      if (t + 1 == count) break;
-      if (working) multiply(yes, yes, t + 1, weights, s);
-    }
-    if (working) multiply(yes, no, count, weights, s);
-    if (!second) meet();
-  } else {
-    // all waves in step: tile t's values and the next one's keys are asked for when everybody has the slots' tiles behind him
-    for (int t = 0; t < count; ++t) {
-      arrived(std::integral_constant<int, 0>{});
-      meet();
+#pragma unroll 1
+  for (bool careful = false;; careful = true) {
+#pragma unroll
+    for (int k = 0; k < kOut; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[k][i] = 0.f;
+    M = kNoScore, sum = 0.f;
+    f32x16v s[2];
+    bf16x8 weights[4];
+    // asked for in the order K0, V0, K1, V1, ...
+    bring_keys(0);
+#pragma unroll
+    for (int t = 0; t < kRing - 2; ++t) {
       bring_vals(t);
       bring_keys(t + 1);
-      if (working) {
-        multiply(no, yes, t, weights, s);
-        soften(t, s, weights);
-      }
-      arrived(std::integral_constant<int, 1>{});
-      meet();
-      if (working) multiply(yes, no, t + 1, weights, s);
     }
+    if constexpr (TURNS) {
+      // Phases: the first half of the waves multiplies in the even ones -- values of tile t - 1 and keys of tile t in phase 2 t -- and works
+      // out weights in the odd ones; the second half is a phase behind.  Slots of tiles that both have read are filled again in the latter.
+      const bool second = wave >= C::kWaves / 2;
+      arrived(std::integral_constant<int, 2 * kRing - 4>{});
+      meet();
+      if (second) meet();
+      multiply(no, yes, 0, weights, s);
+      auto until_weights = [&](auto mask_, int t) {
+        if (second) arrived(std::integral_constant<int, 2 * kRing - 6>{});
+        meet();
+        if (careful && second) clean(t);
+        bring_vals(t + kRing - 2);
+        bring_keys(t + kRing - 1);
+        soften(mask_, t, s, weights);
+        if (!second) arrived(std::integral_constant<int, 2 * kRing - 4>{});
+        meet();
+        if (careful && !second) clean(t);
+      };
+      int t = 0;
+      for (; t < min(plain0, count - 1); ++t) {
+        until_weights(yes, t);
+        multiply(yes, yes, t + 1, weights, s);
+      }
+      for (; t < min(plain1, count - 1); ++t) {
+        until_weights(no, t);
+        multiply(yes, yes, t + 1, weights, s);
+      }
+      for (; t < count - 1; ++t) {
+        until_weights(yes, t);
+        multiply(yes, yes, t + 1, weights, s);
+      }
+      until_weights(yes, t);
+      multiply(yes, no, count, weights, s);
+      if (!second) meet();
+    } else {
+      // all waves in step: tile t's values and the next one's keys are asked for when everybody has the slots' tiles behind him
+      for (int t = 0; t < count; ++t) {
+        arrived(std::integral_constant<int, 0>{});
+        meet();
+        bring_vals(t);
+        bring_keys(t + 1);
+        multiply(no, yes, t, weights, s);
+        soften(yes, t, s, weights);
+        arrived(std::integral_constant<int, 1>{});
+        meet();
+        if (careful) clean(t);
+        multiply(yes, no, t + 1, weights, s);
+      }
+    }
+    arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
+    if (careful) {
+      add_cleaned();
+      break;
+    }
+    float odd = 0.f;   // NaN if anything is not finite
+#pragma unroll
+    for (int k = 0; k < kOut; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd = fmaf(acc[k][i], 0.f, odd);
+    meet();
+    int* const vote = reinterpret_cast<int*>(smem);
+    if (lane == 0) vote[wave] = 0;
+    if (live && odd != 0.f) vote[wave] = 1;
+    meet();
+    int any = 0;
+#pragma unroll
+    for (int w = 0; w < C::kWaves; ++w) any |= vote[w];
+    if (__builtin_amdgcn_readfirstlane(any) == 0) break;
+    meet();
   }
-  arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
-
   sum += __shfl_xor(sum, 32);
   if (!live) return;
   const float l = sum, inv = l == 0.f ? __uint_as_float(0x7fc00000u) : 1.f / l;   // (a row sees itself: its weights are not all 0 unless its scores are -inf)
@@ -394,7 +417,7 @@ bool prompt_form_launch(const PromptArgs& all, hipStream_t s) {
   PromptArgs a = all;
   a.tiles = (int)ceil_div((int64_t)a.max_n * a.group, C::kRows);
   // a launch has fewer than 2^32 threads
-  const int64_t items = (int64_t)a.tiles * a.b * a.hkv, step = 1 << 22;
+  const int64_t items = (int64_t)a.tiles * ceil_div((int64_t)a.b * a.hkv, 8) * 8, step = 1 << 22;
   for (int64_t first = 0; first < items; first += step)
     prompt_kernel<DP, TURNS, DMA><<<(unsigned)std::min(step, items - first), C::kThreads, C::kLds, s>>>(a, first);
   return true;
