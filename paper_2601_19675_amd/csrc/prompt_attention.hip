@@ -227,14 +227,14 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
 
   // What the matrix instructions do in one go: the values of tile t - 1 (with its weights), then the scores of tile t, either may be
   // missing.  Groups of instructions -- the channels' blocks of 16 keys; two steps of d of both halves of the keys -- whose operands are
-  // read from LDS a group before.
-  constexpr int kGroups = 4 + kSteps / 2, kPer = kOut > 4 ? kOut : 4;
+  // read from LDS kReadAhead groups before.
+  constexpr int kGroups = 4 + kSteps / 2, kPer = kOut > 4 ? kOut : 4, kReadAhead = DP > 128 ? 1 : 2;
   auto multiply = [&](auto had_, auto has_, int t, const bf16x8 (&weights)[4], f32x16v (&s)[2]) {
     constexpr int kFirst = decltype(had_)::value ? 0 : 4, kLast = decltype(has_)::value ? kGroups : 4;
     const int key_base = opaque(key_slot(t) + key_at), val_base = opaque(val_slot(t + kRing - 1) + val_at);
-    bf16x8 f[2][kPer];
+    bf16x8 f[kReadAhead + 1][kPer];
     auto read = [&](auto g_) {
-      constexpr int g = decltype(g_)::value, at = g % 2;
+      constexpr int g = decltype(g_)::value, at = g % (kReadAhead + 1);
       if constexpr (g < 4) {
 #pragma unroll
         for (int k = 0; k < kOut; ++k) f[at][k] = value(val_base, g, k);
@@ -246,11 +246,14 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
         }
       }
     };
-    read(std::integral_constant<int, kFirst>{});
+    static_for<kReadAhead>([&](auto i_) {
+      constexpr int g = kFirst + decltype(i_)::value;
+      if constexpr (g < kLast) read(std::integral_constant<int, g>{});
+    });
     static_for<kLast - kFirst>([&](auto i_) {
-      constexpr int g = kFirst + decltype(i_)::value, at = g % 2;
+      constexpr int g = kFirst + decltype(i_)::value, at = g % (kReadAhead + 1);
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (g + 1 < kLast) read(std::integral_constant<int, g + 1>{});
+      if constexpr (g + kReadAhead < kLast) read(std::integral_constant<int, g + kReadAhead>{});
       if constexpr (g < 4) {
 #pragma unroll
         for (int k = 0; k < kOut; ++k) acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at][k], weights[g], acc[k], 0, 0, 0);
@@ -305,6 +308,10 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
         }
         weights[2 * k + u] = bf16x8_of(w[0], w[1], w[2], w[3]);
       }
+    // here, and not where they are used: behind the barrier they would stand before the wave's matrix instructions
+#pragma unroll
+    for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(weights[g]));
+    asm volatile("" : "+v"(sum));
   };
 
   constexpr std::true_type yes;
