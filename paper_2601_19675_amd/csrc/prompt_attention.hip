@@ -119,22 +119,28 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     key_off[i] = 8 * kc < a.d ? (uint32_t)row * (uint32_t)a.k_token * 2 + 16 * kc : 0xffffff00u;   // past every descriptor's end: zeros
     val_off[i] = 8 * vc < a.d ? (uint32_t)row * (uint32_t)a.v_token * 2 + 16 * vc : 0xffffff00u;
   }
-  auto bring = [&](const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot) {
-    const int left = min(kTile, n - (begin + t * kTile));   // keys
+  // (a descriptor is scalar work: nothing that a request has to wait for)
+  auto tile_at = [&](const uint16_t* from, int64_t token, int t) {
+    const int left = n - (begin + t * kTile);   // keys
+    const uint32_t bytes = ((uint32_t)(min(left, kTile) - 1) * (uint32_t)token + (uint32_t)a.d) * 2u;
+    const uint64_t at = (uint64_t)(from + (int64_t)t * kTile * token);
+    return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)(left > 0 ? bytes : 0u), 0x00020000};
+  };
+  auto bring_one = [&](const i32x4& tile, const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot, int i) {
     if constexpr (DMA) {
-      const i32x4 rsrc = buffer_at(from + (int64_t)t * kTile * token, left > 0 ? ((int64_t)(left - 1) * token + a.d) * 2 : 0);
-#pragma unroll
-      for (int i = 0; i < C::kRequests; ++i) request_to_lds(rsrc, off[i], __builtin_amdgcn_readfirstlane(lds + slot + (wave * C::kRequests + i) * 1024));
+      request_to_lds(tile, off[i], lds + slot + (wave * C::kRequests + i) * 1024);
     } else {
-#pragma unroll
-      for (int i = 0; i < C::kRequests; ++i) {
-        const int at = ((wave * C::kRequests + i) * 64 + lane) * 16, row = at / C::kPitch, pos = at % C::kPitch / 16;
-        const int chunk = pos ^ (slot < kRing * C::kBytes ? key_turn<DP>(row) : val_turn<DP>(row));
-        const bool there = row < left && 8 * chunk < a.d;
-        AnyWords<4, 2> w = *reinterpret_cast<const AnyWords<4, 2>*>(from + (there ? ((int64_t)t * kTile + row) * token + 8 * chunk : 0));
-        *reinterpret_cast<u32x4*>(smem + slot + at) = there ? u32x4{w.w[0], w.w[1], w.w[2], w.w[3]} : u32x4{0, 0, 0, 0};
-      }
+      const int at = ((wave * C::kRequests + i) * 64 + lane) * 16, row = at / C::kPitch, pos = at % C::kPitch / 16;
+      const int chunk = pos ^ (slot < kRing * C::kBytes ? key_turn<DP>(row) : val_turn<DP>(row)), key = t * kTile + row;
+      const bool there = begin + key < n && 8 * chunk < a.d;
+      AnyWords<4, 2> w = *reinterpret_cast<const AnyWords<4, 2>*>(from + (there ? key * token + 8 * chunk : 0));
+      *reinterpret_cast<u32x4*>(smem + slot + at) = there ? u32x4{w.w[0], w.w[1], w.w[2], w.w[3]} : u32x4{0, 0, 0, 0};
     }
+  };
+  auto bring = [&](const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot) {
+    const i32x4 tile = tile_at(from, token, t);
+#pragma unroll
+    for (int i = 0; i < C::kRequests; ++i) bring_one(tile, from, token, off, t, slot, i);
   };
   auto bring_keys = [&](int t) { bring(keys0, a.k_token, key_off, t, key_slot(t)); };
   auto bring_vals = [&](int t) { bring(vals0, a.v_token, val_off, t, val_slot(t)); };
@@ -168,7 +174,7 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
   const float factor = fmaxf(fabsf(a.scale), 0x1p-126f);   // positive: a score that is not there is -inf times it
 
   f32x16v acc[kOut];
-  float M, sum;   // the sum is of the weights of the lane's keys
+  float M, sum[4];   // the sums are of the weights of the lane's keys, every fourth pair
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3f803f80u);
 
   // a lane's place in a tile of keys: row r, chunk h; of values: keys 4 h + j of 16, channels 4 (lane & 3) of 16 (lane >> 4 & 1) on
@@ -227,12 +233,12 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
 
   // What the matrix instructions do in one go: the values of tile t - 1 (with its weights), then the scores of tile t, either may be
   // missing.  Groups of instructions -- the channels' blocks of 16 keys; two steps of d of both halves of the keys -- whose operands are
-  // read from LDS kReadAhead groups before.
+  // read from LDS kReadAhead groups before; the first ones' may be read apart (read_), before the barrier that the others have to wait for.
   constexpr int kGroups = 4 + kSteps / 2, kPer = kOut > 4 ? kOut : 4, kReadAhead = DP > 128 ? 1 : 2;
-  auto multiply = [&](auto had_, auto has_, int t, const bf16x8 (&weights)[4], f32x16v (&s)[2]) {
+  bf16x8 f[kReadAhead + 1][kPer];
+  auto multiply = [&](auto had_, auto has_, auto read_, auto multiply_, int t, const bf16x8 (&weights)[4], f32x16v (&s)[2]) {
     constexpr int kFirst = decltype(had_)::value ? 0 : 4, kLast = decltype(has_)::value ? kGroups : 4;
     const int key_base = opaque(key_slot(t) + key_at), val_base = opaque(val_slot(t + kRing - 1) + val_at);
-    bf16x8 f[kReadAhead + 1][kPer];
     auto read = [&](auto g_) {
       constexpr int g = decltype(g_)::value, at = g % (kReadAhead + 1);
       if constexpr (g < 4) {
@@ -246,14 +252,28 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
         }
       }
     };
-    static_for<kReadAhead>([&](auto i_) {
-      constexpr int g = kFirst + decltype(i_)::value;
-      if constexpr (g < kLast) read(std::integral_constant<int, g>{});
-    });
+    if constexpr (decltype(read_)::value)
+      static_for<kReadAhead>([&](auto i_) {
+        constexpr int g = kFirst + decltype(i_)::value;
+        if constexpr (g < kLast) read(std::integral_constant<int, g>{});
+      });
+    if constexpr (!decltype(multiply_)::value) return;
+    constexpr bool kBrings = TURNS && decltype(had_)::value && decltype(has_)::value;
+    i32x4 vals{}, keys{};
+    if constexpr (kBrings) {
+      vals = tile_at(vals0, a.v_token, t + kRing - 2);
+      keys = tile_at(keys0, a.k_token, t + kRing - 1);
+    }
     static_for<kLast - kFirst>([&](auto i_) {
       constexpr int g = kFirst + decltype(i_)::value, at = g % (kReadAhead + 1);
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (g + kReadAhead < kLast) read(std::integral_constant<int, g + kReadAhead>{});
+      // slots of tiles that both halves have read are filled again beside the products, a request at a time: several would wait for each other
+      constexpr int i = (g * 2 * C::kRequests + kGroups - 1) / kGroups;
+      if constexpr (kBrings && i < 2 * C::kRequests && i * kGroups / (2 * C::kRequests) == g) {
+        if constexpr (i < C::kRequests) bring_one(vals, vals0, a.v_token, val_off, t + kRing - 2, val_slot(t + kRing - 2), i);
+        else bring_one(keys, keys0, a.k_token, key_off, t + kRing - 1, key_slot(t + kRing - 1), i - C::kRequests);
+      }
       if constexpr (g < 4) {
 #pragma unroll
         for (int k = 0; k < kOut; ++k) acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at][k], weights[g], acc[k], 0, 0, 0);
@@ -292,7 +312,8 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
       top = fmaxf(top, __shfl_xor(top, 32));
       const float next = top > M + 8.f ? ceilf(top) : M, shrink = exp2_fast(M - next);
       M = next;
-      sum *= shrink;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] *= shrink;
 #pragma unroll
       for (int k = 0; k < kOut; ++k) acc[k] *= shrink;
     }
@@ -304,14 +325,13 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           w[i] = bf16_pair(exp2_fast(fmaf(s[k][8 * u + 2 * i], factor, -M)), exp2_fast(fmaf(s[k][8 * u + 2 * i + 1], factor, -M)));
-          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), ones, sum, false);
+          sum[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), ones, sum[i], false);
         }
         weights[2 * k + u] = bf16x8_of(w[0], w[1], w[2], w[3]);
       }
     // here, and not where they are used: behind the barrier they would stand before the wave's matrix instructions
 #pragma unroll
     for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(weights[g]));
-    asm volatile("" : "+v"(sum));
   };
 
   constexpr std::true_type yes;
@@ -322,50 +342,59 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     for (int k = 0; k < kOut; ++k)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[k][i] = 0.f;
-    M = kNoScore, sum = 0.f;
+    M = kNoScore;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = 0.f;
     f32x16v s[2];
     bf16x8 weights[4];
     // asked for in the order K0, V0, K1, V1, ...
     bring_keys(0);
 #pragma unroll
-    for (int t = 0; t < kRing - 2; ++t) {
+    for (int t = 0; t < (TURNS ? kRing - 1 : 0); ++t) {
       bring_vals(t);
       bring_keys(t + 1);
     }
     if constexpr (TURNS) {
       // Phases: the first half of the waves multiplies in the even ones -- values of tile t - 1 and keys of tile t in phase 2 t -- and works
-      // out weights in the odd ones; the second half is a phase behind.  Slots of tiles that both have read are filled again in the latter.
+      // out weights in the odd ones; the second half is a phase behind.
       const bool second = wave >= C::kWaves / 2;
-      arrived(std::integral_constant<int, 2 * kRing - 4>{});
+      static_assert(2 * C::kRequests <= kGroups, "");
+      arrived(std::integral_constant<int, 2 * kRing - 2>{});
       meet();
-      if (second) meet();
-      multiply(no, yes, 0, weights, s);
-      auto until_weights = [&](auto mask_, int t) {
-        if (second) arrived(std::integral_constant<int, 2 * kRing - 6>{});
+      if (second) {
+        arrived(std::integral_constant<int, 2 * kRing - 3>{});
         meet();
-        if (careful && second) clean(t);
-        bring_vals(t + kRing - 2);
-        bring_keys(t + kRing - 1);
-        soften(mask_, t, s, weights);
-        if (!second) arrived(std::integral_constant<int, 2 * kRing - 4>{});
+        if (careful) clean(0);
+      }
+      multiply(no, yes, yes, yes, 0, weights, s);
+      auto until_weights = [&](auto mask_, auto last_, int t) {
+        // the values of tile t have to be there a phase before their turn
+        if (second) arrived(std::integral_constant<int, 2 * kRing - 4>{});
+        else arrived(std::integral_constant<int, 2 * kRing - 3>{});
         meet();
         if (careful && !second) clean(t);
+        soften(mask_, t, s, weights);
+        multiply(yes, std::integral_constant<bool, !decltype(last_)::value>{}, yes, no, t + 1, weights, s);
+        if (second) arrived(std::integral_constant<int, 2 * kRing - 5>{});
+        else arrived(std::integral_constant<int, 2 * kRing - 4>{});
+        meet();
+        if (careful && second && !decltype(last_)::value) clean(t + 1);
       };
       int t = 0;
       for (; t < min(plain0, count - 1); ++t) {
-        until_weights(yes, t);
-        multiply(yes, yes, t + 1, weights, s);
+        until_weights(yes, no, t);
+        multiply(yes, yes, no, yes, t + 1, weights, s);
       }
       for (; t < min(plain1, count - 1); ++t) {
-        until_weights(no, t);
-        multiply(yes, yes, t + 1, weights, s);
+        until_weights(no, no, t);
+        multiply(yes, yes, no, yes, t + 1, weights, s);
       }
       for (; t < count - 1; ++t) {
-        until_weights(yes, t);
-        multiply(yes, yes, t + 1, weights, s);
+        until_weights(yes, no, t);
+        multiply(yes, yes, no, yes, t + 1, weights, s);
       }
-      until_weights(yes, t);
-      multiply(yes, no, count, weights, s);
+      until_weights(yes, yes, t);
+      multiply(yes, no, no, yes, count, weights, s);
       if (!second) meet();
     } else {
       // all waves in step: tile t's values and the next one's keys are asked for when everybody has the slots' tiles behind him
@@ -374,12 +403,12 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
         meet();
         bring_vals(t);
         bring_keys(t + 1);
-        multiply(no, yes, t, weights, s);
+        multiply(no, yes, yes, yes, t, weights, s);
         soften(yes, t, s, weights);
         arrived(std::integral_constant<int, 1>{});
         meet();
         if (careful) clean(t);
-        multiply(yes, no, t + 1, weights, s);
+        multiply(yes, no, yes, yes, t + 1, weights, s);
       }
     }
     arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
@@ -403,9 +432,10 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     if (__builtin_amdgcn_readfirstlane(any) == 0) break;
     meet();
   }
-  sum += __shfl_xor(sum, 32);
+  float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  l += __shfl_xor(l, 32);
   if (!live) return;
-  const float l = sum, inv = l == 0.f ? __uint_as_float(0x7fc00000u) : 1.f / l;   // (a row sees itself: its weights are not all 0 unless its scores are -inf)
+  const float inv = l == 0.f ? __uint_as_float(0x7fc00000u) : 1.f / l;   // (a row sees itself: its weights are not all 0 unless its scores are -inf)
   uint16_t* O = a.O + token * a.o_token + qhead * a.o_head;
 #pragma unroll
   for (int k = 0; k < kOut; ++k)
