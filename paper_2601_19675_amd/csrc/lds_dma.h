@@ -46,6 +46,12 @@ __device__ __forceinline__ void request_to_lds(i32x4 rsrc, uint32_t voff, uint32
                : "memory", "m0");
 }
 
+// The same, whatever wrote its scalar operands last (a vector instruction, where the compiler had put them into a vector register's lanes).
+__device__ __forceinline__ void request_to_lds_waiting(i32x4 rsrc, uint32_t voff, uint32_t ldsaddr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(ldsaddr), "v"(voff), "s"(rsrc)
+               : "memory", "m0");
+}
+
 // The same with the LDS address as a scalar base plus a compile-time offset: one scalar instruction per request
 // instead of an add into a temporary and a move.
 template <uint32_t OFFSET>

@@ -40,16 +40,14 @@ struct PromptArgs {
   int tiles;                                // of rows, of the longest prompt there may be
 };
 
-// TURNS: eight waves, two to a SIMD, one half of which multiplies while the other works out weights
-template <int DP, bool TURNS>
+template <int DP, int WAVES>
 struct Prompt {
-  static constexpr int kThreads = TURNS ? 512 : 256, kWaves = kThreads / 64, kRows = 32 * kWaves;
+  static constexpr int kThreads = 64 * WAVES, kWaves = WAVES, kRows = 32 * kWaves;
   static constexpr int kPitch = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;     // bytes of a key, or of a value
   static constexpr int kBytes = kTile * kPitch;
-  static constexpr int kRing = TURNS ? 4 : DP > 128 ? 2 : 2;                // tiles of each in LDS
+  static constexpr int kRing = DP > 128 || WAVES < 8 ? 2 : 3;               // tiles of each in LDS
   static constexpr int kLds = 2 * kRing * kBytes;
   static constexpr int kRequests = kBytes / 1024 / kWaves;                  // of 1024 bytes, of a wave for a tile
-  static constexpr int kRequestRows = 1024 / kPitch;
 };
 // 16-byte chunk c of row `key` lies at c ^ turn
 template <int DP>
@@ -66,9 +64,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return __built
 __device__ __forceinline__ bf16x8 bf16x8_of(uint32_t a, uint32_t b, uint32_t c, uint32_t d) { return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d}); }
 
 // DMA: rows of K and V begin at multiples of 16 bytes; otherwise they go through registers
-template <int DP, bool TURNS, bool DMA>
-__global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(PromptArgs a, int64_t first_item) {
-  using C = Prompt<DP, TURNS>;
+template <int DP, int WAVES, bool DMA>
+__global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) void prompt_kernel(PromptArgs a, int64_t first_item) {
+  using C = Prompt<DP, WAVES>;
   constexpr int kSteps = DP / 16, kOut = DP / 32, kRing = C::kRing;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
@@ -120,15 +118,15 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     val_off[i] = 8 * vc < a.d ? (uint32_t)row * (uint32_t)a.v_token * 2 + 16 * vc : 0xffffff00u;
   }
   // (a descriptor is scalar work: nothing that a request has to wait for)
-  auto tile_at = [&](const uint16_t* from, int64_t token, int t) {
+  auto tile_at = [&](const uint16_t* from, int64_t token, int t) __attribute__((always_inline)) {
     const int left = n - (begin + t * kTile);   // keys
     const uint32_t bytes = ((uint32_t)(min(left, kTile) - 1) * (uint32_t)token + (uint32_t)a.d) * 2u;
     const uint64_t at = (uint64_t)(from + (int64_t)t * kTile * token);
     return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), (int)(left > 0 ? bytes : 0u), 0x00020000};
   };
-  auto bring_one = [&](const i32x4& tile, const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot, int i) {
+  auto bring_one = [&](const i32x4& tile, const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot, int i) __attribute__((always_inline)) {
     if constexpr (DMA) {
-      request_to_lds(tile, off[i], lds + slot + (wave * C::kRequests + i) * 1024);
+      request_to_lds_waiting(tile, off[i], lds + slot + (wave * C::kRequests + i) * 1024);
     } else {
       const int at = ((wave * C::kRequests + i) * 64 + lane) * 16, row = at / C::kPitch, pos = at % C::kPitch / 16;
       const int chunk = pos ^ (slot < kRing * C::kBytes ? key_turn<DP>(row) : val_turn<DP>(row)), key = t * kTile + row;
@@ -137,18 +135,18 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
       *reinterpret_cast<u32x4*>(smem + slot + at) = there ? u32x4{w.w[0], w.w[1], w.w[2], w.w[3]} : u32x4{0, 0, 0, 0};
     }
   };
-  auto bring = [&](const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot) {
+  auto bring = [&](const uint16_t* from, int64_t token, const uint32_t (&off)[C::kRequests], int t, int slot) __attribute__((always_inline)) {
     const i32x4 tile = tile_at(from, token, t);
 #pragma unroll
     for (int i = 0; i < C::kRequests; ++i) bring_one(tile, from, token, off, t, slot, i);
   };
-  auto bring_keys = [&](int t) { bring(keys0, a.k_token, key_off, t, key_slot(t)); };
-  auto bring_vals = [&](int t) { bring(vals0, a.v_token, val_off, t, val_slot(t)); };
+  auto bring_keys = [&](int t) __attribute__((always_inline)) { bring(keys0, a.k_token, key_off, t, key_slot(t)); };
+  auto bring_vals = [&](int t) __attribute__((always_inline)) { bring(vals0, a.v_token, val_off, t, val_slot(t)); };
   // until all but the last N tiles that this wave has asked for are there (keys and values count one each)
-  auto arrived = [&](auto n_) {
+  auto arrived = [&](auto n_) __attribute__((always_inline)) {
     if constexpr (DMA) wait_requests<decltype(n_)::value * C::kRequests>();
   };
-  auto meet = [&]() {
+  auto meet = [&]() __attribute__((always_inline)) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -182,7 +180,7 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
   const int key_at = r * C::kPitch + ((h ^ key_turn<DP>(r)) * 16);
   const int val_at = (4 * h + j) * C::kPitch + ((vchunk ^ val_turn<DP>(j)) * 16) + 8 * (lane & 1);
   // channels 32 k + .. of keys 16 g + 4 h .. and 16 g + 8 + 4 h ..: what an instruction takes of the values
-  auto value = [&](int at, int g, int k) {
+  auto value = [&](int at, int g, int k) __attribute__((always_inline)) {
     using P = __attribute__((address_space(3))) s16x4*;
     const uint32_t p = lds + (uint32_t)(DP <= 64 ? at ^ (64 * k) : (at ^ (64 * (k & 3))) + (k >> 2) * 256) + g * 16 * C::kPitch;
     const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)p), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(uintptr_t)(p + 8 * C::kPitch));
@@ -190,7 +188,7 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     return bf16x8_of(u.x, u.y, w.x, w.y);
   };
   // values of tile t that are not finite become 0
-  auto clean = [&](int t) {
+  auto clean = [&](int t) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int at = threadIdx.x * 16; at < C::kBytes; at += C::kThreads * 16) {
       u32x4 v = *reinterpret_cast<u32x4*>(smem + val_slot(t) + at);
@@ -231,107 +229,94 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     }
   };
 
-  // What the matrix instructions do in one go: the values of tile t - 1 (with its weights), then the scores of tile t, either may be
-  // missing.  Groups of instructions -- the channels' blocks of 16 keys; two steps of d of both halves of the keys -- whose operands are
-  // read from LDS kReadAhead groups before; the first ones' may be read apart (read_), before the barrier that the others have to wait for.
-  constexpr int kGroups = 4 + kSteps / 2, kPer = kOut > 4 ? kOut : 4, kReadAhead = DP > 128 ? 1 : 2;
-  bf16x8 f[kReadAhead + 1][kPer];
-  auto multiply = [&](auto had_, auto has_, auto read_, auto multiply_, int t, const bf16x8 (&weights)[4], f32x16v (&s)[2]) {
-    constexpr int kFirst = decltype(had_)::value ? 0 : 4, kLast = decltype(has_)::value ? kGroups : 4;
-    const int key_base = opaque(key_slot(t) + key_at), val_base = opaque(val_slot(t + kRing - 1) + val_at);
-    auto read = [&](auto g_) {
-      constexpr int g = decltype(g_)::value, at = g % (kReadAhead + 1);
-      if constexpr (g < 4) {
-#pragma unroll
-        for (int k = 0; k < kOut; ++k) f[at][k] = value(val_base, g, k);
+  uint32_t weights[16];   // pairs of bfloat16
+  constexpr int kScores = 2 * kSteps, kAll = kScores + 4 * kOut, kAhead = 4;
+  // One turn: the scores of tile t + 1 beside the weights of tile t, then the values of tile t beside the maximum of the new scores.  A matrix
+  // instruction takes as long as what vector instructions a pair of weights takes, and they run side by side; so they are laid out in turn, with the
+  // operands read from LDS kAhead instructions before.  had: there is a tile t; more: there is a tile t + 1, mask: of which some row does not see all.
+  auto turn = [&](auto had_, auto more_, auto mask_, int t, f32x16v (&cur)[2], f32x16v (&next)[2]) __attribute__((always_inline)) {
+    constexpr bool had = decltype(had_)::value, more = decltype(more_)::value, mask = decltype(mask_)::value;
+    constexpr int kFirst = more ? 0 : kScores, kLast = had ? kAll : kScores;
+    const int key_base = opaque(key_slot(t + 1) + key_at), val_base = opaque(val_slot(t + kRing) + val_at);
+    bf16x8 f[kAhead + 1];
+    auto read = [&](auto m_) __attribute__((always_inline)) {
+      constexpr int m = decltype(m_)::value, at = m % (kAhead + 1);
+      if constexpr (m < kScores) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
+        constexpr int u = m % kSteps, k = m / kSteps;
+        f[at] = *reinterpret_cast<const bf16x8*>(smem + (key_base ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kPitch);
       } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
-          const int u = 2 * (g - 4) + (i >> 1), k = i & 1;
-          f[at][i] = *reinterpret_cast<const bf16x8*>(smem + (key_base ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kPitch);
-        }
+        f[at] = value(val_base, (m - kScores) / kOut, (m - kScores) % kOut);
       }
     };
-    if constexpr (decltype(read_)::value)
-      static_for<kReadAhead>([&](auto i_) {
-        constexpr int g = kFirst + decltype(i_)::value;
-        if constexpr (g < kLast) read(std::integral_constant<int, g>{});
-      });
-    if constexpr (!decltype(multiply_)::value) return;
-    constexpr bool kBrings = TURNS && decltype(had_)::value && decltype(has_)::value;
     i32x4 vals{}, keys{};
-    if constexpr (kBrings) {
-      vals = tile_at(vals0, a.v_token, t + kRing - 2);
-      keys = tile_at(keys0, a.k_token, t + kRing - 1);
+    if constexpr (had && more) {
+      vals = tile_at(vals0, a.v_token, t + kRing - 1);
+      keys = tile_at(keys0, a.k_token, t + kRing);
     }
-    static_for<kLast - kFirst>([&](auto i_) {
-      constexpr int g = kFirst + decltype(i_)::value, at = g % (kReadAhead + 1);
+    static_for<kAhead>([&](auto i_) __attribute__((always_inline)) {
+      constexpr int m = kFirst + decltype(i_)::value;
+      if constexpr (m < kLast) read(std::integral_constant<int, m>{});
+    });
+    const int key0 = begin + (t + 1) * kTile;   // counted from the half wave's first key: what is left are constants
+    const int from_ = opaque(lo - key0 - 4 * h), to_ = opaque(hi - key0 - 4 * h);
+    float top[2] = {-INFINITY, -INFINITY};
+    auto highest = [&](auto e_) __attribute__((always_inline)) {
+      constexpr int e = decltype(e_)::value, k = e / 16, i = e % 16, at = 32 * k + 8 * (i >> 2) + (i & 3);
+      if constexpr (mask) next[k][i] = ((at >= from_) & (at < to_)) ? next[k][i] : -INFINITY;
+      top[e & 1] = fmaxf(top[e & 1], next[k][i]);
+    };
+    static_for<kLast - kFirst>([&](auto i_) __attribute__((always_inline)) {
+      constexpr int m = kFirst + decltype(i_)::value, at = m % (kAhead + 1);
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (g + kReadAhead < kLast) read(std::integral_constant<int, g + kReadAhead>{});
-      // slots of tiles that both halves have read are filled again beside the products, a request at a time: several would wait for each other
-      constexpr int i = (g * 2 * C::kRequests + kGroups - 1) / kGroups;
-      if constexpr (kBrings && i < 2 * C::kRequests && i * kGroups / (2 * C::kRequests) == g) {
-        if constexpr (i < C::kRequests) bring_one(vals, vals0, a.v_token, val_off, t + kRing - 2, val_slot(t + kRing - 2), i);
-        else bring_one(keys, keys0, a.k_token, key_off, t + kRing - 1, key_slot(t + kRing - 1), i - C::kRequests);
+      if constexpr (m + kAhead < kLast) read(std::integral_constant<int, m + kAhead>{});
+      // slots of tiles that everybody has read are filled again, a request at a time: several would wait for each other
+      constexpr int n = (m * 2 * C::kRequests + kAll - 1) / kAll;
+      if constexpr (had && more && n < 2 * C::kRequests && n * kAll / (2 * C::kRequests) == m) {
+        if constexpr (n < C::kRequests) bring_one(vals, vals0, a.v_token, val_off, t + kRing - 1, val_slot(t + kRing - 1), n);
+        else bring_one(keys, keys0, a.k_token, key_off, t + kRing, key_slot(t + kRing), n - C::kRequests);
       }
-      if constexpr (g < 4) {
-#pragma unroll
-        for (int k = 0; k < kOut; ++k) acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at][k], weights[g], acc[k], 0, 0, 0);
+      if constexpr (m < kScores) {
+        constexpr int u = m % kSteps, k = m / kSteps;
+        if (u == 0) next[k] = f32x16v{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        next[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at], fq[u], next[k], 0, 0, 0);
       } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int u = 2 * (g - 4) + (i >> 1), k = i & 1;
-          if (u == 0) s[k] = f32x16v{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-          s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at][i], fq[u], s[k], 0, 0, 0);
-        }
+        constexpr int g = (m - kScores) / kOut, k = (m - kScores) % kOut;
+        acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[at], bf16x8_of(weights[4 * g], weights[4 * g + 1], weights[4 * g + 2], weights[4 * g + 3]), acc[k], 0, 0, 0);
+      }
+      if constexpr (had && m < kScores) {
+        constexpr int from = 16 * m / kScores, to = 16 * (m + 1) / kScores;
+        static_for<to - from>([&](auto j_) __attribute__((always_inline)) {
+          constexpr int w = from + decltype(j_)::value, k = w / 8, e = w % 8 * 2;
+          weights[w] = bf16_pair(exp2_fast(fmaf(cur[k][e], factor, -M)), exp2_fast(fmaf(cur[k][e + 1], factor, -M)));
+          sum[w & 3] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, weights[w]), ones, sum[w & 3], false);
+        });
+      } else if constexpr (more && m >= kScores) {
+        constexpr int from = 32 * (m - kScores) / (4 * kOut), to = 32 * (m + 1 - kScores) / (4 * kOut);
+        static_for<to - from>([&](auto j_) __attribute__((always_inline)) { highest(std::integral_constant<int, from + decltype(j_)::value>{}); });
       }
     });
     __builtin_amdgcn_sched_barrier(0);
-  };
-  // the weights of tile t; what has been summed so far is brought to their maximum
-  auto soften = [&](auto mask_, int t, f32x16v (&s)[2], bf16x8 (&weights)[4]) {
-    if constexpr (decltype(mask_)::value) {
-      const int key0 = begin + t * kTile;
-      // counted from the half wave's first key: what is left are constants
-      const int from_ = opaque(lo - key0 - 4 * h), to_ = opaque(hi - key0 - 4 * h);
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = 32 * k + 8 * (i >> 2) + (i & 3);
-          s[k][i] = ((at >= from_) & (at < to_)) ? s[k][i] : -INFINITY;
-        }
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[k][i]);
-    top *= factor;
-    if (__any(top > M + 8.f)) {
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = top > M + 8.f ? ceilf(top) : M, shrink = exp2_fast(M - next);
-      M = next;
+    if constexpr (!more) return;
+    if constexpr (!had) static_for<32>([&](auto e_) __attribute__((always_inline)) { highest(e_); });
+    // what has been summed so far is brought to the new maximum
+    float most = fmaxf(top[0], top[1]) * factor;
+    if (__any(most > M + 8.f)) {
+      most = fmaxf(most, __shfl_xor(most, 32));
+      const float to = most > M + 8.f ? ceilf(most) : M, shrink = exp2_fast(M - to);
+      M = to;
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum[i] *= shrink;
 #pragma unroll
       for (int k = 0; k < kOut; ++k) acc[k] *= shrink;
     }
+  };
+  // ... of the last tile: there are no scores beside its weights
+  auto last_weights = [&](f32x16v (&cur)[2]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[i] = bf16_pair(exp2_fast(fmaf(s[k][8 * u + 2 * i], factor, -M)), exp2_fast(fmaf(s[k][8 * u + 2 * i + 1], factor, -M)));
-          sum[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), ones, sum[i], false);
-        }
-        weights[2 * k + u] = bf16x8_of(w[0], w[1], w[2], w[3]);
-      }
-    // here, and not where they are used: behind the barrier they would stand before the wave's matrix instructions
-#pragma unroll
-    for (int g = 0; g < 4; ++g) asm volatile("" : "+v"(weights[g]));
+    for (int w = 0; w < 16; ++w) {
+      weights[w] = bf16_pair(exp2_fast(fmaf(cur[w / 8][w % 8 * 2], factor, -M)), exp2_fast(fmaf(cur[w / 8][w % 8 * 2 + 1], factor, -M)));
+      sum[w & 3] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, weights[w]), ones, sum[w & 3], false);
+    }
   };
 
   constexpr std::true_type yes;
@@ -345,72 +330,44 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     M = kNoScore;
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = 0.f;
-    f32x16v s[2];
-    bf16x8 weights[4];
+    f32x16v s0[2], s1[2];
     // asked for in the order K0, V0, K1, V1, ...
     bring_keys(0);
 #pragma unroll
-    for (int t = 0; t < (TURNS ? kRing - 1 : 0); ++t) {
+    for (int t = 0; t < kRing - 1; ++t) {
       bring_vals(t);
       bring_keys(t + 1);
     }
-    if constexpr (TURNS) {
-      // Phases: the first half of the waves multiplies in the even ones -- values of tile t - 1 and keys of tile t in phase 2 t -- and works
-      // out weights in the odd ones; the second half is a phase behind.
-      const bool second = wave >= C::kWaves / 2;
-      static_assert(2 * C::kRequests <= kGroups, "");
-      arrived(std::integral_constant<int, 2 * kRing - 2>{});
+    arrived(std::integral_constant<int, 2 * kRing - 2>{});
+    meet();
+    turn(no, yes, yes, -1, s0, s0);
+    // the values of tile t and the keys of the next are there, and everybody has those before them behind him
+    auto next_tiles = [&](int t) __attribute__((always_inline)) {
+      arrived(std::integral_constant<int, 2 * kRing - 4>{});
       meet();
-      if (second) {
-        arrived(std::integral_constant<int, 2 * kRing - 3>{});
-        meet();
-        if (careful) clean(0);
+      if (careful) clean(t);
+    };
+    int t = 0;
+    auto turns = [&](auto mask_, int to) __attribute__((always_inline)) {   // up to the scores of tile `to`
+      for (; t + 1 < to; t += 2) {
+        next_tiles(t);
+        turn(yes, yes, mask_, t, s0, s1);
+        next_tiles(t + 1);
+        turn(yes, yes, mask_, t + 1, s1, s0);
       }
-      multiply(no, yes, yes, yes, 0, weights, s);
-      auto until_weights = [&](auto mask_, auto last_, int t) {
-        // the values of tile t have to be there a phase before their turn
-        if (second) arrived(std::integral_constant<int, 2 * kRing - 4>{});
-        else arrived(std::integral_constant<int, 2 * kRing - 3>{});
-        meet();
-        if (careful && !second) clean(t);
-        soften(mask_, t, s, weights);
-        multiply(yes, std::integral_constant<bool, !decltype(last_)::value>{}, yes, no, t + 1, weights, s);
-        if (second) arrived(std::integral_constant<int, 2 * kRing - 5>{});
-        else arrived(std::integral_constant<int, 2 * kRing - 4>{});
-        meet();
-        if (careful && second && !decltype(last_)::value) clean(t + 1);
-      };
-      int t = 0;
-      for (; t < min(plain0, count - 1); ++t) {
-        until_weights(yes, no, t);
-        multiply(yes, yes, no, yes, t + 1, weights, s);
+      if (t < to) {
+        next_tiles(t);
+        turn(yes, yes, mask_, t, s0, s1);
+        s0[0] = s1[0], s0[1] = s1[1];
+        ++t;
       }
-      for (; t < min(plain1, count - 1); ++t) {
-        until_weights(no, no, t);
-        multiply(yes, yes, no, yes, t + 1, weights, s);
-      }
-      for (; t < count - 1; ++t) {
-        until_weights(yes, no, t);
-        multiply(yes, yes, no, yes, t + 1, weights, s);
-      }
-      until_weights(yes, yes, t);
-      multiply(yes, no, no, yes, count, weights, s);
-      if (!second) meet();
-    } else {
-      // all waves in step: tile t's values and the next one's keys are asked for when everybody has the slots' tiles behind him
-      for (int t = 0; t < count; ++t) {
-        arrived(std::integral_constant<int, 0>{});
-        meet();
-        bring_vals(t);
-        bring_keys(t + 1);
-        multiply(no, yes, yes, yes, t, weights, s);
-        soften(yes, t, s, weights);
-        arrived(std::integral_constant<int, 1>{});
-        meet();
-        if (careful) clean(t);
-        multiply(yes, no, yes, yes, t + 1, weights, s);
-      }
-    }
+    };
+    turns(yes, min(plain0 - 1, count - 1));
+    turns(no, min(plain1 - 1, count - 1));
+    turns(yes, count - 1);
+    next_tiles(t);
+    last_weights(s0);
+    turn(yes, no, no, t, s0, s1);
     arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
     if (careful) {
       add_cleaned();
@@ -447,23 +404,23 @@ __global__ __launch_bounds__((Prompt<DP, TURNS>::kThreads)) void prompt_kernel(P
     }
 }
 
-template <int DP, bool TURNS, bool DMA>
+template <int DP, int WAVES, bool DMA>
 bool prompt_form_launch(const PromptArgs& all, hipStream_t s) {
-  using C = Prompt<DP, TURNS>;
-  if (!lds_opt_in<prompt_kernel<DP, TURNS, DMA>>(C::kLds)) return false;
+  using C = Prompt<DP, WAVES>;
+  if (!lds_opt_in<prompt_kernel<DP, WAVES, DMA>>(C::kLds)) return false;
   PromptArgs a = all;
   a.tiles = (int)ceil_div((int64_t)a.max_n * a.group, C::kRows);
   // a launch has fewer than 2^32 threads
   const int64_t items = (int64_t)a.tiles * ceil_div((int64_t)a.b * a.hkv, 8) * 8, step = 1 << 22;
   for (int64_t first = 0; first < items; first += step)
-    prompt_kernel<DP, TURNS, DMA><<<(unsigned)std::min(step, items - first), C::kThreads, C::kLds, s>>>(a, first);
+    prompt_kernel<DP, WAVES, DMA><<<(unsigned)std::min(step, items - first), C::kThreads, C::kLds, s>>>(a, first);
   return true;
 }
-template <int DP, bool TURNS>
+template <int DP, int WAVES>
 bool prompt_launch(const PromptArgs& a, hipStream_t s) {
   const bool lines = (uintptr_t)a.K % 16 == 0 && (uintptr_t)a.V % 16 == 0 && a.k_token % 8 == 0 && a.k_head % 8 == 0 && a.v_token % 8 == 0 &&
                      a.v_head % 8 == 0 && a.k_token < (1 << 24) && a.v_token < (1 << 24);
-  return lines ? prompt_form_launch<DP, TURNS, true>(a, s) : prompt_form_launch<DP, TURNS, false>(a, s);
+  return lines ? prompt_form_launch<DP, WAVES, true>(a, s) : prompt_form_launch<DP, WAVES, false>(a, s);
 }
 
 }  // namespace
@@ -480,8 +437,8 @@ ptq_status prompt_attention_launch(const void* Q, int64_t q_token, int64_t q_hea
   a.scale = (float)(softmax_scale * 1.4426950408889634);
   a.t = (int)t, a.b = (int)b, a.hkv = (int)hkv, a.group = (int)(hq / hkv), a.d = (int)d, a.max_n = (int)max_n, a.causal = causal;
   a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
-  const bool launched = d <= 64 ? prompt_launch<64, true>(a, s) : d <= 96 ? prompt_launch<96, true>(a, s)
-                        : d <= 128 ? prompt_launch<128, true>(a, s) : prompt_launch<256, false>(a, s);
+  const bool launched = d <= 64 ? prompt_launch<64, 8>(a, s) : d <= 96 ? prompt_launch<96, 8>(a, s)
+                        : d <= 128 ? prompt_launch<128, 8>(a, s) : prompt_launch<256, 4>(a, s);
   if (!launched) return PTQ_ERR_HIP;
   PTQ_HIP_CHECK_LAUNCH();
   return PTQ_OK;
