@@ -45,9 +45,17 @@ struct Prompt {
   static constexpr int kThreads = 64 * WAVES, kWaves = WAVES, kRows = 32 * kWaves;
   static constexpr int kPitch = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;     // bytes of a key, or of a value
   static constexpr int kBytes = kTile * kPitch;
-  static constexpr int kRing = DP > 128 || WAVES < 8 ? 2 : 3;               // tiles of each in LDS
+  static constexpr bool kPairs = DP <= 128 && WAVES == 8;                   // a barrier for two tiles
+  static constexpr int kRing = kPairs ? 4 : 2;                              // tiles of each in LDS
   static constexpr int kLds = 2 * kRing * kBytes;
   static constexpr int kRequests = kBytes / 1024 / kWaves;                  // of 1024 bytes, of a wave for a tile
+};
+// what a turn (see there) has to do
+enum {
+  kHad = 1, kMore = 2,        // there is a tile t, a tile t + 1
+  kMask = 4,                  // some row does not see all of tile t + 1
+  kBrings = 8,                // it asks for the tiles that have their turn after those that are there
+  kBegun = 16, kBegins = 32   // its first operands have been read by the turn before; it reads the next turn's
 };
 // 16-byte chunk c of row `key` lies at c ^ turn
 template <int DP>
@@ -233,30 +241,39 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
   constexpr int kScores = 2 * kSteps, kAll = kScores + 4 * kOut, kAhead = 4;
   // One turn: the scores of tile t + 1 beside the weights of tile t, then the values of tile t beside the maximum of the new scores.  A matrix
   // instruction takes as long as what vector instructions a pair of weights takes, and they run side by side; so they are laid out in turn, with the
-  // operands read from LDS kAhead instructions before.  had: there is a tile t; more: there is a tile t + 1, mask: of which some row does not see all.
-  auto turn = [&](auto had_, auto more_, auto mask_, int t, f32x16v (&cur)[2], f32x16v (&next)[2]) __attribute__((always_inline)) {
-    constexpr bool had = decltype(had_)::value, more = decltype(more_)::value, mask = decltype(mask_)::value;
-    constexpr int kFirst = more ? 0 : kScores, kLast = had ? kAll : kScores;
+  // operands read from LDS kAhead instructions before.
+  bf16x8 f[kAhead + 1];
+  auto turn = [&](auto what_, int t, f32x16v (&cur)[2], f32x16v (&next)[2]) __attribute__((always_inline)) {
+    constexpr int what = decltype(what_)::value;
+    constexpr bool had = what & kHad, more = what & kMore, mask = what & kMask, brings = what & kBrings, begun = what & kBegun, begins = what & kBegins;
+    constexpr int kFirst = more ? 0 : kScores, kLast = had ? kAll : kScores, kSlot = begun ? kAll : 0;
     const int key_base = opaque(key_slot(t + 1) + key_at), val_base = opaque(val_slot(t + kRing) + val_at);
-    bf16x8 f[kAhead + 1];
+    const int key_base2 = opaque(key_slot(t + 2) + key_at);
     auto read = [&](auto m_) __attribute__((always_inline)) {
-      constexpr int m = decltype(m_)::value, at = m % (kAhead + 1);
-      if constexpr (m < kScores) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
-        constexpr int u = m % kSteps, k = m / kSteps;
-        f[at] = *reinterpret_cast<const bf16x8*>(smem + (key_base ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kPitch);
+      constexpr int m = decltype(m_)::value, at = (kSlot + m) % (kAhead + 1);
+      if constexpr (m < kScores || m >= kAll) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
+        constexpr int u = m % kAll % kSteps, k = m % kAll / kSteps;
+        f[at] = *reinterpret_cast<const bf16x8*>(smem + ((m < kAll ? key_base : key_base2) ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kPitch);
       } else {
         f[at] = value(val_base, (m - kScores) / kOut, (m - kScores) % kOut);
       }
     };
-    i32x4 vals{}, keys{};
-    if constexpr (had && more) {
-      vals = tile_at(vals0, a.v_token, t + kRing - 1);
-      keys = tile_at(keys0, a.k_token, t + kRing);
-    }
-    static_for<kAhead>([&](auto i_) __attribute__((always_inline)) {
-      constexpr int m = kFirst + decltype(i_)::value;
-      if constexpr (m < kLast) read(std::integral_constant<int, m>{});
+    // tiles that are asked for: values, keys, of one turn or two
+    constexpr int kTiles = !brings ? 0 : C::kPairs ? 4 : 2;
+    i32x4 tiles[4];
+    auto tile_of = [&](auto i_, auto&& f) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_)::value, pair = C::kPairs ? i >> 1 : 0;
+      if constexpr (i % 2 == 0) f(vals0, a.v_token, val_off, t + (C::kPairs ? 2 : kRing - 1) + pair, val_slot(t + (C::kPairs ? 2 : kRing - 1) + pair));
+      else f(keys0, a.k_token, key_off, t + (C::kPairs ? 3 : kRing) + pair, key_slot(t + (C::kPairs ? 3 : kRing) + pair));
+    };
+    static_for<kTiles>([&](auto i_) __attribute__((always_inline)) {
+      tile_of(i_, [&](const uint16_t* from, int64_t token, const auto&, int tile, int) __attribute__((always_inline)) { tiles[decltype(i_)::value] = tile_at(from, token, tile); });
     });
+    if constexpr (!begun)
+      static_for<kAhead>([&](auto i_) __attribute__((always_inline)) {
+        constexpr int m = kFirst + decltype(i_)::value;
+        if constexpr (m < kLast) read(std::integral_constant<int, m>{});
+      });
     const int key0 = begin + (t + 1) * kTile;   // counted from the half wave's first key: what is left are constants
     const int from_ = opaque(lo - key0 - 4 * h), to_ = opaque(hi - key0 - 4 * h);
     float top[2] = {-INFINITY, -INFINITY};
@@ -266,14 +283,16 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
       top[e & 1] = fmaxf(top[e & 1], next[k][i]);
     };
     static_for<kLast - kFirst>([&](auto i_) __attribute__((always_inline)) {
-      constexpr int m = kFirst + decltype(i_)::value, at = m % (kAhead + 1);
+      constexpr int m = kFirst + decltype(i_)::value, at = (kSlot + m) % (kAhead + 1);
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (m + kAhead < kLast) read(std::integral_constant<int, m + kAhead>{});
+      if constexpr (m + kAhead < kLast || begins) read(std::integral_constant<int, m + kAhead>{});
       // slots of tiles that everybody has read are filled again, a request at a time: several would wait for each other
-      constexpr int n = (m * 2 * C::kRequests + kAll - 1) / kAll;
-      if constexpr (had && more && n < 2 * C::kRequests && n * kAll / (2 * C::kRequests) == m) {
-        if constexpr (n < C::kRequests) bring_one(vals, vals0, a.v_token, val_off, t + kRing - 1, val_slot(t + kRing - 1), n);
-        else bring_one(keys, keys0, a.k_token, key_off, t + kRing, key_slot(t + kRing), n - C::kRequests);
+      constexpr int kRequests = kTiles * C::kRequests, n = (m * kRequests + kAll - 1) / kAll;
+      if constexpr (n < kRequests && n * kAll / (kRequests + !kRequests) == m) {
+        constexpr int i = n / C::kRequests;
+        tile_of(std::integral_constant<int, i>{}, [&](const uint16_t* from, int64_t token, const auto& off, int tile, int slot) __attribute__((always_inline)) {
+          bring_one(tiles[i], from, token, off, tile, slot, n % C::kRequests);
+        });
       }
       if constexpr (m < kScores) {
         constexpr int u = m % kSteps, k = m / kSteps;
@@ -319,8 +338,6 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
     }
   };
 
-  constexpr std::true_type yes;
-  constexpr std::false_type no;
 #pragma unroll 1
   for (bool careful = false;; careful = true) {
 #pragma unroll
@@ -331,43 +348,60 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = 0.f;
     f32x16v s0[2], s1[2];
-    // asked for in the order K0, V0, K1, V1, ...
     bring_keys(0);
+    constexpr int kPrologue = C::kPairs ? 2 : kRing - 1;
 #pragma unroll
-    for (int t = 0; t < kRing - 1; ++t) {
+    for (int t = 0; t < kPrologue; ++t) {
       bring_vals(t);
       bring_keys(t + 1);
     }
-    arrived(std::integral_constant<int, 2 * kRing - 2>{});
+    arrived(std::integral_constant<int, 2 * kPrologue>{});
     meet();
-    turn(no, yes, yes, -1, s0, s0);
-    // the values of tile t and the keys of the next are there, and everybody has those before them behind him
+    turn(std::integral_constant<int, kMore | kMask>{}, -1, s0, s0);
+    // What has its turn now -- in pairs: before every other turn -- is there, and everybody has what was before it behind him.
     auto next_tiles = [&](int t) __attribute__((always_inline)) {
-      arrived(std::integral_constant<int, 2 * kRing - 4>{});
+      arrived(std::integral_constant<int, 0>{});
       meet();
-      if (careful) clean(t);
-    };
-    int t = 0;
-    auto turns = [&](auto mask_, int to) __attribute__((always_inline)) {   // up to the scores of tile `to`
-      for (; t + 1 < to; t += 2) {
-        next_tiles(t);
-        turn(yes, yes, mask_, t, s0, s1);
-        next_tiles(t + 1);
-        turn(yes, yes, mask_, t + 1, s1, s0);
+      if (careful) {
+        clean(t);
+        if (C::kPairs) clean(t + 1);
       }
-      if (t < to) {
-        next_tiles(t);
-        turn(yes, yes, mask_, t, s0, s1);
+    };
+    int t = 0;   // even turns go from s0 to s1, odd ones back
+    if constexpr (C::kPairs) {
+      auto pairs = [&](auto mask_, int to) __attribute__((always_inline)) {   // up to the scores of tile `to`, which is even
+        constexpr int what = kHad | kMore | decltype(mask_)::value;
+        for (; t < to; t += 2) {
+          next_tiles(t);
+          turn(std::integral_constant<int, what | kBrings | kBegins>{}, t, s0, s1);
+          turn(std::integral_constant<int, what | kBegun>{}, t + 1, s1, s0);
+        }
+      };
+      const int last = (count - 1) & ~1;
+      pairs(std::integral_constant<int, kMask>{}, min(plain0 & ~1, last));
+      pairs(std::integral_constant<int, 0>{}, min((plain1 - 1) & ~1, last));
+      pairs(std::integral_constant<int, kMask>{}, last);
+      next_tiles(t);
+      if (t < count - 1) {
+        turn(std::integral_constant<int, kHad | kMore | kMask>{}, t, s0, s1);
         s0[0] = s1[0], s0[1] = s1[1];
         ++t;
       }
-    };
-    turns(yes, min(plain0 - 1, count - 1));
-    turns(no, min(plain1 - 1, count - 1));
-    turns(yes, count - 1);
-    next_tiles(t);
+    } else {
+      auto steps = [&](auto mask_, int to) __attribute__((always_inline)) {
+        for (; t < to; ++t) {
+          next_tiles(t);
+          turn(std::integral_constant<int, kHad | kMore | kBrings | decltype(mask_)::value>{}, t, s0, s1);
+          s0[0] = s1[0], s0[1] = s1[1];
+        }
+      };
+      steps(std::integral_constant<int, kMask>{}, min(plain0 - 1, count - 1));
+      steps(std::integral_constant<int, 0>{}, min(plain1 - 1, count - 1));
+      steps(std::integral_constant<int, kMask>{}, count - 1);
+      next_tiles(t);
+    }
     last_weights(s0);
-    turn(yes, no, no, t, s0, s1);
+    turn(std::integral_constant<int, kHad>{}, t, s0, s1);
     arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
     if (careful) {
       add_cleaned();
