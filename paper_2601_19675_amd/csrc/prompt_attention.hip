@@ -38,6 +38,7 @@ struct PromptArgs {
   float scale;                              // softmax_scale log2(e)
   int t, b, hkv, group, d, max_n, causal, window;
   int tiles;                                // of rows, of the longest prompt there may be
+  int ways;                                 // dies that share a group
 };
 
 template <int DP, int WAVES>
@@ -45,8 +46,7 @@ struct Prompt {
   static constexpr int kThreads = 64 * WAVES, kWaves = WAVES, kRows = 32 * kWaves;
   static constexpr int kPitch = DP <= 64 ? 128 : DP <= 128 ? 256 : 512;     // bytes of a key, or of a value
   static constexpr int kBytes = kTile * kPitch;
-  static constexpr bool kPairs = DP <= 128 && WAVES == 8;                   // a barrier for two tiles
-  static constexpr int kRing = kPairs ? 4 : 2;                              // tiles of each in LDS
+  static constexpr int kRing = 2;                                           // tiles of each in LDS
   static constexpr int kLds = 2 * kRing * kBytes;
   static constexpr int kRequests = kBytes / 1024 / kWaves;                  // of 1024 bytes, of a wave for a tile
 };
@@ -54,8 +54,6 @@ struct Prompt {
 enum {
   kHad = 1, kMore = 2,        // there is a tile t, a tile t + 1
   kMask = 4,                  // some row does not see all of tile t + 1
-  kBrings = 8,                // it asks for the tiles that have their turn after those that are there
-  kBegun = 16, kBegins = 32   // its first operands have been read by the turn before; it reads the next turn's
 };
 // 16-byte chunk c of row `key` lies at c ^ turn
 template <int DP>
@@ -73,18 +71,21 @@ __device__ __forceinline__ bf16x8 bf16x8_of(uint32_t a, uint32_t b, uint32_t c, 
 
 // DMA: rows of K and V begin at multiples of 16 bytes; otherwise they go through registers
 template <int DP, int WAVES, bool DMA>
-__global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) void prompt_kernel(PromptArgs a, int64_t first_item) {
+__global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : DP > 64 || !DMA ? 2 : 3) void prompt_kernel(PromptArgs a, int64_t first_item) {
   using C = Prompt<DP, WAVES>;
   constexpr int kSteps = DP / 16, kOut = DP / 32, kRing = C::kRing;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5;
 
-  // Groups (prompt, key head) go round the dies, so that a group's row tiles share its keys and values in one L2; the last rows, which see
-  // most, first.  (Consecutive workgroups of a die go to its shader engines in turn, however busy those are: they have to be alike.)
-  const int64_t block = first_item + blockIdx.x, idx = block >> 3, group = idx / a.tiles * 8 + (block & 7);
-  if (group >= (int64_t)a.b * a.hkv) return;
-  const int tile = a.tiles - 1 - (int)(idx % a.tiles), seq = (int)(group / a.hkv), head = (int)(group % a.hkv);
+  // Groups (prompt, key head) go round the dies, so that a group's row tiles share its keys and values in one L2; where there are too few of them for that,
+  // several dies share a group.  The last rows, which see most, first.  (Consecutive workgroups of a die go to its shader engines in turn,
+  // however busy those are, so neighbours have to be alike: with the groups next to each other, of which some are short, 1233 us in place of 925.)
+  const int64_t block = first_item + blockIdx.x, idx = block >> 3;
+  const int each = (a.tiles + a.ways - 1) / a.ways, nth = (int)(idx % each);
+  const int64_t unit = idx / each * 8 + (block & 7), group = unit / a.ways;
+  const int tile = a.tiles - 1 - (nth * a.ways + (int)(unit % a.ways)), seq = (int)(group / a.hkv), head = (int)(group % a.hkv);
+  if (group >= (int64_t)a.b * a.hkv || tile < 0) return;
   const int64_t from64 = a.cu[seq], to64 = a.cu[seq + 1];
   if (from64 < 0 || to64 > a.t || to64 <= from64) return;
   const int first = (int)from64, n = min((int)(to64 - from64), a.max_n), rows = n * a.group, row0 = tile * C::kRows;
@@ -245,35 +246,27 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
   bf16x8 f[kAhead + 1];
   auto turn = [&](auto what_, int t, f32x16v (&cur)[2], f32x16v (&next)[2]) __attribute__((always_inline)) {
     constexpr int what = decltype(what_)::value;
-    constexpr bool had = what & kHad, more = what & kMore, mask = what & kMask, brings = what & kBrings, begun = what & kBegun, begins = what & kBegins;
-    constexpr int kFirst = more ? 0 : kScores, kLast = had ? kAll : kScores, kSlot = begun ? kAll : 0;
+    constexpr bool had = what & kHad, more = what & kMore, mask = what & kMask;
+    constexpr int kFirst = more ? 0 : kScores, kLast = had ? kAll : kScores;
     const int key_base = opaque(key_slot(t + 1) + key_at), val_base = opaque(val_slot(t + kRing) + val_at);
-    const int key_base2 = opaque(key_slot(t + 2) + key_at);
     auto read = [&](auto m_) __attribute__((always_inline)) {
-      constexpr int m = decltype(m_)::value, at = (kSlot + m) % (kAhead + 1);
-      if constexpr (m < kScores || m >= kAll) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
-        constexpr int u = m % kAll % kSteps, k = m % kAll / kSteps;
-        f[at] = *reinterpret_cast<const bf16x8*>(smem + ((m < kAll ? key_base : key_base2) ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kPitch);
+      constexpr int m = decltype(m_)::value, at = m % (kAhead + 1);
+      if constexpr (m < kScores) {    // (turns of keys 32 apart are the same, and leave chunk bit 4 alone)
+        constexpr int u = m % kSteps, k = m / kSteps;
+        f[at] = *reinterpret_cast<const bf16x8*>(smem + (key_base ^ (32 * (u & 7))) + (u >> 3) * 256 + k * 32 * C::kPitch);
       } else {
         f[at] = value(val_base, (m - kScores) / kOut, (m - kScores) % kOut);
       }
     };
-    // tiles that are asked for: values, keys, of one turn or two
-    constexpr int kTiles = !brings ? 0 : C::kPairs ? 4 : 2;
-    i32x4 tiles[4];
-    auto tile_of = [&](auto i_, auto&& f) __attribute__((always_inline)) {
-      constexpr int i = decltype(i_)::value, pair = C::kPairs ? i >> 1 : 0;
-      if constexpr (i % 2 == 0) f(vals0, a.v_token, val_off, t + (C::kPairs ? 2 : kRing - 1) + pair, val_slot(t + (C::kPairs ? 2 : kRing - 1) + pair));
-      else f(keys0, a.k_token, key_off, t + (C::kPairs ? 3 : kRing) + pair, key_slot(t + (C::kPairs ? 3 : kRing) + pair));
-    };
-    static_for<kTiles>([&](auto i_) __attribute__((always_inline)) {
-      tile_of(i_, [&](const uint16_t* from, int64_t token, const auto&, int tile, int) __attribute__((always_inline)) { tiles[decltype(i_)::value] = tile_at(from, token, tile); });
+    i32x4 vals{}, keys{};   // the tiles that are asked for
+    if constexpr (had && more) {
+      vals = tile_at(vals0, a.v_token, t + kRing - 1);
+      keys = tile_at(keys0, a.k_token, t + kRing);
+    }
+    static_for<kAhead>([&](auto i_) __attribute__((always_inline)) {
+      constexpr int m = kFirst + decltype(i_)::value;
+      if constexpr (m < kLast) read(std::integral_constant<int, m>{});
     });
-    if constexpr (!begun)
-      static_for<kAhead>([&](auto i_) __attribute__((always_inline)) {
-        constexpr int m = kFirst + decltype(i_)::value;
-        if constexpr (m < kLast) read(std::integral_constant<int, m>{});
-      });
     const int key0 = begin + (t + 1) * kTile;   // counted from the half wave's first key: what is left are constants
     const int from_ = opaque(lo - key0 - 4 * h), to_ = opaque(hi - key0 - 4 * h);
     float top[2] = {-INFINITY, -INFINITY};
@@ -283,16 +276,14 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
       top[e & 1] = fmaxf(top[e & 1], next[k][i]);
     };
     static_for<kLast - kFirst>([&](auto i_) __attribute__((always_inline)) {
-      constexpr int m = kFirst + decltype(i_)::value, at = (kSlot + m) % (kAhead + 1);
+      constexpr int m = kFirst + decltype(i_)::value, at = m % (kAhead + 1);
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (m + kAhead < kLast || begins) read(std::integral_constant<int, m + kAhead>{});
+      if constexpr (m + kAhead < kLast) read(std::integral_constant<int, m + kAhead>{});
       // slots of tiles that everybody has read are filled again, a request at a time: several would wait for each other
-      constexpr int kRequests = kTiles * C::kRequests, n = (m * kRequests + kAll - 1) / kAll;
-      if constexpr (n < kRequests && n * kAll / (kRequests + !kRequests) == m) {
-        constexpr int i = n / C::kRequests;
-        tile_of(std::integral_constant<int, i>{}, [&](const uint16_t* from, int64_t token, const auto& off, int tile, int slot) __attribute__((always_inline)) {
-          bring_one(tiles[i], from, token, off, tile, slot, n % C::kRequests);
-        });
+      constexpr int n = (m * 2 * C::kRequests + kAll - 1) / kAll;
+      if constexpr (had && more && n < 2 * C::kRequests && n * kAll / (2 * C::kRequests) == m) {
+        if constexpr (n < C::kRequests) bring_one(vals, vals0, a.v_token, val_off, t + kRing - 1, val_slot(t + kRing - 1), n);
+        else bring_one(keys, keys0, a.k_token, key_off, t + kRing, key_slot(t + kRing), n - C::kRequests);
       }
       if constexpr (m < kScores) {
         constexpr int u = m % kSteps, k = m / kSteps;
@@ -348,58 +339,42 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : 2) vo
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = 0.f;
     f32x16v s0[2], s1[2];
+    // asked for in the order K0, V0, K1, V1, ...
     bring_keys(0);
-    constexpr int kPrologue = C::kPairs ? 2 : kRing - 1;
 #pragma unroll
-    for (int t = 0; t < kPrologue; ++t) {
+    for (int t = 0; t < kRing - 1; ++t) {
       bring_vals(t);
       bring_keys(t + 1);
     }
-    arrived(std::integral_constant<int, 2 * kPrologue>{});
+    arrived(std::integral_constant<int, 2 * kRing - 2>{});
     meet();
     turn(std::integral_constant<int, kMore | kMask>{}, -1, s0, s0);
-    // What has its turn now -- in pairs: before every other turn -- is there, and everybody has what was before it behind him.
+    // the values of tile t and the keys of the next are there, and everybody has those before them behind him
     auto next_tiles = [&](int t) __attribute__((always_inline)) {
-      arrived(std::integral_constant<int, 0>{});
+      arrived(std::integral_constant<int, 2 * kRing - 4>{});
       meet();
-      if (careful) {
-        clean(t);
-        if (C::kPairs) clean(t + 1);
-      }
+      if (careful) clean(t);
     };
-    int t = 0;   // even turns go from s0 to s1, odd ones back
-    if constexpr (C::kPairs) {
-      auto pairs = [&](auto mask_, int to) __attribute__((always_inline)) {   // up to the scores of tile `to`, which is even
-        constexpr int what = kHad | kMore | decltype(mask_)::value;
-        for (; t < to; t += 2) {
-          next_tiles(t);
-          turn(std::integral_constant<int, what | kBrings | kBegins>{}, t, s0, s1);
-          turn(std::integral_constant<int, what | kBegun>{}, t + 1, s1, s0);
-        }
-      };
-      const int last = (count - 1) & ~1;
-      pairs(std::integral_constant<int, kMask>{}, min(plain0 & ~1, last));
-      pairs(std::integral_constant<int, 0>{}, min((plain1 - 1) & ~1, last));
-      pairs(std::integral_constant<int, kMask>{}, last);
-      next_tiles(t);
-      if (t < count - 1) {
-        turn(std::integral_constant<int, kHad | kMore | kMask>{}, t, s0, s1);
+    int t = 0;
+    auto turns = [&](auto mask_, int to) __attribute__((always_inline)) {   // up to the scores of tile `to`
+      constexpr std::integral_constant<int, kHad | kMore | decltype(mask_)::value> what{};
+      for (; t + 1 < to; t += 2) {
+        next_tiles(t);
+        turn(what, t, s0, s1);
+        next_tiles(t + 1);
+        turn(what, t + 1, s1, s0);
+      }
+      if (t < to) {
+        next_tiles(t);
+        turn(what, t, s0, s1);
         s0[0] = s1[0], s0[1] = s1[1];
         ++t;
       }
-    } else {
-      auto steps = [&](auto mask_, int to) __attribute__((always_inline)) {
-        for (; t < to; ++t) {
-          next_tiles(t);
-          turn(std::integral_constant<int, kHad | kMore | kBrings | decltype(mask_)::value>{}, t, s0, s1);
-          s0[0] = s1[0], s0[1] = s1[1];
-        }
-      };
-      steps(std::integral_constant<int, kMask>{}, min(plain0 - 1, count - 1));
-      steps(std::integral_constant<int, 0>{}, min(plain1 - 1, count - 1));
-      steps(std::integral_constant<int, kMask>{}, count - 1);
-      next_tiles(t);
-    }
+    };
+    turns(std::integral_constant<int, kMask>{}, min(plain0 - 1, count - 1));
+    turns(std::integral_constant<int, 0>{}, min(plain1 - 1, count - 1));
+    turns(std::integral_constant<int, kMask>{}, count - 1);
+    next_tiles(t);
     last_weights(s0);
     turn(std::integral_constant<int, kHad>{}, t, s0, s1);
     arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
@@ -444,8 +419,11 @@ bool prompt_form_launch(const PromptArgs& all, hipStream_t s) {
   if (!lds_opt_in<prompt_kernel<DP, WAVES, DMA>>(C::kLds)) return false;
   PromptArgs a = all;
   a.tiles = (int)ceil_div((int64_t)a.max_n * a.group, C::kRows);
+  const int64_t groups = (int64_t)a.b * a.hkv;
+  a.ways = 1;
+  while (a.ways < 8 && ceil_div(groups * a.ways, 8) * 8 * 20 > groups * a.ways * 21) a.ways *= 2;   // a twentieth of the dies' time idle at most
   // a launch has fewer than 2^32 threads
-  const int64_t items = (int64_t)a.tiles * ceil_div((int64_t)a.b * a.hkv, 8) * 8, step = 1 << 22;
+  const int64_t items = ceil_div(a.tiles, a.ways) * ceil_div(groups * a.ways, 8) * 8, step = 1 << 22;
   for (int64_t first = 0; first < items; first += step)
     prompt_kernel<DP, WAVES, DMA><<<(unsigned)std::min(step, items - first), C::kThreads, C::kLds, s>>>(a, first);
   return true;
@@ -471,8 +449,8 @@ ptq_status prompt_attention_launch(const void* Q, int64_t q_token, int64_t q_hea
   a.scale = (float)(softmax_scale * 1.4426950408889634);
   a.t = (int)t, a.b = (int)b, a.hkv = (int)hkv, a.group = (int)(hq / hkv), a.d = (int)d, a.max_n = (int)max_n, a.causal = causal;
   a.window = (int)std::min<int64_t>(window, INT32_MAX / 2);
-  const bool launched = d <= 64 ? prompt_launch<64, 8>(a, s) : d <= 96 ? prompt_launch<96, 8>(a, s)
-                        : d <= 128 ? prompt_launch<128, 8>(a, s) : prompt_launch<256, 4>(a, s);
+  const bool launched = d <= 64 ? prompt_launch<64, 4>(a, s) : d <= 96 ? prompt_launch<96, 4>(a, s)
+                        : d <= 128 ? prompt_launch<128, 4>(a, s) : prompt_launch<256, 4>(a, s);
   if (!launched) return PTQ_ERR_HIP;
   PTQ_HIP_CHECK_LAUNCH();
   return PTQ_OK;
