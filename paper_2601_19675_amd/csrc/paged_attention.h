@@ -37,8 +37,9 @@ struct AttendArgs {
   // through what is behind them
   const int32_t *cu_groups, *shared;
   int groups, max_shared;
+  const float *pre_part, *pre_ml;        // the rows form's: where the chunk form has left its parts
   float *alone, *alone_ml;               // [token][head][d] and [2]: parts of tiles of rows that a share has all of
-  int2* where;                           // [token][head]: the row of part and ml that has the first part (-1: alone has it), and how many there are
+  int2* where;                           // [token][head]: the row of pre_part and pre_ml that has the first part (-1: alone has it), and how many there are
 };
 
 // a sequence's queries and keys

@@ -50,6 +50,28 @@ __device__ __forceinline__ Sequence own_of(const AttendArgs& a, int s) {
   if constexpr (SHARED) q.begin = min(max(q.begin, shared_of(a, s)), q.end);
   return q;
 }
+// The parts that a (token, head) has of its prefix: where row p of them is.
+struct PrefixParts {
+  const float *part, *ml;
+  int64_t first;
+  int step, most, parts;
+  __device__ __forceinline__ int64_t row(int p) const { return p == 0 ? first : min(first + (2 * p - 1) * (int64_t)step, (int64_t)most); }
+};
+__device__ __forceinline__ PrefixParts prefix_parts(const AttendArgs& a, int seq, int64_t at) {
+  PrefixParts r{a.alone, a.alone_ml, at, 0, INT32_MAX, 0};
+  if (shared_of(a, seq) == 0) return r;
+  const int2 where = a.where[at];
+  if (where.x >= 0) {
+    r.part = a.pre_part;
+    r.ml = a.pre_ml;
+    r.step = a.slot_rows;
+    // (where sequences do not lie one after the other, nobody may have written `where`: whatever it holds, what is read is part of the workspace)
+    r.most = 2 * kChunkShares * a.slot_rows - 1;
+    r.first = min(where.x, r.most);
+  }
+  r.parts = where.x < 0 ? 1 : min(max(where.y, 0), kChunkShares);
+  return r;
+}
 struct __attribute__((packed, aligned(4))) Four { float e[4]; };
 // 2^-e, by its bits: those of 1, and -2^23 times e (which the compiler makes two instructions)
 __device__ __forceinline__ float power_below(int e) {
@@ -482,6 +504,42 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
       for (int j = 0; j < 4; ++j) o[j] *= inv;
     }
     const int tok = q.first + row / a.group, h = head * a.group + row % a.group;
+    if constexpr (SHARED) {
+      if (a.splits == 1) {   // all there is of the sequence's own keys: the prefix's parts join them here, sixteen at a time
+        const PrefixParts pre = prefix_parts(a, seq, (int64_t)tok * a.hq + h);
+        for (int p0 = 0; p0 < pre.parts; p0 += 16) {
+          f32x4 v[16];
+          f32x2 ml[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int64_t at = pre.row(min(p0 + j, pre.parts - 1));
+            v[j] = *reinterpret_cast<const f32x4*>(pre.part + at * a.d + c);
+            ml[j] = *reinterpret_cast<const f32x2*>(pre.ml + 2 * at);
+          }
+          float next = top;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) next = fmaxf(next, ml[j][0]);
+          const float before = exp2_fast(top - next) * sum;
+          float w[16], all = before;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            w[j] = p0 + j < pre.parts ? exp2_fast(ml[j][0] - next) * ml[j][1] : 0.f;
+            all += w[j];
+          }
+          const float inv = all == 0.f ? 0.f : 1.f / all;   // a row that has seen nothing: zeros
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            o[i] *= before * inv;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i] += (w[j] * inv) * v[j][i];
+          }
+          top = next;
+          sum = all;
+        }
+        store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, o);
+        continue;
+      }
+    }
     if (SHARED || !alone) {
       const int64_t at = ((int64_t)part * a.t + tok) * a.hq + h;
       *reinterpret_cast<f32x4*>(a.part + at * a.d + c) = f32x4{o[0], o[1], o[2], o[3]};
@@ -553,26 +611,17 @@ __global__ __launch_bounds__(64) void attend_join_kernel(AttendArgs a) {
 }
 
 // Joins the parts of a (token, head) that shares a prefix: those of the prefix, then those of what is behind it.  As above.
-__global__ __launch_bounds__(64) void shared_join_kernel(AttendArgs pre, AttendArgs a) {
+__global__ __launch_bounds__(64) void shared_join_kernel(AttendArgs a) {
   const int tok = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, c = lane * 4;
   const int seq = last_not_above(a.cu_q, 0, a.b, tok);
   const Sequence q = sequence_of(a, seq);
   if (tok < q.first || tok - q.first >= min(q.queries, a.max_q)) return;
   const int64_t first = (int64_t)tok * a.hq + h, step = (int64_t)a.t * a.hq;
-  int2 where = shared_of(a, seq) > 0 ? pre.where[first] : int2{0, 0};
-  // (where sequences do not lie one after the other, nobody may have written it: whatever it holds, what is read is part of the workspace)
-  const int most = 2 * kChunkShares * pre.slot_rows;
-  where = int2{min(max(where.x, -1), most - 1), min(max(where.y, 0), kChunkShares)};
-  const int of_prefix = where.y, parts = of_prefix + (a.splits > 1 ? a.parts[tok] : 1);
-  // the row of part p, and whose
-  auto row_of = [&](int p) { return p >= of_prefix ? first + (p - of_prefix) * step : where.x < 0 ? first : (int64_t)min(where.x + (p > 0 ? 2 * p - 1 : 0) * pre.slot_rows, most - 1); };
-  auto ml_of = [&](int p) {
-    return *reinterpret_cast<const f32x2*>((p >= of_prefix ? a.ml : where.x < 0 ? pre.alone_ml : pre.ml) + 2 * row_of(p));
-  };
-  const int cc = c < a.d ? c : 0;
-  auto part_of = [&](int p) {
-    return *reinterpret_cast<const f32x4*>((p >= of_prefix ? a.part : where.x < 0 ? pre.alone : pre.part) + row_of(p) * a.d + cc);
-  };
+  const PrefixParts pre = prefix_parts(a, seq, first);
+  const int parts = pre.parts + a.parts[tok], cc = c < a.d ? c : 0;
+  auto row_of = [&](int p) { return p < pre.parts ? pre.row(p) : first + (p - pre.parts) * step; };
+  auto ml_of = [&](int p) { return *reinterpret_cast<const f32x2*>((p < pre.parts ? pre.ml : a.ml) + 2 * row_of(p)); };
+  auto part_of = [&](int p) { return *reinterpret_cast<const f32x4*>((p < pre.parts ? pre.part : a.part) + row_of(p) * a.d + cc); };
   float top = kNoScore, sum = 0.f;
   for (int s = lane; s < parts; s += 64) top = fmaxf(top, ml_of(s)[0]);
 #pragma unroll
@@ -756,13 +805,18 @@ ptq_status paged_attention_shared_launch(const void* Q, int64_t q_token, int64_t
   pre.where = reinterpret_cast<int2*>(pre.alone_ml + 2 * rows);
   a.parts = reinterpret_cast<int*>(pre.where + rows);
   pre.splits = 2;
-  pre.slot_rows = (int)p.slot_rows;
-  a.splits = max_kv < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)p.splits;
+  a.slot_rows = pre.slot_rows = (int)p.slot_rows;
+  a.pre_part = pre.part, a.pre_ml = pre.ml;
+  a.alone = pre.alone, a.alone_ml = pre.alone_ml, a.where = pre.where;
+  // What is behind the prefixes is seldom long, and with one workgroup to a sequence and key head the parts join there: 13 us and no second kernel in place of
+  // 42 and 12 (64 sequences, 8 key heads, 146 to 730 keys behind a prefix).  The difference of the two bounds says how long it may be.
+  const int64_t own = max_kv - a.max_shared;
+  a.splits = own < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)p.splits;
   a.least_share = a.splits > 1 ? (int)std::max<int64_t>(2, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
   const ptq_status rc = paged_attention_prefix_launch(pre, bits, s);
   if (rc != PTQ_OK) return rc;
   if (!rows_launch_any<true>(a, bits, s)) return PTQ_ERR_HIP;
-  shared_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(pre, a);
+  if (a.splits > 1) shared_join_kernel<<<dim3((unsigned)t, (unsigned)hq), 64, 0, s>>>(a);
   PTQ_HIP_CHECK_LAUNCH();
   return PTQ_OK;
 }

@@ -44,6 +44,9 @@ constexpr int kTile = 64;   // keys
 // Workgroups that share the work, one to a compute unit.  It is counted in tiles of keys, and what comes before and after an item's
 // tiles (queries and first codes 13000 cycles, outputs 8000, a tile 3200 to 5900) as kStart of them.
 constexpr int kShares = kChunkShares, kStart = 4, kLeastShare = 2 * kStart;
+// Of prefixes, whose tiles of rows are few and alike, tiles of keys alone count, and where there are shares enough none has two items, each of which
+// takes its beginning and end of 10 us.  us, so | as above: 8 items of 1000 keys 13 | 27, of 32768 keys 60 | 74
+constexpr int kLeastPrefixShare = 2;
 constexpr int kValueLift = 4;         // V' = 2^kValueLift vs (code - zero)
 constexpr int kMetas = 8, kMetaAhead = 4;   // tiles whose Meta is in LDS, and how far before its turn it is brought there
 
@@ -120,7 +123,7 @@ __device__ __forceinline__ int item_work(const AttendArgs& a, int seq, int tile)
   if (tile * ROWS >= rows_of<SHARED>(a, q)) return 0;
   int begin, end;
   span_of<ROWS, SHARED>(a, q, tile, begin, end);
-  return kStart + max(0, end - begin + kTile - 1) / kTile;
+  return (SHARED ? 0 : kStart) + max(0, end - begin + kTile - 1) / kTile;
 }
 
 template <int BITS, int DP, bool SHARED>
@@ -133,18 +136,40 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
 
   // the workgroup's share: `left` pieces of work from piece `off` of an item on; `at` is the item's place in the order of all
   int seq, head, tile, off = 0, left = INT32_MAX, at = 0, each = 1;
+  bool padded = false;   // no share has more than one item
   int4 begun{0, 0, 0, 0};   // parts of the item that this share begins and does not end (0: there is none); its sequence, key head, tile
   int4* const begun_at = reinterpret_cast<int4*>(a.parts) + (blockIdx.x & 7) * (kShares / 8) + (blockIdx.x >> 3);
   if (a.splits > 1) {
     // consecutive shares on one die, where they find each other's codes in the L2
     const int sequences = SHARED ? a.groups : a.b, pairs = sequences * tiles, lane = threadIdx.x & 63;
-    int total = 0;   // of one key head
-    for (int p0 = 0; p0 < pairs; p0 += kWave) total += p0 + lane < pairs ? item_work<C::kRows, SHARED>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+    int total = 0, work = 0;   // of one key head; the lane's of the last 64 tiles of rows
+    for (int p0 = 0; p0 < pairs; p0 += kWave) {
+      work = p0 + lane < pairs ? item_work<C::kRows, SHARED>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+      total += work;
+    }
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o);
     total = __builtin_amdgcn_readfirstlane(total);
-    const int all = total * a.c.heads;
-    each = max(kLeastShare, (all + kShares - 1) / kShares);
+    int all = total * a.c.heads;
+    each = max(SHARED ? kLeastPrefixShare : kLeastShare, (all + kShares - 1) / kShares);
+    if constexpr (SHARED) {
+      // an item counts for whole shares of its own if there are so many
+      for (int tries = 0; tries < 16 && pairs <= kWave && !padded; ++tries) {
+        int shares = (work + each - 1) / each;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) shares += __shfl_xor(shares, o);
+        shares = __builtin_amdgcn_readfirstlane(shares);
+        padded = (int64_t)shares * a.c.heads <= kShares;
+        if (padded) {
+          work = (work + each - 1) / each * each;
+          total = shares * each;
+          all = total * a.c.heads;
+        } else {
+          each += each / 8 + 1;
+        }
+      }
+      if (!padded) each = max(kLeastPrefixShare, (all + kShares - 1) / kShares);
+    }
     const int64_t mine = ((blockIdx.x & 7) * (kShares / 8) + (blockIdx.x >> 3)) * (int64_t)each;
     if (mine >= all) {
       if (threadIdx.x == 0) *begun_at = begun;
@@ -155,7 +180,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     const int within = (int)mine % total;
     int before = 0;
     for (int p0 = 0;; p0 += kWave) {   // the first item that reaches past `within`
-      const int n = p0 + lane < pairs ? item_work<C::kRows, SHARED>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
+      const int n = SHARED && pairs <= kWave ? work : p0 + lane < pairs ? item_work<C::kRows, SHARED>(a, (p0 + lane) / tiles, (p0 + lane) % tiles) : 0;
       int upto = n;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
@@ -200,10 +225,11 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   // the keys that some row of the workgroup sees, and those of them in this share
   int lo, hi, lo_a, hi_a, lo_b, hi_b, begin, end;
   span_of<C::kRows, SHARED>(a, q, tile, begin, end);
-  const int whole = kStart + max(0, end - begin + kTile - 1) / kTile, take = min(whole - off, left);
+  constexpr int start = SHARED ? 0 : kStart;
+  const int whole = start + max(0, end - begin + kTile - 1) / kTile, take = min(whole - off, left);
   const bool alone = take == whole;
-  end = min(end, begin + max(0, off + take - kStart) * kTile);
-  begin += max(0, off - kStart) * kTile;
+  end = min(end, begin + max(0, off + take - start) * kTile);
+  begin += max(0, off - start) * kTile;
   const int count = end > begin ? (end - begin + kTile - 1) / kTile : 0;
   // ... and those that the wave's rows see: some of them [lo_a, hi_b), all of them [lo_b, hi_a)
   const int wrow = row0 + 32 * wave;
@@ -261,7 +287,9 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
     // the row's own sequence says what of the prefix it sees
     lo = 0, hi = 0;
     if (live) {
-      const int own = last_not_above(a.cu_q, a.cu_groups[seq], a.cu_groups[seq + 1], token);
+      const int from = a.cu_groups[seq], to = a.cu_groups[seq + 1];
+      int own = min(from + token - q.first, to - 1);   // where each has one token
+      if (a.cu_q[own] != token || a.cu_q[own + 1] != token + 1) own = last_not_above(a.cu_q, from, to, token);
       const Sequence o = sequence_of(a, own);
       int unused;
       visible(a, o, token - o.first, unused, hi);
@@ -744,7 +772,7 @@ __global__ __launch_bounds__(Chunk<DP>::kThreads) void attend_chunk_kernel(Atten
   if (a.splits == 1) return;
   if (off == 0 && !alone) begun = int4{(at + whole - 1) / each - at / each + 1, seq, head, tile};
   left -= take;
-  if (left <= 0) break;
+  if (left <= 0 || padded) break;
   at += whole;
   off = 0;
   ++tile;
