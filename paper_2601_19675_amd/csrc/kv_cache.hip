@@ -77,13 +77,13 @@ __global__ __launch_bounds__(256) void kv_write_kernel(WriteArgs a) {
     constexpr int i = decltype(i_)::value;
     float v[8];
     run_to_f32<DT, 8>(x[i], c, a.d, v);
-    uint32_t w[BITS / 4];
-    row_codes_of<BITS, i>(v, grid, w);
+    uint32_t u[8];
+    row_codes_of<BITS, i>(v, grid, u);
     if ((uint32_t)slot[i] < places && c < a.d) {
       const int64_t row = kv_row(rows, (uint32_t)slot[i] >> a.c.page_shift, slot[i] & ((1 << a.c.page_shift) - 1));
       uint8_t* out = a.c.codes + row * a.c.row_bytes + lane * BITS;
-      if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out) = uint2{w[0], w[1]};
-      else *reinterpret_cast<uint32_t*>(out) = w[0];
+      if constexpr (BITS == 8) *reinterpret_cast<uint2*>(out) = uint2{four_bytes(u[0], u[1], u[2], u[3]), four_bytes(u[4], u[5], u[6], u[7])};
+      else *reinterpret_cast<uint32_t*>(out) = four_bytes(u[0], u[4], u[1], u[5]) | (four_bytes(u[2], u[6], u[3], u[7]) << 4);
     }
   });
 }

@@ -66,35 +66,34 @@ __device__ __forceinline__ RowGrid row_grid(const RowExtremes& e) {
   return RowGrid{scale, z[0], finite ? inv : 0.f, finite, odd};
 }
 
-// Codes of eight values of the row whose grid lane I of every four lanes has, as they are stored.
-template <int BITS, int I>
-__device__ __forceinline__ void row_codes_of(const float (&v)[8], const RowGrid& g, uint32_t (&w)[BITS / 4]) {
+// Codes of N values of the row whose grid lane I of every four lanes has: the low bits of u.
+template <int BITS, int I, int N>
+__device__ __forceinline__ void row_codes_of(const float (&v)[N], const RowGrid& g, uint32_t (&code)[N]) {
   constexpr double kTop = (1 << BITS) - 1;
   const float inv_i = of_four<I>(g.inv), z_i = of_four<I>(g.zero);
   // 1.5 2^23 + a whole number has that number in its low bits, and adding it rounds there: code = rne(x inv + zero), which is rne(x / scale) + zero
   // as long as x inv + zero, off by less than 2^-14 (see whole_codes; the sum adds 2^-17), is not that close to a middle
   constexpr float kWhole = 12582912.f;
   const float from = z_i + kWhole;
-  float u[8], far = 0.f;
+  float u[N], far = 0.f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < N; ++e) {
     u[e] = fmaf(v[e], inv_i, from);
     far = fmaxf(far, fabsf(fmaf(v[e], inv_i, from - u[e])));
   }
   if (__any(far > 0.5f - 0x1p-14f) | g.odd) {
     const float s = of_four<I>(g.scale), good = of_four<I>(g.finite ? 1.f : 0.f);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < N; ++e)
       u[e] = kWhole + (good != 0.f ? fminf((float)rint((double)v[e] / (double)s) + z_i, (float)kTop) : 0.f);
   }
-  auto byte_pair = [&](int e0, int e1) { return __builtin_amdgcn_perm(__float_as_uint(u[e1]), __float_as_uint(u[e0]), 0x0c0c0400u); };
-  auto bytes = [&](int e0, int e1, int e2, int e3) { return __builtin_amdgcn_perm(byte_pair(e2, e3), byte_pair(e0, e1), 0x05040100u); };
-  if constexpr (BITS == 8) {
-    w[0] = bytes(0, 1, 2, 3);
-    w[1] = bytes(4, 5, 6, 7);
-  } else {
-    w[0] = bytes(0, 4, 1, 5) | (bytes(2, 6, 3, 7) << 4);
-  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) code[e] = __float_as_uint(u[e]);
+}
+// the low bytes of four numbers
+__device__ __forceinline__ uint32_t byte_pair(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x0c0c0400u); }
+__device__ __forceinline__ uint32_t four_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(byte_pair(c, d), byte_pair(a, b), 0x05040100u);
 }
 
 }  // namespace ptq

@@ -3,7 +3,7 @@
 //   y_a = scale (x_a cos - x_b sin),   y_b = scale (x_a sin + x_b cos),
 // alone (Y may be X), or with the keys going on into the paged cache in the same launch.
 //
-// Bound: bytes, each channel once in and out.  A thread has the same eight pairs of several heads of a token, so that cosines and sines are
+// Bound: bytes, each channel once in and out.  A thread has the same four pairs of several heads of a token, so that cosines and sines are
 // worked out once for all of them and stay in registers; consecutive threads have a head's row side by side, and consecutive workgroups
 // the heads of the same tokens.  All of it is float64, which runs at float32's rate here and hides behind the memory: what
 // is rounded to a key's type, and decides its codes, is the exact value but for 2^-50.
@@ -18,6 +18,7 @@ namespace ptq {
 namespace {
 
 constexpr int kHeadsAhead = 4;   // heads whose channels are on their way together
+constexpr int kPairs = 4;        // of a lane
 
 struct RotaryArgs {
   const void* X; void* Y;
@@ -28,36 +29,35 @@ struct RotaryArgs {
   double scale;
 };
 
-// Which two runs of eight channels a lane has, and whether they are pairs that turn (eight frequencies from 8 lane on; rot % 16 == 0).
-struct LaneRuns { int a, b; bool turns; };
+// Which two runs of four channels a lane has, and whether they are pairs that turn (four frequencies from 4 lane on; rot % 16 == 0).
+struct LaneRuns { int a, b; bool turns, apart; };   // apart: b is half of the turned channels behind a
 __device__ __forceinline__ LaneRuns lane_runs(int lane, int rot, int interleaved) {
-  if (interleaved) return LaneRuns{16 * lane, 16 * lane + 8, 16 * lane < rot};
-  if (16 * lane < rot) return LaneRuns{8 * lane, 8 * lane + rot / 2, true};
-  return LaneRuns{16 * lane, 16 * lane + 8, false};
+  const bool turns = 8 * lane < rot, apart = turns && !interleaved;
+  return LaneRuns{apart ? 4 * lane : 8 * lane, apart ? 4 * lane + rot / 2 : 8 * lane + 4, turns, apart};
 }
 // cosines and sines of the lane's pairs; those of a lane without are not used
-__device__ __forceinline__ void lane_angles(const LaneRuns& runs, int lane, int position, const double* freq, double scale, CosSin (&t)[8]) {
-  double f[8];
+__device__ __forceinline__ void lane_angles(const LaneRuns& runs, int lane, int position, const double* freq, double scale, CosSin (&t)[kPairs]) {
+  double f[kPairs];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) f[e] = freq[runs.turns ? 8 * lane + e : 0];
+  for (int e = 0; e < kPairs; ++e) f[e] = freq[runs.turns ? kPairs * lane + e : 0];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) t[e] = cos_sin(position, f[e], scale);
+  for (int e = 0; e < kPairs; ++e) t[e] = cos_sin(position, f[e], scale);
 }
-__device__ __forceinline__ void turn_runs(float (&u)[8], float (&v)[8], const LaneRuns& runs, int interleaved, const CosSin (&t)[8]) {
+__device__ __forceinline__ void turn_runs(float (&u)[kPairs], float (&v)[kPairs], const LaneRuns& runs, const CosSin (&t)[kPairs]) {
   if (!runs.turns) return;
-  if (interleaved) {
+  if (runs.apart) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      turn(u[2 * e], u[2 * e + 1], t[e]);
-      turn(v[2 * e], v[2 * e + 1], t[4 + e]);
-    }
+    for (int e = 0; e < kPairs; ++e) turn(u[e], v[e], t[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) turn(u[e], v[e], t[e]);
+    for (int e = 0; e < 2; ++e) {
+      turn(u[2 * e], u[2 * e + 1], t[e]);
+      turn(v[2 * e], v[2 * e + 1], t[2 + e]);
+    }
   }
 }
 
-// LANES lanes to a row of up to 16 LANES channels (d % 16 == 0, rot % 16 == 0); workgroup (tile, slice)
+// LANES lanes to a row of up to 8 LANES channels (d % 16 == 0, rot % 16 == 0); workgroup (tile, slice)
 template <int DT, int LANES>
 __device__ __forceinline__ void rotary_rows(const RotaryArgs& a, int tile, int slice) {
   constexpr int kTokens = 256 / LANES;
@@ -68,27 +68,27 @@ __device__ __forceinline__ void rotary_rows(const RotaryArgs& a, int tile, int s
   const ST* X = static_cast<const ST*>(a.X) + safe * a.x_token;
   ST* Y = static_cast<ST*>(a.Y) + safe * a.y_token;
   const int position = a.positions[safe];
-  CosSin angles[8];
+  CosSin angles[kPairs];
   bool ready = false;
   for (int h0 = first; h0 < last; h0 += kHeadsAhead) {
-    Run<DT, 8> x[kHeadsAhead][2];
+    Run<DT, 4> x[kHeadsAhead][2];
 #pragma unroll
     for (int i = 0; i < kHeadsAhead; ++i) {
       const ST* row = X + min(h0 + i, last - 1) * a.x_head;
-      x[i][0] = load_run<DT, 8, false>(row, runs.a, a.d);
-      x[i][1] = load_run<DT, 8, false>(row, runs.b, a.d);
+      x[i][0] = load_run<DT, 4, false>(row, runs.a, a.d);
+      x[i][1] = load_run<DT, 4, false>(row, runs.b, a.d);
     }
     if (!ready) lane_angles(runs, lane, position, a.freq, a.scale, angles);
     ready = true;
 #pragma unroll
     for (int i = 0; i < kHeadsAhead; ++i) {
-      float u[8], v[8];
-      run_to_f32<DT, 8>(x[i][0], runs.a, a.d, u);
-      run_to_f32<DT, 8>(x[i][1], runs.b, a.d, v);
-      turn_runs(u, v, runs, a.interleaved, angles);
+      float u[4], v[4];
+      run_to_f32<DT, 4>(x[i][0], runs.a, a.d, u);
+      run_to_f32<DT, 4>(x[i][1], runs.b, a.d, v);
+      turn_runs(u, v, runs, angles);
       if (token < a.t && h0 + i < last) {
-        store_run<DT, 8, false>(Y + (h0 + i) * a.y_head, runs.a, a.d, u);
-        store_run<DT, 8, false>(Y + (h0 + i) * a.y_head, runs.b, a.d, v);
+        store_run<DT, 4, false>(Y + (h0 + i) * a.y_head, runs.a, a.d, u);
+        store_run<DT, 4, false>(Y + (h0 + i) * a.y_head, runs.b, a.d, v);
       }
     }
   }
@@ -161,7 +161,6 @@ __device__ __forceinline__ void cache_rows(const RotaryCacheArgs& a, int tile, i
   using ST = typename StoredType<DT>::type;
   const int lane = threadIdx.x % LANES, token = tile * kTokens + threadIdx.x / LANES, safe = min(token, a.q.t - 1);
   LaneRuns runs = lane_runs(lane, a.q.rot, a.q.interleaved);
-  if (which) runs.turns = false;
   const int first = slice * a.per, last = min(a.c.heads, first + a.per);
   const ST* X = static_cast<const ST*>(which ? a.X[1] : a.X[0]) + safe * (which ? a.token[1] : a.token[0]);
   const int64_t stride = which ? a.head[1] : a.head[0];
@@ -169,30 +168,30 @@ __device__ __forceinline__ void cache_rows(const RotaryCacheArgs& a, int tile, i
   const bool there = (uint32_t)slot < (uint32_t)(a.c.pages << a.c.page_shift);
   const int place = there ? slot : 0;
   const uint32_t page = (uint32_t)place >> a.c.page_shift, offset = place & ((1 << a.c.page_shift) - 1);
-  CosSin angles[8];
+  CosSin angles[kPairs];
   bool ready = which != 0;
   for (int h0 = first; h0 < last; h0 += kHeadsAhead) {
-    Run<DT, 8> x[kHeadsAhead][2];
+    Run<DT, 4> x[kHeadsAhead][2];
 #pragma unroll
     for (int i = 0; i < kHeadsAhead; ++i) {
       const ST* row = X + min(h0 + i, last - 1) * stride;
-      x[i][0] = load_run<DT, 8, false>(row, runs.a, a.q.d);
-      x[i][1] = load_run<DT, 8, false>(row, runs.b, a.q.d);
+      x[i][0] = load_run<DT, 4, false>(row, runs.a, a.q.d);
+      x[i][1] = load_run<DT, 4, false>(row, runs.b, a.q.d);
     }
     if (!ready) lane_angles(runs, lane, position, a.q.freq, a.q.scale, angles);
     ready = true;
-    float v[kHeadsAhead][2][8];
+    float v[kHeadsAhead][2][4];
     RowExtremes most;
 #pragma unroll
     for (int i = 0; i < kHeadsAhead; ++i) {
-      run_to_f32<DT, 8>(x[i][0], runs.a, a.q.d, v[i][0]);
-      run_to_f32<DT, 8>(x[i][1], runs.b, a.q.d, v[i][1]);
-      turn_runs(v[i][0], v[i][1], runs, a.q.interleaved, angles);
+      run_to_f32<DT, 4>(x[i][0], runs.a, a.q.d, v[i][0]);
+      run_to_f32<DT, 4>(x[i][1], runs.b, a.q.d, v[i][1]);
+      if (!which) turn_runs(v[i][0], v[i][1], runs, angles);
       RowExtremes row;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
           v[i][k][e] = as_stored<DT>(v[i][k][e]);
           row.take(v[i][k][e]);
         }
@@ -209,17 +208,26 @@ __device__ __forceinline__ void cache_rows(const RotaryCacheArgs& a, int tile, i
     }
     static_for<kHeadsAhead>([&](auto i_) {
       constexpr int i = decltype(i_)::value;
-      uint32_t w[2][BITS / 4];
-      row_codes_of<BITS, i>(v[i][0], grid, w[0]);
-      row_codes_of<BITS, i>(v[i][1], grid, w[1]);
-      if (there && h0 + i < last && runs.a < a.q.d) {   // (d % 16 == 0: a lane has both of its runs or neither)
-        uint8_t* out = a.c.codes + row_at(h0 + i) * a.c.row_bytes;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          uint8_t* at = out + (k ? runs.b : runs.a) / 8 * BITS;
-          if constexpr (BITS == 8) *reinterpret_cast<uint2*>(at) = uint2{w[k][0], w[k][1]};
-          else *reinterpret_cast<uint32_t*>(at) = w[k][0];
+      uint32_t u[2][4];
+      row_codes_of<BITS, i>(v[i][0], grid, u[0]);
+      row_codes_of<BITS, i>(v[i][1], grid, u[1]);
+      const bool store = there && h0 + i < last && runs.a < a.q.d;   // (d % 16 == 0: a lane has both of its runs or neither)
+      uint8_t* out = a.c.codes + row_at(store ? h0 + i : first) * a.c.row_bytes;
+      if constexpr (BITS == 8) {
+        if (store) {
+          *reinterpret_cast<uint32_t*>(out + runs.a) = four_bytes(u[0][0], u[0][1], u[0][2], u[0][3]);
+          *reinterpret_cast<uint32_t*>(out + runs.b) = four_bytes(u[1][0], u[1][1], u[1][2], u[1][3]);
         }
+      } else {
+        // a word has eight codes: bytes 0 and 2 are of the first four, 1 and 3 of the others, which the lane has itself or the one beside it
+        auto half = [](const uint32_t (&c)[4]) {
+          return __builtin_amdgcn_perm(0, byte_pair(c[0], c[1]), 0x0c010c00u) | (__builtin_amdgcn_perm(0, byte_pair(c[2], c[3]), 0x0c010c00u) << 4);
+        };
+        const uint32_t ha = half(u[0]), hb = half(u[1]);
+        const bool second = lane & 1;
+        const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(second ? ha : hb), kDppSwapPairs, 0xf, 0xf, true);
+        const uint32_t low = !runs.apart || !second ? ha : other, high = !runs.apart ? hb : second ? hb : other;
+        if (store) *reinterpret_cast<uint32_t*>(out + (runs.apart && second ? runs.b - 4 : runs.a) / 2) = low | (high << 8);
       }
     });
   }
@@ -232,13 +240,13 @@ __global__ __launch_bounds__(256) void rotary_cache_kernel(RotaryCacheArgs a) {
   else cache_rows<DT, BITS, LANES>(a, tile, (part - a.q.slices) % a.slices, (part - a.q.slices) / a.slices);
 }
 
-int lanes_of(int64_t d) { return d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+int lanes_of(int64_t d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
 // Heads of a workgroup: as many as leave the device 2048 workgroups (eight to a compute unit), between one round of loads and eight of them.
 // (The angles of a round's heads take as long as turning one head.)
 int heads_per(int64_t tiles, int64_t heads) {
-  const int64_t most = std::max<int64_t>(1, tiles * heads / 2048);
-  return (int)std::min<int64_t>(heads, std::min<int64_t>(8 * kHeadsAhead, ceil_div(most, kHeadsAhead) * kHeadsAhead));
+  const int64_t most = std::min<int64_t>(8, ceil_div(std::max<int64_t>(1, tiles * heads / 2048), kHeadsAhead)), rounds = ceil_div(heads, kHeadsAhead);
+  return (int)(ceil_div(rounds, ceil_div(rounds, most)) * kHeadsAhead);   // as many as that, and alike
 }
 // tiles of a launch, which has fewer than 2^32 threads
 int64_t launch_tiles(int64_t slices) { return std::max<int64_t>(1, (1 << 23) / slices); }
@@ -264,9 +272,9 @@ void rotary_typed(const RotaryArgs& all, hipStream_t s) {
     a.Y = static_cast<ST*>(all.Y) + first * tokens * a.y_token;
     a.positions = all.positions + first * tokens;
     a.t = (int)std::min<int64_t>(n * tokens, all.t - first * tokens);
-    if (lanes == 4) rotary_kernel<DT, 4><<<grid, 256, 0, s>>>(a);
-    else if (lanes == 8) rotary_kernel<DT, 8><<<grid, 256, 0, s>>>(a);
-    else rotary_kernel<DT, 16><<<grid, 256, 0, s>>>(a);
+    if (lanes == 8) rotary_kernel<DT, 8><<<grid, 256, 0, s>>>(a);
+    else if (lanes == 16) rotary_kernel<DT, 16><<<grid, 256, 0, s>>>(a);
+    else rotary_kernel<DT, 32><<<grid, 256, 0, s>>>(a);
   }
 }
 
@@ -291,9 +299,9 @@ void rotary_cache_typed(const RotaryCacheArgs& all, hipStream_t s) {
     for (int i = 0; i < 2; ++i) a.X[i] = static_cast<const ST*>(all.X[i]) + at * a.token[i];
     a.q.t = (int)std::min<int64_t>(n * tokens, all.q.t - at);
     const unsigned grid = (unsigned)(n * each);
-    if (lanes == 4) rotary_cache_kernel<DT, BITS, 4><<<grid, 256, 0, s>>>(a);
-    else if (lanes == 8) rotary_cache_kernel<DT, BITS, 8><<<grid, 256, 0, s>>>(a);
-    else rotary_cache_kernel<DT, BITS, 16><<<grid, 256, 0, s>>>(a);
+    if (lanes == 8) rotary_cache_kernel<DT, BITS, 8><<<grid, 256, 0, s>>>(a);
+    else if (lanes == 16) rotary_cache_kernel<DT, BITS, 16><<<grid, 256, 0, s>>>(a);
+    else rotary_cache_kernel<DT, BITS, 32><<<grid, 256, 0, s>>>(a);
   }
 }
 
