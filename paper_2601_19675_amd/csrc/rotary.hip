@@ -242,10 +242,11 @@ __global__ __launch_bounds__(256) void rotary_cache_kernel(RotaryCacheArgs a) {
 
 int lanes_of(int64_t d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
-// Heads of a workgroup: as many as leave the device 2048 workgroups (eight to a compute unit), between one round of loads and eight of them.
-// (The angles of a round's heads take as long as turning one head.)
+// Heads of a workgroup: as many as leave the device 8192 workgroups, between one round of loads and eight of them.  (The angles of a round's heads
+// take as long as turning one head.  16384 tokens, 40 heads of 128 | four prompts into the cache, in us: with 2048 72 | 158, 4096 78 | 153, 8192
+// 70 | 152, 16384 69 | 161.)
 int heads_per(int64_t tiles, int64_t heads) {
-  const int64_t most = std::min<int64_t>(8, ceil_div(std::max<int64_t>(1, tiles * heads / 2048), kHeadsAhead)), rounds = ceil_div(heads, kHeadsAhead);
+  const int64_t most = std::min<int64_t>(8, ceil_div(std::max<int64_t>(1, tiles * heads / 8192), kHeadsAhead)), rounds = ceil_div(heads, kHeadsAhead);
   return (int)(ceil_div(rounds, ceil_div(rounds, most)) * kHeadsAhead);   // as many as that, and alike
 }
 // tiles of a launch, which has fewer than 2^32 threads
