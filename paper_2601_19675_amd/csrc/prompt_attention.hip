@@ -277,11 +277,11 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : DP > 
     };
     static_for<kLast - kFirst>([&](auto i_) __attribute__((always_inline)) {
       constexpr int m = kFirst + decltype(i_)::value, at = m % (kAhead + 1);
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (m % 2 == 0) __builtin_amdgcn_sched_barrier(0);
       if constexpr (m + kAhead < kLast) read(std::integral_constant<int, m + kAhead>{});
-      // slots of tiles that everybody has read are filled again, a request at a time: several would wait for each other
-      constexpr int n = (m * 2 * C::kRequests + kAll - 1) / kAll;
-      if constexpr (had && more && n < 2 * C::kRequests && n * kAll / (2 * C::kRequests) == m) {
+      // slots of tiles that everybody has read are filled again, early in the turn, but a request at a time: several would wait for each other
+      constexpr int n = m / 2;
+      if constexpr (had && more && n < 2 * C::kRequests && m == 2 * n) {
         if constexpr (n < C::kRequests) bring_one(vals, vals0, a.v_token, val_off, t + kRing - 1, val_slot(t + kRing - 1), n);
         else bring_one(keys, keys0, a.k_token, key_off, t + kRing, key_slot(t + kRing), n - C::kRequests);
       }
