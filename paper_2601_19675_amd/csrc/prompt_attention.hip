@@ -240,6 +240,7 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : DP > 
 
   uint32_t weights[16];   // pairs of bfloat16
   constexpr int kScores = 2 * kSteps, kAll = kScores + 4 * kOut, kAhead = 4;
+  static_assert(2 * 2 * C::kRequests <= kAll, "");   // (every request has its place in a turn)
   // One turn: the scores of tile t + 1 beside the weights of tile t, then the values of tile t beside the maximum of the new scores.  A matrix
   // instruction takes as long as what vector instructions a pair of weights takes, and they run side by side; so they are laid out in turn, with the
   // operands read from LDS kAhead instructions before.

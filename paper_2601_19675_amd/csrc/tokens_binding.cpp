@@ -249,6 +249,13 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
   });
 }
 
+// The call goes to the current device: all tensors have to be there.
+template <class... T>
+void here(const T&... t) {
+  const auto at = c10::hip::getCurrentHIPStream().device_index();
+  if (!((t.device().index() == at) && ...)) refuse(PyExc_ValueError, "tensors of another device than the current one");
+}
+
 // X and Y of a rotation, positions and frequencies
 void rotary_ok(const Tensor& X, const Tensor& Y, const Tensor& positions, const Tensor& freq) {
   PTQ_CHECK(X.dim() == 3 && X.stride(2) == 1 && Y.sizes() == X.sizes() && Y.stride(2) == 1 && Y.scalar_type() == X.scalar_type());
@@ -263,6 +270,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor &X = tensor(a[0]), &positions = tensor(a[1]), &freq = tensor(a[2]), &Y = tensor(a[3]);
     const double scale = number(a[4]);
     const int interleaved = truth(a[5]);
+    here(X, positions, freq, Y);
     rotary_ok(X, Y, positions, freq);
     ptq_dtype dt;
     if (!dtype_of(X, dt)) return PTQ_ERR_DTYPE;
@@ -283,6 +291,7 @@ PyObject* rotary_kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count)
     const int64_t bits = whole(a[6]);
     const double scale = number(a[11]);
     const int interleaved = truth(a[12]);
+    here(Q, K, V, positions, freq, slots, codes, scales, zeros, O);
     rotary_ok(Q, O, positions, freq);
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.sizes() == K.sizes() && V.stride(2) == 1 && K.scalar_type() == Q.scalar_type() && V.scalar_type() == Q.scalar_type());
     const int64_t t = K.size(0), heads = K.size(1), d = K.size(2);
@@ -308,6 +317,7 @@ PyObject* kv_cache_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return status_of([&]() -> ptq_status {
     const Tensor &fc = tensor(a[0]), &fs = tensor(a[1]), &fz = tensor(a[2]), &source = tensor(a[3]), &codes = tensor(a[4]), &scales = tensor(a[5]),
                  &zeros = tensor(a[6]), &target = tensor(a[7]);
+    here(fc, fs, fz, source, codes, scales, zeros, target);
     PTQ_CHECK(fc.dim() == 5 && codes.dim() == 5 && fc.size(4) == codes.size(4));
     const Cache from = cache_of(fc, fs, fz, 8, fc.size(4)), to = cache_of(codes, scales, zeros, 8, codes.size(4));
     PTQ_CHECK(from.heads == to.heads && from.page == to.page);
@@ -329,6 +339,7 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const int64_t max_n = whole(a[4]), window = whole(a[8]);
     const double scale = number(a[5]);
     const int causal = truth(a[7]);
+    here(Q, K, V, cu, O);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && K.scalar_type() == Q.scalar_type() &&
               V.scalar_type() == Q.scalar_type());
@@ -355,6 +366,8 @@ PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t count
     const int64_t max_q = whole(a[2]), bits = whole(a[6]), max_kv = whole(a[9]), max_shared = whole(a[12]);
     const double scale = number(a[13]);
     const int causal = truth(a[15]);
+    here(Q, cu, codes, scales, zeros, table, lens, cu_groups, shared, O);
+    if (ws) here(*ws);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     const int64_t t = Q.size(0), hq = Q.size(1), d = Q.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
