@@ -38,6 +38,8 @@ struct AttendArgs {
   const int32_t *cu_groups, *shared;
   int groups, max_shared;
   const float *pre_part, *pre_ml;        // the rows form's: where the chunk form has left its parts
+  int few_blocks;                        // the rows form's: sequences of more blocks than that behind their prefix have shares of the work, the others a workgroup
+  int mixed;                             // both in one launch: workgroups z < b are the sequences', the others share
   float *alone, *alone_ml;               // [token][head][d] and [2]: parts of tiles of rows that a share has all of
   int2* where;                           // [token][head]: the row of pre_part and pre_ml that has the first part (-1: alone has it), and how many there are
 };

@@ -47,6 +47,12 @@ constexpr int kFarExponent = 40;   // of a value's scale that the sum of the wei
 __device__ __forceinline__ int share_blocks(const AttendArgs& a, const Sequence& q) {
   return q.queries == 0 ? 0 : max(1, (q.end - q.begin + kShareBlock - 1) / kShareBlock);
 }
+// ... in the shares that SHARED has
+template <bool SHARED>
+__device__ __forceinline__ int shared_out(const AttendArgs& a, const Sequence& q) {
+  const int blocks = share_blocks(a, q);
+  return SHARED && blocks <= a.few_blocks ? 0 : blocks;
+}
 // a sequence, of one that shares a prefix what is behind it
 template <bool SHARED>
 __device__ __forceinline__ Sequence own_of(const AttendArgs& a, int s) {
@@ -118,18 +124,20 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
   // the workgroup's share: blocks [off, off + left) of sequence seq and on, `before` blocks before that sequence
   int seq = blockIdx.z, off = 0;
   int before = 0, share = 1, left = INT32_MAX;
-  if (a.splits > 1) {
+  const bool mixed = SHARED && a.mixed, whole = a.splits == 1 || (mixed && (int)blockIdx.z < a.b);
+  const int nth = mixed ? (int)blockIdx.z - a.b : (int)blockIdx.x, all = mixed ? (int)gridDim.z - a.b : (int)gridDim.x;   // of the workgroups with shares
+  if (!whole) {
     int total = 0;
-    for (int s0 = 0; s0 < a.b; s0 += kWave) total += s0 + lane < a.b ? share_blocks(a, own_of<SHARED>(a, s0 + lane)) : 0;
+    for (int s0 = 0; s0 < a.b; s0 += kWave) total += s0 + lane < a.b ? shared_out<SHARED>(a, own_of<SHARED>(a, s0 + lane)) : 0;
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) total += __shfl_xor(total, o);
     total = __builtin_amdgcn_readfirstlane(total);
-    share = max(a.least_share, (int)((total + gridDim.x - 1) / gridDim.x));
-    const int64_t mine = (int64_t)blockIdx.x * share;
+    share = max(a.least_share, (total + all - 1) / all);
+    const int64_t mine = (int64_t)nth * share;
     if (mine >= total) return;
     left = min(share, total - (int)mine);
     for (int s0 = 0;; s0 += kWave) {   // the first sequence that reaches past `mine`
-      const int n = s0 + lane < a.b ? share_blocks(a, own_of<SHARED>(a, s0 + lane)) : 0;
+      const int n = s0 + lane < a.b ? shared_out<SHARED>(a, own_of<SHARED>(a, s0 + lane)) : 0;
       int upto = n;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
@@ -152,14 +160,15 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
   if (seq >= a.b) return;
   const Sequence q = own_of<SHARED>(a, seq);
   const int queries = min(q.queries, a.max_q), rows = queries * a.group;
-  if (rows == 0) {
-    if (a.splits == 1) return;
+  const int blocks = share_blocks(a, q);
+  if (rows == 0 || (SHARED && (blocks > a.few_blocks) == whole)) {   // (not this workgroup's)
+    if (whole) return;
     continue;
   }
-  const int blocks = share_blocks(a, q), take = min(blocks - off, left);
+  const int take = min(blocks - off, left);
   const int from = q.begin + off * kShareBlock, to = min(q.end, from + take * kShareBlock);
   const bool alone = take == blocks;   // nobody else has keys of this sequence
-  const int part = alone ? 0 : (int)blockIdx.x - before / share;
+  const int part = alone ? 0 : nth - before / share;
 
   // the lane's query row, d as the keys have it: channels [g DP / 4, (g + 1) DP / 4)
   const int token = q.first + r / a.group, qhead = head * a.group + r % a.group;
@@ -509,7 +518,7 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
     }
     const int tok = q.first + row / a.group, h = head * a.group + row % a.group;
     if constexpr (SHARED) {
-      if (a.splits == 1) {   // all there is of the sequence's own keys: the prefix's parts join them here, sixteen at a time
+      if (whole) {   // all there is of the sequence's own keys: the prefix's parts join them here, sixteen at a time
         const PrefixParts pre = prefix_parts(a, seq, (int64_t)tok * a.hq + h);
         for (int p0 = 0; p0 < pre.parts; p0 += 16) {
           f32x4 v[16];
@@ -555,7 +564,11 @@ __global__ __launch_bounds__(kWaves * 64, DP > 128 || !HALVES ? 1 : 2) void atte
       store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, o);
     }
   }
-  if (a.splits == 1) return;
+  if (whole) {
+    if (mixed && head == 0)   // nothing to join
+      for (int i = threadIdx.x; i < queries; i += kWaves * 64) a.parts[q.first + i] = 0;
+    return;
+  }
   if (off == 0 && head == 0) {
     const int parts = alone ? 1 : (before + blocks - 1) / share - before / share + 1;
     for (int i = threadIdx.x; i < queries; i += kWaves * 64) a.parts[q.first + i] = parts;
@@ -620,9 +633,11 @@ __global__ __launch_bounds__(64) void shared_join_kernel(AttendArgs a) {
   const int seq = last_not_above(a.cu_q, 0, a.b, tok);
   const Sequence q = sequence_of(a, seq);
   if (tok < q.first || tok - q.first >= min(q.queries, a.max_q)) return;
+  const int own = min(a.parts[tok], a.splits);
+  if (own <= 0) return;   // written by the one workgroup that had it
   const int64_t first = (int64_t)tok * a.hq + h, step = (int64_t)a.t * a.hq;
   const PrefixParts pre = prefix_parts(a, seq, first);
-  const int parts = pre.parts + a.parts[tok], cc = c < a.d ? c : 0;
+  const int parts = pre.parts + own, cc = c < a.d ? c : 0;
   auto row_of = [&](int p) { return p < pre.parts ? pre.row(p) : first + (p - pre.parts) * step; };
   auto ml_of = [&](int p) { return *reinterpret_cast<const f32x2*>((p < pre.parts ? pre.ml : a.ml) + 2 * row_of(p)); };
   auto part_of = [&](int p) { return *reinterpret_cast<const f32x4*>((p < pre.parts ? pre.part : a.part) + row_of(p) * a.d + cc); };
@@ -657,6 +672,7 @@ __global__ __launch_bounds__(64) void shared_join_kernel(AttendArgs a) {
   store_run<PTQ_BF16, 4, false>(a.O + tok * a.o_token + h * a.o_head, c, a.d, v);
 }
 
+constexpr int kFewKeys = 2048;         // behind a prefix: one workgroup's
 constexpr int64_t kPartRows = 65536;   // rows times splits at most: what the workspace holds
 
 int64_t most_splits(int64_t rows, int64_t max_kv) {
@@ -671,7 +687,8 @@ template <int BITS, int DP, bool HALVES, bool WHOLE, bool SHARED>
 bool rows_form_launch(const AttendArgs& a, hipStream_t s) {
   constexpr int kBytes = kWaves * kRows * (DP + 4 + 4) * (int)sizeof(float);
   if (!lds_opt_in<attend_rows_kernel<BITS, DP, HALVES, WHOLE, SHARED>>(kBytes)) return false;
-  const dim3 grid = a.splits > 1 ? dim3((unsigned)shares(a.c.heads), (unsigned)a.c.heads, 1) : dim3(1, (unsigned)a.c.heads, (unsigned)a.b);
+  dim3 grid = a.splits > 1 ? dim3((unsigned)shares(a.c.heads), (unsigned)a.c.heads, 1) : dim3(1, (unsigned)a.c.heads, (unsigned)a.b);
+  if (SHARED && a.mixed) grid = dim3(1, (unsigned)a.c.heads, (unsigned)(a.b + shares(a.c.heads)));
   attend_rows_kernel<BITS, DP, HALVES, WHOLE, SHARED><<<grid, kWaves * 64, kBytes, s>>>(a);
   return true;
 }
@@ -813,9 +830,14 @@ ptq_status paged_attention_shared_launch(const void* Q, int64_t q_token, int64_t
   a.pre_part = pre.part, a.pre_ml = pre.ml;
   a.alone = pre.alone, a.alone_ml = pre.alone_ml, a.where = pre.where;
   // What is behind the prefixes is seldom long, and with one workgroup to a sequence and key head the parts join there: 25 us and no second kernel in place of
-  // 42 and 11 (64 sequences, 8 key heads, 151 to 732 keys behind a prefix).  The difference of the two bounds says how long it may be.
+  // 42 and 11 (64 sequences, 8 key heads, 151 to 732 keys behind a prefix).  The difference of the two bounds says how long it
+  // seems to be.  A sequence behind a short prefix, or of no group, has more than that: it goes in shares beside the others, if the bounds leave room for one.
+  // (8 behind 32768 keys and one of 33000 by itself: 88 us, with a workgroup to each 359.  Where there is none it costs 2 us: 64 behind 32768 87 and 85.)
   const int64_t own = max_kv - a.max_shared;
-  a.splits = own < 2048 || b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 ? 1 : (int)p.splits;
+  const bool never = b * hkv >= 4 * kShares || b * ceil_div(max_kv, kShareBlock) > INT32_MAX / 2 || p.splits == 1;
+  a.mixed = !never && own < kFewKeys && max_kv > kFewKeys;
+  a.splits = never || (own < kFewKeys && !a.mixed) ? 1 : (int)p.splits;
+  a.few_blocks = a.mixed ? kFewKeys / kShareBlock : a.splits > 1 ? 0 : INT32_MAX;
   a.least_share = a.splits > 1 ? (int)std::max<int64_t>(2, ceil_div(ceil_div(max_kv, kShareBlock), a.splits - 1)) : 1;
   const ptq_status rc = paged_attention_prefix_launch(pre, bits, s);
   if (rc != PTQ_OK) return rc;

@@ -119,6 +119,26 @@ def test_chunks_go_the_usual_way():
     p.check(absolute=True)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("kv,groups", [([2600, 2700, 2590, 2650], [(0, 3, 2560)]),            # one of no group among them
+                                       ([2650, 2600, 2700, 2590], [(1, 3, 2560)]),
+                                       ([3000, 2900, 2800, 2950, 5, 0], [(0, 2, 2752), (2, 2, 64)]),   # behind a long prefix, a short one, none
+                                       ([2112, 2048, 2049, 2176, 2177, 4000], [(0, 2, 2048)]),   # behind none: about 2048 keys, and more
+                                       ([4300, 4300, 4300], [(0, 2, 4160)])])
+@pytest.mark.parametrize("new", [1, 3])
+def test_long_sequences_beside_short_ones_behind_a_prefix(bits, kv, groups, new):
+    Shared(kv, [min(new, k) for k in kv], 8, 2, 64, bits, 16, groups, seed=len(kv) + new).check(absolute=True)
+
+
+def test_long_sequences_beside_short_ones_do_not_depend_on_the_workspace():
+    p = Shared([2600, 2700, 2590, 2650, 4000], [1, 2, 1, 2, 1], 8, 2, 128, 8, 32, [(0, 3, 2560)], seed=6)
+    ws = torch.zeros(ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 128, sum(p.new), max(p.kv)), dtype=torch.uint8, device="cuda")
+    first = p.run(ws=ws)
+    for fill in (255, 0x41, 0x7f):
+        ws.fill_(fill)
+        assert torch.equal(p.run(ws=ws), first)
+
+
 @pytest.mark.parametrize("page", [1, 16])
 def test_pages_that_are_not_there(page):
     p = Shared([300, 290, 280], [1, 2, 1], 8, 2, 64, 8, page, [(0, 3, 256)], seed=page)
