@@ -628,8 +628,9 @@ ptq_status ptq_prompt_attention(const void* Q, int64_t q_token, int64_t q_head, 
 /*
  * ptq_paged_attention for sequences that share prefixes (forks of a sequence, requests behind one long text): the keys of a prefix are read and
  * multiplied once for all queries behind it.  The result is ptq_paged_attention's with the same arguments and window 0, but for how it is rounded: a
- * prefix is gone through as chunks are, with their roundings, where more than one sequence has it and no key head has more than 16 rows (tokens
- * times group) of a sequence; otherwise the call does what ptq_paged_attention does.
+ * prefix is gone through as chunks are, with their roundings, where more than one sequence has it, no key head has more than 16 rows (tokens
+ * times group) of a sequence, and the bounds (b, groups, max_shared, max_kv) say that it saves time: prefixes of more than 4 MB of codes and some eight
+ * sequences behind each.  Otherwise the call does what ptq_paged_attention does.
  *
  * cu_groups  groups + 1 int32 on the device, never falling: sequences cu_groups[j] .. cu_groups[j + 1] share a prefix.  Sequences of no group, and groups
  *            that begin before sequence 0 or end past b, share nothing.

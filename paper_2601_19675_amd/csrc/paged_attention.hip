@@ -795,6 +795,23 @@ SharedPlan shared_plan(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
   return p;
 }
 }  // namespace
+namespace {
+// Whether prefixes gone through apart take less time than every sequence's whole way, in us as measured and by what the bounds say.  Every sequence by itself: 15, and
+// 0.135 to a megabyte of codes (pages that several name are in the caches).  Apart: 25, 1.7e-4 for a key of a prefix, a key head and a tile of 256 rows of 128 channels,
+// 0.25 for each of a row's parts beyond 32, and what is behind the prefixes as before.  A prefix that a die's L2 holds (4 MB) is read from there by all
+// sequences as fast.  32 heads of 128 channels over 8, 8 bits, apart | by itself: 8 behind 1000 keys 27 | 18, 64 41 | 28; 4 behind 8192 35 | 27, 8
+// 35 | 36, 16 37 | 55; 4 behind 32768 72 | 54, 8 72 | 90, 64 87 | 493.  16 heads over 1: 16 behind 32768 94 | 38.  32 over 32: 8 behind 2048 35 | 31, 12 39 | 47.  The numbers
+// are fitted to these and their like; the one miss seen is 16 in two groups behind 8192 with up to 7800 keys of their own, 71 | 66.
+bool prefixes_pay(const AttendArgs& a, int bits) {
+  const double key = (double)a.c.heads * a.d * 2 * bits / 8 * 1e-6;   // megabytes
+  const double tiles = (double)ceil_div((int64_t)a.t * a.group, 256) + a.groups - 1, prefix = a.max_shared;
+  if (prefix * key <= 4.0) return false;
+  const double parts = std::min(kChunkShares / (a.c.heads * tiles), prefix / 128);
+  const double each = 15 + 0.135 * a.b * key * a.max_kv;
+  const double apart = 25 + 1.7e-4 * a.c.heads * tiles * prefix * a.d / 128 + 0.25 * std::max(0.0, parts - 32) + 0.135 * a.b * key * (a.max_kv - prefix);
+  return apart < each;
+}
+}  // namespace
 size_t paged_attention_shared_workspace_bytes(int64_t hq, int64_t d, int64_t t, int64_t max_kv) {
   return std::max(align_up((size_t)shared_plan(hq, d, t, max_kv).floats * sizeof(float), 256), paged_attention_workspace_bytes(hq, d, t, max_kv));
 }
@@ -810,7 +827,7 @@ ptq_status paged_attention_shared_launch(const void* Q, int64_t q_token, int64_t
   a.cu_groups = cu_groups, a.shared = shared, a.groups = (int)groups, a.max_shared = (int)std::min(max_shared, max_kv);
   // Chunks of tokens are bound by their products, which are no fewer with a prefix in common, and prefixes of less than a block are not gone
   // through apart.
-  if (max_q * a.group > kRows || a.max_shared < 64 || groups == 0 || paged_attention_prefix_tiles(a) > kMostSharedTiles)
+  if (max_q * a.group > kRows || a.max_shared < 64 || groups == 0 || paged_attention_prefix_tiles(a) > kMostSharedTiles || !prefixes_pay(a, bits))
     return paged_attention_launch(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt, kv_lens,
                                   max_kv, softmax_scale, causal, 0, O, o_token, o_head, ws, s);
   const SharedPlan p = shared_plan(hq, d, t, max_kv);

@@ -37,16 +37,34 @@ class Shared(Problem):
             shared.append(common)
         return ends, shared
 
-    def run(self, causal=True, window=0, ws=None, ends=None, shared=None, max_shared=None, O=None):
+    behind = 1000    # what the bounds leave for keys behind a prefix: below 2048 a workgroup has a sequence's, else all are shared out
+
+    def bounds(self, shared):
+        """Few keys of few heads are no work to save: the bounds that the call chooses its way by say that there is more, and sequences that hold nothing and
+        ask nothing follow the others.  max_kv, max_shared, how many follow."""
+        heads, most = self.codes.shape[2], max(shared, default=0)
+        follow = 900 // heads - len(self.kv)
+        if most < 64 or follow <= 0:
+            return max(self.kv), most, 0
+        most = max(most, -(-8_000_000 // (heads * self.d * 2 * self.bits // 8)))    # keys of 8 MB
+        return max(max(self.kv), most + self.behind), most, follow
+
+    def run(self, causal=True, window=0, ws=None, ends=None, shared=None, max_shared=None, O=None, loose=True):
         assert window == 0
         if ends is None:
             ends, shared = self.groups_of()
+        if loose and max_shared is None:
+            max_kv, most, follow = self.bounds(shared)
+        else:
+            max_kv, most, follow = max(self.kv), max(shared, default=0) if max_shared is None else max_shared, 0
+        cu = np.concatenate([self.cu, np.full(follow, self.cu[-1], dtype=self.cu.dtype)])
+        table = np.concatenate([self.table, np.zeros((follow, self.table.shape[1]), dtype=self.table.dtype)])
+        kv = list(self.kv) + [0] * follow
         q = torch.tensor(self.Q.astype(np.float32), device="cuda").bfloat16()
         O = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device="cuda") if O is None else O
         t = lambda a: torch.tensor(a, device="cuda")
-        ptq.ptq_paged_attention_shared(q, t(self.cu), max(self.new), t(self.codes), t(self.scales), t(self.zeros), self.bits, t(self.table), dev(self.kv),
-                                       max(self.kv), dev(ends), dev(shared), max(shared, default=0) if max_shared is None else max_shared, self.scale, O,
-                                       causal=causal, ws=ws)
+        ptq.ptq_paged_attention_shared(q, t(cu), max(self.new), t(self.codes), t(self.scales), t(self.zeros), self.bits, t(table), dev(kv), max_kv, dev(ends),
+                                       dev(shared), most, self.scale, O, causal=causal, ws=ws)
         torch.cuda.synchronize()
         return O
 
@@ -115,7 +133,7 @@ def test_a_group_among_sequences_of_none():
 
 def test_chunks_go_the_usual_way():
     p = Shared([500, 470, 600], [40, 20, 1], 8, 2, 64, 8, 16, [(0, 3, 400)], seed=5)
-    assert torch.equal(p.run(), Problem.run(p))
+    assert torch.equal(p.run(loose=False), Problem.run(p))
     p.check(absolute=True)
 
 
@@ -132,11 +150,43 @@ def test_long_sequences_beside_short_ones_behind_a_prefix(bits, kv, groups, new)
 
 def test_long_sequences_beside_short_ones_do_not_depend_on_the_workspace():
     p = Shared([2600, 2700, 2590, 2650, 4000], [1, 2, 1, 2, 1], 8, 2, 128, 8, 32, [(0, 3, 2560)], seed=6)
-    ws = torch.zeros(ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 128, sum(p.new), max(p.kv)), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 128, sum(p.new), p.bounds(p.groups_of()[1])[0]), dtype=torch.uint8, device="cuda")
     first = p.run(ws=ws)
     for fill in (255, 0x41, 0x7f):
         ws.fill_(fill)
         assert torch.equal(p.run(ws=ws), first)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("kv,groups", [([5200, 5300, 5100, 2650], [(0, 3, 2560)]), ([700, 650, 9000, 64, 1], [(0, 2, 600)])])
+def test_all_sequences_in_shares(bits, kv, groups):
+    p = Shared(kv, [1] * len(kv), 8, 2, 64, bits, 16, groups, seed=len(kv))
+    p.behind = 5000
+    p.check(absolute=True)
+
+
+def test_a_workgroup_to_each_and_bounds_below_the_prefix():
+    """Bounds of less than 2048 keys; keys from a bound on are each sequence's own."""
+    p = Shared([1450, 1500, 1410], [1, 1, 1], 32, 32, 128, 8, 64, [(0, 3, 1400)], seed=3)
+    follow = 25
+    run = Shared.run
+
+    def bounded(most):
+        p.bounds = lambda shared: (1500, most, follow)
+        p.run = lambda causal=True, window=0, **kw: run(p, causal, window, **kw)
+        p.check(absolute=True)
+        return p.run()
+
+    plain = Problem.run(p)
+    assert not any(torch.equal(bounded(most), plain) for most in (1400, 1023, 1024))
+
+
+def test_which_way_it_goes():
+    """Outputs of the two ways differ in their roundings: work to save goes through the prefixes apart, little work as in ptq_paged_attention."""
+    p = Shared([1300, 1250, 1400, 1211], [1] * 4, 8, 2, 64, 8, 16, [(0, 4, 1200)], seed=2)
+    plain = Problem.run(p)
+    assert torch.equal(p.run(loose=False), plain)
+    assert not torch.equal(p.run(), plain)
 
 
 @pytest.mark.parametrize("page", [1, 16])
@@ -173,7 +223,7 @@ def test_sizes_of_values(bits, k_size, v_size):
 
 def test_results_do_not_depend_on_the_workspace_or_the_call():
     p = Shared([3000 + 11 * i for i in range(20)], [1] * 20, 8, 2, 128, 8, 16, [(0, 12, 2900), (13, 7, 3000)], seed=8)
-    need = ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 128, 20, max(p.kv))
+    need = ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 128, 20, p.bounds(p.groups_of()[1])[0])
     ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
     first = p.run(ws=ws)
     assert torch.equal(p.run(ws=ws), first)
@@ -189,11 +239,12 @@ def test_replayed_and_on_another_stream():
     t = lambda a: torch.tensor(a, device="cuda")
     Q = torch.tensor(p.Q.astype(np.float32), device="cuda").bfloat16()
     O, want = torch.zeros_like(Q), torch.zeros_like(Q)
-    lens, shared, ends = dev(p.kv), dev([640]), dev([0, 4])
+    many = 400    # sequences that hold nothing follow, and the bounds are far: work to save
+    lens, shared, ends = dev(list(p.kv) + [0] * many), dev([640]), dev([0, 4])
     cache = t(p.codes), t(p.scales), t(p.zeros)
-    cu, table = t(p.cu), t(p.table)
-    ws = [torch.empty(ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 64, 4, 800), dtype=torch.uint8, device="cuda") for _ in range(2)]
-    call = lambda o, w: ptq.ptq_paged_attention_shared(Q, cu, 1, *cache, 8, table, lens, 800, ends, shared, 640, p.scale, o, ws=w)
+    cu, table = dev(list(p.cu) + [4] * many), t(np.concatenate([p.table, np.zeros((many, p.table.shape[1]), dtype=np.int32)]))
+    ws = [torch.empty(ptq.ptq_workspace_bytes(ptq.OP_SHARED_ATTENTION, 8, 64, 4, 33000), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    call = lambda o, w: ptq.ptq_paged_attention_shared(Q, cu, 1, *cache, 8, table, lens, 33000, ends, shared, 32000, p.scale, o, ws=w)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
@@ -203,7 +254,7 @@ def test_replayed_and_on_another_stream():
     with torch.cuda.graph(graph):
         call(O, ws[0])
     for i in range(4):
-        lens.copy_(dev([c - 5 * i for c in p.kv]))
+        lens[:4].copy_(dev([c - 5 * i for c in p.kv]))
         shared.fill_(640 - 100 * i)
         graph.replay()
         call(want, ws[1])
