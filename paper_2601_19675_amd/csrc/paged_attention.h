@@ -162,7 +162,8 @@ struct ChunkItems { int64_t tiles, busy; };
 ChunkItems paged_attention_chunk_items(const AttendArgs& a);
 ptq_status paged_attention_chunk_launch(const AttendArgs& a, int bits, hipStream_t s);
 // the prefixes that groups share, in shares; parts are left in part, ml, alone, alone_ml and where
-int64_t paged_attention_prefix_tiles(const AttendArgs& a);   // tiles of rows of all groups, at most
+int64_t paged_attention_prefix_tiles(const AttendArgs& a);   // tiles of rows that a workgroup looks through for its share
+int64_t paged_attention_prefix_work(const AttendArgs& a);    // what they hold, in tiles of keys of all key heads, at most
 ptq_status paged_attention_prefix_launch(const AttendArgs& a, int bits, hipStream_t s);
 
 }  // namespace ptq

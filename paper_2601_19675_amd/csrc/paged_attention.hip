@@ -826,8 +826,9 @@ ptq_status paged_attention_shared_launch(const void* Q, int64_t q_token, int64_t
                              softmax_scale, causal, 0, O, o_token, o_head);
   a.cu_groups = cu_groups, a.shared = shared, a.groups = (int)groups, a.max_shared = (int)std::min(max_shared, max_kv);
   // Chunks of tokens are bound by their products, which are no fewer with a prefix in common, and prefixes of less than a block are not gone
-  // through apart.
-  if (max_q * a.group > kRows || a.max_shared < 64 || groups == 0 || paged_attention_prefix_tiles(a) > kMostSharedTiles || !prefixes_pay(a, bits))
+  // through apart.  Every workgroup looks through all tiles of rows for its share, and counts work in 32 bits, with whole shares up to six times of it.
+  if (max_q * a.group > kRows || a.max_shared < 64 || groups == 0 || paged_attention_prefix_tiles(a) > kMostSharedTiles ||
+      paged_attention_prefix_work(a) > INT32_MAX / 8 || !prefixes_pay(a, bits))
     return paged_attention_launch(Q, q_token, q_head, t, hq, d, cu_q, b, max_q, codes, scales, zeros, pages, page, hkv, bits, table, ldt, kv_lens,
                                   max_kv, softmax_scale, causal, 0, O, o_token, o_head, ws, s);
   const SharedPlan p = shared_plan(hq, d, t, max_kv);

@@ -864,8 +864,12 @@ bool prefix_launch(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t paged_attention_prefix_tiles(const AttendArgs& a) {
-  return (int64_t)a.groups * ceil_div((int64_t)a.t * a.group, a.d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows);
+namespace {
+int64_t prefix_rows(const AttendArgs& a) { return a.d > 128 ? Chunk<256>::kRows : Chunk<128>::kRows; }
+}  // namespace
+int64_t paged_attention_prefix_tiles(const AttendArgs& a) { return (int64_t)a.groups * ceil_div((int64_t)a.t * a.group, prefix_rows(a)); }
+int64_t paged_attention_prefix_work(const AttendArgs& a) {   // (a group's last tile of rows may be part of one)
+  return (ceil_div((int64_t)a.t * a.group, prefix_rows(a)) + a.groups) * a.c.heads * ceil_div(a.max_shared, kTile);
 }
 
 ptq_status paged_attention_prefix_launch(const AttendArgs& a, int bits, hipStream_t s) {
