@@ -608,7 +608,8 @@ ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_
  *   O = sum_j p_j v_j / sum_j p_j,   p_j = exp(softmax_scale q . k_j - max)
  *
  * Scores, running maxima and sums are float32; weights are rounded to bfloat16 (2^-8 of each), and the sum is of the rounded ones.  A token that is not
- * seen has no effect, whatever it holds; one that is seen and is not finite makes what it reaches not finite.  Scores are float32: |softmax_scale
+ * seen has no effect, whatever it holds; one that is seen and is not finite makes what it reaches not finite.  Values may be of any size; not finite, they take up
+ * to twice the time, and from 2^95 on, where sums may leave float32's range, up to three times.  Scores are float32: |softmax_scale
  * q . k| beyond 1e38 makes the row NaN or leaves keys out.
  *
  * Q, K, V, O  token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_BF16.  O may be Q with the same

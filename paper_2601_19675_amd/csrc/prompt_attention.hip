@@ -23,7 +23,8 @@
 //
 // A key that a row does not see leaves it as it is, whatever it holds: its score is replaced.  A value that is not finite would meet a weight of 0
 // all the same (0 times it is not 0): a workgroup that ends with anything not finite starts over, takes such values out of the tiles that it
-// reads, and adds them at the end for the rows that see them.
+// reads, and adds them at the end for the rows that see them.  Sums that are not finite even so are too large for float32 (weights are up to
+// 2^8, values up to 2^128): it starts over once more, and those rows have a maximum 2^kLift above the one that they ended with.
 #include <algorithm>
 
 #include "lds_dma.h"
@@ -39,6 +40,8 @@ typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
 typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
 
 constexpr int kTile = 64;   // keys
+// 2^24 keys with values below 2^128 and weights of 2^(8 - kLift) are within float32.  (A weight below 2^(kLift - 126) of the largest is lost.)
+constexpr float kLift = 34.f;
 
 struct PromptArgs {
   const uint16_t *Q, *K, *V; uint16_t* O;   // bfloat16
@@ -339,13 +342,14 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : DP > 
     }
   };
 
+  M = kNoScore;
 #pragma unroll 1
-  for (bool careful = false;; careful = true) {
+  for (int go = 0;; ++go) {
+    const bool careful = go > 0;
 #pragma unroll
     for (int k = 0; k < kOut; ++k)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[k][i] = 0.f;
-    M = kNoScore;
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] = 0.f;
     f32x16v s0[2], s1[2];
@@ -388,25 +392,28 @@ __global__ __launch_bounds__((Prompt<DP, WAVES>::kThreads), DP > 128 ? 1 : DP > 
     last_weights(s0);
     turn(std::integral_constant<int, kHad>{}, t, s0, s1);
     arrived(std::integral_constant<int, 0>{});   // nothing comes into LDS that is somebody else's by then
-    if (careful) {
-      add_cleaned();
-      break;
+    if (go < 2) {
+      float odd = 0.f;   // NaN if anything is not finite
+#pragma unroll
+      for (int k = 0; k < kOut; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = fmaf(acc[k][i], 0.f, odd);
+      // (in the second go only rows whose weights are numbers gain by another)
+      const uint64_t again = __ballot(live && odd != 0.f && (!careful || fabsf((sum[0] + sum[1]) + (sum[2] + sum[3])) < INFINITY));
+      const uint32_t again_rows = (uint32_t)again | (uint32_t)(again >> 32);
+      M = careful && (again_rows >> r & 1) ? M + kLift : kNoScore;
+      meet();
+      int* const vote = reinterpret_cast<int*>(smem);
+      if (lane == 0) vote[wave] = again != 0;
+      meet();
+      int any = 0;
+#pragma unroll
+      for (int w = 0; w < C::kWaves; ++w) any |= vote[w];
+      meet();
+      if (__builtin_amdgcn_readfirstlane(any) != 0) continue;
     }
-    float odd = 0.f;   // NaN if anything is not finite
-#pragma unroll
-    for (int k = 0; k < kOut; ++k)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) odd = fmaf(acc[k][i], 0.f, odd);
-    meet();
-    int* const vote = reinterpret_cast<int*>(smem);
-    if (lane == 0) vote[wave] = 0;
-    if (live && odd != 0.f) vote[wave] = 1;
-    meet();
-    int any = 0;
-#pragma unroll
-    for (int w = 0; w < C::kWaves; ++w) any |= vote[w];
-    if (__builtin_amdgcn_readfirstlane(any) == 0) break;
-    meet();
+    if (careful) add_cleaned();
+    break;
   }
   float l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
   l += __shfl_xor(l, 32);
