@@ -43,6 +43,7 @@ class PagedCache:
         self.lens = [0] * sequences
         self.free = list(range(pages))[::-1]
         self.users = [0] * pages
+        self.behind = [False] * sequences   # whether it still is the fork, or the parent, that its family began with
         self.families, self.groups_device, self.shared_device, self.max_shared = [], None, None, 0
 
     def _put(self, a) -> torch.Tensor:
@@ -56,6 +57,7 @@ class PagedCache:
     def extend(self, new: list[int]) -> dict:
         """Makes room for new[s] more tokens of each sequence; what the calls have to know about these tokens."""
         slots, cu, positions, whole = [], [0], [], all(n == 0 or self.lens[s] == 0 for s, n in enumerate(new))
+        taken = any(n > 0 and self.lens[s] == 0 for s, n in enumerate(new))
         for s, n in enumerate(new):
             for j in range(self.lens[s], self.lens[s] + n):
                 if j % self.page == 0:
@@ -65,11 +67,13 @@ class PagedCache:
             self.lens[s] += n
             cu.append(cu[-1] + n)
         self.table_device.copy_(self.table)   # in place: a graph that was captured goes on reading it
+        if taken:
+            self._share()
         return {"slots": self._put(slots), "cu_q": self._put(cu), "max_q": max(new), "kv_lens": self._put(self.lens),
                 "positions": self._put(positions), "whole": whole}
 
     def release(self, s: int) -> None:
-        """Sequence s, with no tokens to come, is gone; pages that nobody else has are free again."""
+        """Sequence s is gone; pages that nobody else has are free again, and s is there for another sequence."""
         for i in range(-(-self.lens[s] // self.page)):
             page = int(self.table[s, i])
             self.users[page] -= 1
@@ -77,19 +81,27 @@ class PagedCache:
                 self.free.append(page)
         self.table[s] = -1
         self.lens[s] = 0
+        self.behind[s] = False
         self.table_device.copy_(self.table)
         self._share()
 
     def _share(self) -> None:
-        """Tells the attention which sequences lie behind what: between families there are groups that share nothing.  A family begins with a sequence that
-        is still there, whose pages are the ones that are read."""
+        """Tells the attention which sequences lie behind what: between families there are groups that share nothing.  Of a family it is the longest run of
+        members that no other sequence has come between (one that holds nothing may lie there).  It begins with a member, whose pages are the
+        ones that are read."""
         if not self.families:
             return
         cu, shared = [0], []
         for family, length in self.families:
-            alive = [s for s in family if self.lens[s] >= length > 0]
-            cu += [alive[0] if alive else family[0], family[-1] + 1]
-            shared += [0, length if alive else 0]
+            runs = [[]]
+            for s in family:
+                if self.behind[s]:
+                    runs[-1].append(s)
+                elif self.lens[s] > 0:
+                    runs.append([])
+            run = max(runs, key=len)
+            cu += [run[0], run[-1] + 1] if run else [family[0], family[0]]
+            shared += [0, length if run else 0]
         if self.groups_device is None:
             self.groups_device, self.shared_device = self._put(cu), self._put(shared)
         else:   # in place, as the table
@@ -120,6 +132,7 @@ class PagedCache:
             ptq.ptq_kv_cache_copy_pages(*cache, self._put(source), *cache, self._put(target))
         self.table_device.copy_(self.table)
         self.families, self.groups_device = [(family, self.lens[family[0]]) for family in families], None
+        self.behind = [any(s in family and length > 0 for family, length in self.families) for s in range(len(self.lens))]
         self.max_shared = max(length for _, length in self.families)
         self._share()
 

@@ -84,3 +84,31 @@ def test_answers(bits):
     for i, s in enumerate(left):
         near(half, gamma, [out[i:i + 1]], tokens[s] + [x5[i:i + 1]], bits)
     apart_from_each_other(half, x5, at, out)
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("gone", [0, 2, 4])
+def test_a_slot_taken_by_another_sequence(bits, gone):
+    """A fork, or the parent, goes, and another prompt comes into its slot, between sequences that still lie behind what they share."""
+    half, gamma, rand = make(bits)
+    cache, tokens = half.cache, [[rand(300)] for _ in range(5)]
+    half(tokens[0][0], None, cache.extend(counts({0: 300})))
+    cache.fork([[0, 1, 2, 3, 4]])
+    cache.max_shared = FAR_SHARED
+    for s in range(1, 5):
+        tokens[s] = [tokens[0][0]]
+
+    def step():
+        x = rand(5)
+        at = cache.extend(counts({s: 1 for s in range(5)}))
+        out = half(x, None, at)[0].clone()
+        for s in range(5):
+            tokens[s].append(x[s:s + 1])
+            near(half, gamma, [out[s:s + 1]], tokens[s], bits)
+        apart_from_each_other(half, x, at, out)
+    step()
+    cache.release(gone)
+    tokens[gone] = [rand(350)]
+    half(tokens[gone][0], None, cache.extend(counts({gone: 350})))
+    step()
+    step()
