@@ -45,6 +45,7 @@ class PagedCache:
         self.users = [0] * pages
         self.behind = [False] * sequences   # whether it still is the fork, or the parent, that its family began with
         self.families, self.groups_device, self.shared_device, self.max_shared = [], None, None, 0
+        self.outdated = []   # what graphs of before a fork may still read: that nothing is shared
 
     def _put(self, a) -> torch.Tensor:
         return torch.tensor(a, dtype=torch.int32, device=self.table_device.device)
@@ -102,11 +103,14 @@ class PagedCache:
             run = max(runs, key=len)
             cu += [run[0], run[-1] + 1] if run else [family[0], family[0]]
             shared += [0, length if run else 0]
-        if self.groups_device is None:
-            self.groups_device, self.shared_device = self._put(cu), self._put(shared)
-        else:   # in place, as the table
+        if self.shared_device is not None and len(shared) == len(self.shared_device):   # in place, as the table
             self.groups_device.copy_(self._put(cu))
             self.shared_device.copy_(self._put(shared))
+            return
+        if self.shared_device is not None:
+            self.shared_device.zero_()
+            self.outdated.append((self.groups_device, self.shared_device))
+        self.groups_device, self.shared_device = self._put(cu), self._put(shared)
 
     def fork(self, families: list[list[int]]) -> None:
         """families[j] = [sequence, forks ...]: the forks, empty ones that follow it, become copies of the sequence.  Full pages are shared, the page in which
@@ -131,7 +135,7 @@ class PagedCache:
             cache = self.codes, self.scales, self.zeros
             ptq.ptq_kv_cache_copy_pages(*cache, self._put(source), *cache, self._put(target))
         self.table_device.copy_(self.table)
-        self.families, self.groups_device = [(family, self.lens[family[0]]) for family in families], None
+        self.families = [(family, self.lens[family[0]]) for family in families]
         self.behind = [any(s in family and length > 0 for family, length in self.families) for s in range(len(self.lens))]
         self.max_shared = max(length for _, length in self.families)
         self._share()

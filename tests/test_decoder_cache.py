@@ -86,3 +86,23 @@ def test_pages_are_freed_once():
     for s in (5, 6, 7, 0, 2):
         cache.release(s)
     assert not any(cache.users) and sorted(cache.free) == list(range(len(cache.users)))
+
+
+def test_a_graph_of_before_a_second_fork_goes_on_reading_what_is_so():
+    """It has the tensors' addresses: they stay what they are, or stay there and say that nothing is shared."""
+    cache = forked()
+    groups, shared = cache.groups_device, cache.shared_device
+    at = groups.data_ptr(), shared.data_ptr()
+    for s in (1, 2, 3, 4, 6, 7):
+        cache.release(s)
+    cache.fork([[0, 1, 2], [5, 6]])                            # as many families: in place
+    assert cache.groups_device is groups and cache.shared_device is shared
+    check(cache, [0, 1, 2, 5, 6])
+    for s in (1, 2, 6):
+        cache.release(s)
+    cache.fork([[5, 6, 7]])
+    check(cache, [5, 6, 7])
+    assert cache.groups_device is not groups and shared.tolist() == [0] * 4
+    del groups, shared
+    taken = [cache._put([7] * n) for n in (4, 5) for _ in range(50)]
+    assert not {t.data_ptr() for t in taken} & set(at)         # nobody else has got their memory
