@@ -91,6 +91,7 @@ def test_pages_are_freed_once():
 def test_a_graph_of_before_a_second_fork_goes_on_reading_what_is_so():
     """It has the tensors' addresses: they stay what they are, or stay there and say that nothing is shared."""
     cache = forked()
+    cache.extend([15] * 8)                                     # (whole pages: nothing is copied on a device)
     groups, shared = cache.groups_device, cache.shared_device
     at = groups.data_ptr(), shared.data_ptr()
     for s in (1, 2, 3, 4, 6, 7):
