@@ -53,6 +53,16 @@ bool truth(PyObject* o) {
   return v != 0;
 }
 
+// The call goes to the current device: all tensors have to be there.
+const Tensor* address_of(const Tensor& t) { return &t; }
+const Tensor* address_of(const Tensor* t) { return t; }
+template <class... T>
+void here(const T&... t) {
+  const auto at = c10::hip::getCurrentHIPStream().device_index();
+  for (const Tensor* p : {address_of(t)...})
+    if (p && p->device().index() != at) refuse(PyExc_ValueError, "tensors of another device than the current one");
+}
+
 // storage types that the library does not know become its own status
 bool dtype_of(const Tensor& t, ptq_dtype& d) {
   switch (t.scalar_type()) {
@@ -115,6 +125,7 @@ PyObject* rmsnorm_quantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor *gamma = optional(a[3]), *residual = optional(a[4]), *out = optional(a[5]);
     const double eps = number(a[6]);
     const int normalize = truth(a[7]);
+    here(X, codes, scales, gamma, residual, out);
     PTQ_CHECK(X.dim() == 2 && X.stride(1) == 1);
     const int64_t t = X.size(0), n = X.size(1);
     PTQ_CHECK(codes.scalar_type() == at::kChar && codes.dim() == 2 && codes.size(0) == t && codes.size(1) == n && codes.stride(1) == 1);
@@ -139,6 +150,7 @@ PyObject* int8_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return status_of([&]() -> ptq_status {
     const Tensor &A = tensor(a[0]), &as_ = tensor(a[1]), &W = tensor(a[2]), &ws_ = tensor(a[3]), &O = tensor(a[4]);
     const Tensor *bias = optional(a[5]), *ws = optional(a[6]);
+    here(A, as_, W, ws_, O, bias, ws);
     PTQ_CHECK(A.scalar_type() == at::kChar && A.dim() == 2 && A.stride(1) == 1);
     PTQ_CHECK(W.scalar_type() == at::kChar && W.dim() == 2 && W.stride(1) == 1 && W.size(1) == A.size(1));
     const int64_t t = A.size(0), n = A.size(1), m = W.size(0);
@@ -179,6 +191,7 @@ PyObject* kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return status_of([&]() -> ptq_status {
     const Tensor &K = tensor(a[0]), &V = tensor(a[1]), &slots = tensor(a[2]), &codes = tensor(a[4]), &scales = tensor(a[5]), &zeros = tensor(a[6]);
     const int64_t bits = whole(a[3]);
+    here(K, V, slots, codes, scales, zeros);
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && V.scalar_type() == K.scalar_type());
     const int64_t t = K.size(0), heads = K.size(1), d = K.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -201,6 +214,7 @@ PyObject* kv_cache_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor &codes = tensor(a[0]), &scales = tensor(a[1]), &zeros = tensor(a[2]), &table = tensor(a[4]), &cu = tensor(a[5]),
                  &K = tensor(a[7]), &V = tensor(a[8]);
     const int64_t bits = whole(a[3]), max_kv = whole(a[6]);
+    here(codes, scales, zeros, table, cu, K, V);
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && V.scalar_type() == K.scalar_type());
     const int64_t rows = K.size(0), heads = K.size(1), d = K.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -229,6 +243,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const int64_t max_q = whole(a[2]), bits = whole(a[6]), max_kv = whole(a[9]), window = whole(a[13]);
     const double scale = number(a[10]);
     const int causal = truth(a[12]);
+    here(Q, cu, codes, scales, zeros, table, lens, O, ws);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     const int64_t t = Q.size(0), hq = Q.size(1), d = Q.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -247,13 +262,6 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
                                  max_kv, scale, causal, window, ptr(O), O.stride(0), O.stride(1), w.at, w.bytes, s);
     });
   });
-}
-
-// The call goes to the current device: all tensors have to be there.
-template <class... T>
-void here(const T&... t) {
-  const auto at = c10::hip::getCurrentHIPStream().device_index();
-  if (!((t.device().index() == at) && ...)) refuse(PyExc_ValueError, "tensors of another device than the current one");
 }
 
 // X and Y of a rotation, positions and frequencies
@@ -366,8 +374,7 @@ PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t count
     const int64_t max_q = whole(a[2]), bits = whole(a[6]), max_kv = whole(a[9]), max_shared = whole(a[12]);
     const double scale = number(a[13]);
     const int causal = truth(a[15]);
-    here(Q, cu, codes, scales, zeros, table, lens, cu_groups, shared, O);
-    if (ws) here(*ws);
+    here(Q, cu, codes, scales, zeros, table, lens, cu_groups, shared, O, ws);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     const int64_t t = Q.size(0), hq = Q.size(1), d = Q.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
