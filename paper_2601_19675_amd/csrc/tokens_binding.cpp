@@ -53,14 +53,15 @@ bool truth(PyObject* o) {
   return v != 0;
 }
 
-// The call goes to the current device: all tensors have to be there.
+// The current stream, of the current device: all tensors have to be there.  (Asking for it twice would take 0.4 us.)
 const Tensor* address_of(const Tensor& t) { return &t; }
 const Tensor* address_of(const Tensor* t) { return t; }
 template <class... T>
-void here(const T&... t) {
-  const auto at = c10::hip::getCurrentHIPStream().device_index();
+ptq_stream stream_of(const T&... t) {
+  const auto current = c10::hip::getCurrentHIPStream();
   for (const Tensor* p : {address_of(t)...})
-    if (p && p->device().index() != at) refuse(PyExc_ValueError, "tensors of another device than the current one");
+    if (p && p->device().index() != current.device_index()) refuse(PyExc_ValueError, "tensors of another device than the current one");
+  return current.stream();
 }
 
 // storage types that the library does not know become its own status
@@ -72,8 +73,6 @@ bool dtype_of(const Tensor& t, ptq_dtype& d) {
     default: return false;
   }
 }
-
-ptq_stream stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 // the caller's workspace, or a new one of the size the call needs
 struct Workspace {
@@ -125,7 +124,7 @@ PyObject* rmsnorm_quantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor *gamma = optional(a[3]), *residual = optional(a[4]), *out = optional(a[5]);
     const double eps = number(a[6]);
     const int normalize = truth(a[7]);
-    here(X, codes, scales, gamma, residual, out);
+    const ptq_stream s = stream_of(X, codes, scales, gamma, residual, out);
     PTQ_CHECK(X.dim() == 2 && X.stride(1) == 1);
     const int64_t t = X.size(0), n = X.size(1);
     PTQ_CHECK(codes.scalar_type() == at::kChar && codes.dim() == 2 && codes.size(0) == t && codes.size(1) == n && codes.stride(1) == 1);
@@ -135,7 +134,6 @@ PyObject* rmsnorm_quantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
       PTQ_CHECK(!r || (r->scalar_type() == X.scalar_type() && r->dim() == 2 && r->size(0) == t && r->size(1) == n && r->stride(1) == 1));
     ptq_dtype dt;
     if (!dtype_of(X, dt)) return PTQ_ERR_DTYPE;
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_rmsnorm_quantize(ptr(X), dt, X.stride(0), t, n, ptr(residual), residual ? residual->stride(0) : 0, ptr(out),
                                   out ? out->stride(0) : 0, ptr(gamma), eps, normalize, as<int8_t>(codes), codes.stride(0),
@@ -150,7 +148,7 @@ PyObject* int8_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return status_of([&]() -> ptq_status {
     const Tensor &A = tensor(a[0]), &as_ = tensor(a[1]), &W = tensor(a[2]), &ws_ = tensor(a[3]), &O = tensor(a[4]);
     const Tensor *bias = optional(a[5]), *ws = optional(a[6]);
-    here(A, as_, W, ws_, O, bias, ws);
+    const ptq_stream s = stream_of(A, as_, W, ws_, O, bias, ws);
     PTQ_CHECK(A.scalar_type() == at::kChar && A.dim() == 2 && A.stride(1) == 1);
     PTQ_CHECK(W.scalar_type() == at::kChar && W.dim() == 2 && W.stride(1) == 1 && W.size(1) == A.size(1));
     const int64_t t = A.size(0), n = A.size(1), m = W.size(0);
@@ -162,7 +160,6 @@ PyObject* int8_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
     ptq_dtype dt;
     if (!dtype_of(O, dt)) return PTQ_ERR_DTYPE;
     const Workspace w(ws, A, PTQ_OP_INT8_LINEAR, m, n, t, 0);
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_int8_linear(as<int8_t>(A), A.stride(0), as<float>(as_), t, as<int8_t>(W), W.stride(0), as<float>(ws_), m, n,
                              static_cast<const float*>(ptr(bias)), ptr(O), dt, O.stride(0), w.at, w.bytes, s);
@@ -191,7 +188,7 @@ PyObject* kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return status_of([&]() -> ptq_status {
     const Tensor &K = tensor(a[0]), &V = tensor(a[1]), &slots = tensor(a[2]), &codes = tensor(a[4]), &scales = tensor(a[5]), &zeros = tensor(a[6]);
     const int64_t bits = whole(a[3]);
-    here(K, V, slots, codes, scales, zeros);
+    const ptq_stream s = stream_of(K, V, slots, codes, scales, zeros);
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && V.scalar_type() == K.scalar_type());
     const int64_t t = K.size(0), heads = K.size(1), d = K.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -199,7 +196,6 @@ PyObject* kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
     PTQ_CHECK(whole_numbers(slots, t));
     ptq_dtype dt;
     if (!dtype_of(K, dt)) return PTQ_ERR_DTYPE;
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_kv_cache_write(ptr(K), K.stride(0), K.stride(1), ptr(V), V.stride(0), V.stride(1), dt, t, heads, d, as<int32_t>(slots), (int)bits,
                                 as<uint8_t>(codes), as<float>(scales), as<uint8_t>(zeros), c.pages, c.page, s);
@@ -214,7 +210,7 @@ PyObject* kv_cache_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor &codes = tensor(a[0]), &scales = tensor(a[1]), &zeros = tensor(a[2]), &table = tensor(a[4]), &cu = tensor(a[5]),
                  &K = tensor(a[7]), &V = tensor(a[8]);
     const int64_t bits = whole(a[3]), max_kv = whole(a[6]);
-    here(codes, scales, zeros, table, cu, K, V);
+    const ptq_stream s = stream_of(codes, scales, zeros, table, cu, K, V);
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && V.scalar_type() == K.scalar_type());
     const int64_t rows = K.size(0), heads = K.size(1), d = K.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -224,7 +220,6 @@ PyObject* kv_cache_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
     PTQ_CHECK(whole_numbers(cu, b + 1));
     ptq_dtype dt;
     if (!dtype_of(K, dt)) return PTQ_ERR_DTYPE;
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_kv_cache_read(as<uint8_t>(codes), as<float>(scales), as<uint8_t>(zeros), c.pages, c.page, heads, d, (int)bits, as<int32_t>(table),
                                table.size(1), b, as<int32_t>(cu), rows, max_kv, ptr(K), K.stride(0), K.stride(1), ptr(V), V.stride(0),
@@ -243,7 +238,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const int64_t max_q = whole(a[2]), bits = whole(a[6]), max_kv = whole(a[9]), window = whole(a[13]);
     const double scale = number(a[10]);
     const int causal = truth(a[12]);
-    here(Q, cu, codes, scales, zeros, table, lens, O, ws);
+    const ptq_stream s = stream_of(Q, cu, codes, scales, zeros, table, lens, O, ws);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     const int64_t t = Q.size(0), hq = Q.size(1), d = Q.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -255,7 +250,6 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     ptq_dtype dt;
     if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
     const Workspace w(ws, Q, PTQ_OP_PAGED_ATTENTION, hq, d, t, max_kv);
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_paged_attention(ptr(Q), dt, Q.stride(0), Q.stride(1), t, hq, d, as<int32_t>(cu), b, max_q, as<uint8_t>(codes), as<float>(scales),
                                  as<uint8_t>(zeros), c.pages, c.page, c.heads, (int)bits, as<int32_t>(table), table.size(1), as<int32_t>(lens),
@@ -278,11 +272,10 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const Tensor &X = tensor(a[0]), &positions = tensor(a[1]), &freq = tensor(a[2]), &Y = tensor(a[3]);
     const double scale = number(a[4]);
     const int interleaved = truth(a[5]);
-    here(X, positions, freq, Y);
+    const ptq_stream s = stream_of(X, positions, freq, Y);
     rotary_ok(X, Y, positions, freq);
     ptq_dtype dt;
     if (!dtype_of(X, dt)) return PTQ_ERR_DTYPE;
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_rotary(ptr(X), X.stride(0), X.stride(1), dt, X.size(0), X.size(1), X.size(2), as<int32_t>(positions), as<double>(freq), 2 * freq.numel(),
                         scale, interleaved, ptr(Y), Y.stride(0), Y.stride(1), s);
@@ -299,7 +292,7 @@ PyObject* rotary_kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count)
     const int64_t bits = whole(a[6]);
     const double scale = number(a[11]);
     const int interleaved = truth(a[12]);
-    here(Q, K, V, positions, freq, slots, codes, scales, zeros, O);
+    const ptq_stream s = stream_of(Q, K, V, positions, freq, slots, codes, scales, zeros, O);
     rotary_ok(Q, O, positions, freq);
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.sizes() == K.sizes() && V.stride(2) == 1 && K.scalar_type() == Q.scalar_type() && V.scalar_type() == Q.scalar_type());
     const int64_t t = K.size(0), heads = K.size(1), d = K.size(2);
@@ -309,7 +302,6 @@ PyObject* rotary_kv_cache_write(PyObject*, PyObject* const* a, Py_ssize_t count)
     PTQ_CHECK(whole_numbers(slots, t));
     ptq_dtype dt;
     if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_rotary_kv_cache_write(ptr(Q), Q.stride(0), Q.stride(1), Q.size(1), ptr(K), K.stride(0), K.stride(1), ptr(V), V.stride(0), V.stride(1), dt,
                                        t, heads, d, as<int32_t>(positions), as<double>(freq), 2 * freq.numel(), scale, interleaved, as<int32_t>(slots),
@@ -325,13 +317,12 @@ PyObject* kv_cache_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t count) {
   return status_of([&]() -> ptq_status {
     const Tensor &fc = tensor(a[0]), &fs = tensor(a[1]), &fz = tensor(a[2]), &source = tensor(a[3]), &codes = tensor(a[4]), &scales = tensor(a[5]),
                  &zeros = tensor(a[6]), &target = tensor(a[7]);
-    here(fc, fs, fz, source, codes, scales, zeros, target);
+    const ptq_stream s = stream_of(fc, fs, fz, source, codes, scales, zeros, target);
     PTQ_CHECK(fc.dim() == 5 && codes.dim() == 5 && fc.size(4) == codes.size(4));
     const Cache from = cache_of(fc, fs, fz, 8, fc.size(4)), to = cache_of(codes, scales, zeros, 8, codes.size(4));
     PTQ_CHECK(from.heads == to.heads && from.page == to.page);
     const int64_t n = source.numel();
     PTQ_CHECK(whole_numbers(source, n) && whole_numbers(target, n));
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_kv_cache_copy_pages(as<uint8_t>(fc), as<float>(fs), as<uint8_t>(fz), from.pages, as<uint8_t>(codes), as<float>(scales), as<uint8_t>(zeros),
                                      to.pages, to.page, to.heads, codes.size(4), as<int32_t>(source), as<int32_t>(target), n, s);
@@ -347,7 +338,7 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     const int64_t max_n = whole(a[4]), window = whole(a[8]);
     const double scale = number(a[5]);
     const int causal = truth(a[7]);
-    here(Q, K, V, cu, O);
+    const ptq_stream s = stream_of(Q, K, V, cu, O);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     PTQ_CHECK(K.dim() == 3 && K.stride(2) == 1 && V.stride(2) == 1 && V.sizes() == K.sizes() && K.scalar_type() == Q.scalar_type() &&
               V.scalar_type() == Q.scalar_type());
@@ -355,7 +346,6 @@ PyObject* prompt_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
     PTQ_CHECK(cu.scalar_type() == at::kInt && cu.is_contiguous() && cu.numel() >= 1);
     ptq_dtype dt;
     if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_prompt_attention(ptr(Q), Q.stride(0), Q.stride(1), ptr(K), K.stride(0), K.stride(1), ptr(V), V.stride(0), V.stride(1), dt, Q.size(0),
                                   Q.size(1), K.size(1), Q.size(2), as<int32_t>(cu), cu.numel() - 1, max_n, scale, causal, window, ptr(O), O.stride(0),
@@ -374,7 +364,7 @@ PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t count
     const int64_t max_q = whole(a[2]), bits = whole(a[6]), max_kv = whole(a[9]), max_shared = whole(a[12]);
     const double scale = number(a[13]);
     const int causal = truth(a[15]);
-    here(Q, cu, codes, scales, zeros, table, lens, cu_groups, shared, O, ws);
+    const ptq_stream s = stream_of(Q, cu, codes, scales, zeros, table, lens, cu_groups, shared, O, ws);
     PTQ_CHECK(Q.dim() == 3 && Q.stride(2) == 1 && O.stride(2) == 1 && O.sizes() == Q.sizes() && O.scalar_type() == Q.scalar_type());
     const int64_t t = Q.size(0), hq = Q.size(1), d = Q.size(2);
     const Cache c = cache_of(codes, scales, zeros, bits, d);
@@ -387,7 +377,6 @@ PyObject* paged_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t count
     ptq_dtype dt;
     if (!dtype_of(Q, dt)) return PTQ_ERR_DTYPE;
     const Workspace w(ws, Q, PTQ_OP_SHARED_ATTENTION, hq, d, t, max_kv);
-    const ptq_stream s = stream();
     return released([&] {
       return ptq_paged_attention_shared(ptr(Q), dt, Q.stride(0), Q.stride(1), t, hq, d, as<int32_t>(cu), b, max_q, as<uint8_t>(codes), as<float>(scales),
                                         as<uint8_t>(zeros), c.pages, c.page, c.heads, (int)bits, as<int32_t>(table), table.size(1), as<int32_t>(lens),
