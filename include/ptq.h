@@ -525,7 +525,8 @@ ptq_status ptq_kv_cache_read(const uint8_t* codes, const float* scales, const ui
  * tokens times group, to a key head) the values are too, and the sum is of the rounded weights.  With fewer rows the matrix unit adds the products of
  * 4-bit values to within 2^-17 of the largest.  The largest is that of the keys that the row sees: a key that is not seen has no effect, not in
  * one bit, whatever its scales hold; one that is seen and whose scales are NaN makes the row NaN.  Values may be of any size; scales outside
- * 2^-18 to 2^4 (4 bits: 2^8) in chunks, and outside 2^-40 to 2^40 otherwise, take up to twice the time.
+ * 2^-18 to 2^4 (4 bits: 2^8) in chunks, and outside 2^-40 to 2^40 otherwise, take up to twice the time.  In chunks |softmax_scale q . k| beyond 2^30 may
+ * make the row NaN (scores and the maximum that they are taken from are float32, whole multiples of 2^7 there).
  *
  * Q, O      token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_BF16.  O is not Q.
  * cu_q, kv_lens   b + 1 and b int32 on the device.  A sequence that would begin before token 0 or end past t is left out; keys past
@@ -609,8 +610,9 @@ ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_
  *
  * Scores, running maxima and sums are float32; weights are rounded to bfloat16 (2^-8 of each), and the sum is of the rounded ones.  A token that is not
  * seen has no effect, whatever it holds; one that is seen and is not finite makes what it reaches not finite.  Values may be of any size; not finite, they take up
- * to twice the time, and from 2^95 on, where sums may leave float32's range, up to three times.  Scores are float32: |softmax_scale
- * q . k| beyond 1e38 makes the row NaN or leaves keys out.
+ * to twice the time, and from 2^95 on, where sums may leave float32's range, up to three times.  Scores are float32, and so is the maximum that they are
+ * taken from: |softmax_scale q . k| beyond 2^30, where both are whole multiples of 2^7, may make the row NaN, and q . k that
+ * float32 does not hold does that or leaves keys out.
  *
  * Q, K, V, O  token i, head h at i * token stride + h * head stride (elements, >= 0), d values side by side; PTQ_BF16.  O may be Q with the same
  *           strides; otherwise it overlaps none of the others.  K and V whose bases lie on 16 bytes and whose strides are multiples
@@ -629,7 +631,7 @@ ptq_status ptq_prompt_attention(const void* Q, int64_t q_token, int64_t q_head, 
 /*
  * ptq_paged_attention for sequences that share prefixes (forks of a sequence, requests behind one long text): the keys of a prefix are read and
  * multiplied once for all queries behind it.  The result is ptq_paged_attention's with the same arguments and window 0, but for how it is rounded: a
- * prefix is gone through as chunks are, with their roundings, where more than one sequence has it, no key head has more than 16 rows (tokens
+ * prefix is gone through as chunks are, with their roundings and scores up to 2^30, where more than one sequence has it, no key head has more than 16 rows (tokens
  * times group) of a sequence, and the bounds (b, groups, max_shared, max_kv) say that it saves time: prefixes of more than 4 MB of codes and some eight
  * sequences behind each.  Otherwise the call does what ptq_paged_attention does.
  *

@@ -79,6 +79,28 @@ def test_large_values_and_scores_that_grow():
     held(attend(Q, K, V, [n], scale=1.0), *reference(Q, K, V, [n], 1.0, True, 0))
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("exponent", [4, 12, 17, 20, 22])
+@pytest.mark.parametrize("scale", [1.0, -1.0, 0.75])
+def test_scores_up_to_2_30(d, exponent, scale):
+    """Scores are whole multiples of 2^exponent up to 256 of them, exactly: a row's mean is that of the tokens with the highest one, whose weights are all
+    the same number.  The rest: n others of no more than exp(-|scale| 2^exponent) of it, twice the largest value off; n additions of float32, 2^-14
+    of the values' mean size; the output's own rounding, 2^-8."""
+    n, g = 700, torch.Generator(device="cuda").manual_seed(exponent)
+    Q, K, V = (torch.zeros(n, h, d, dtype=BF16, device="cuda") for h in (2, 1, 1))
+    Q[:, :, 5] = 2.0 ** exponent
+    k = torch.randint(-256, 257, (n,), device="cuda", generator=g)
+    K[:, 0, 5] = k.to(BF16)
+    V[:] = rand(n, 1, d, seed=exponent)
+    got = attend(Q, K, V, [n], scale=scale).double()
+    s = (math.copysign(1, scale) * k).double()[None].expand(n, n).tril() + torch.full((n, n), -1e3, device="cuda").double().triu(1)
+    top = (s == s.amax(dim=1, keepdim=True)).double()
+    mean = lambda v: (top @ v / top.sum(dim=1, keepdim=True))[:, None]
+    want, size = mean(V[:, 0].double()), mean(V[:, 0].double().abs())
+    others = n * math.exp(-abs(scale) * 2.0 ** exponent) * 2 * V.double().abs().max()
+    assert bool(((got - want).abs() <= (2.0 ** -8 + 2.0 ** -15) * want.abs() + 2.0 ** -14 * size + others).all())
+
+
 def test_keys_that_are_not_numbers_beside_large_values():
     n, d = 200, 64
     Q, K, V = (x.contiguous() for x in qkv([n], 1, 1, d, seed=6))
