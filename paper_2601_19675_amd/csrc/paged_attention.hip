@@ -799,9 +799,11 @@ namespace {
 // Whether prefixes gone through apart take less time than every sequence's whole way, in us as measured and by what the bounds say.  Every sequence by itself: 15, and
 // 0.135 to a megabyte of codes (pages that several name are in the caches).  Apart: 25, 1.7e-4 for a key of a prefix, a key head and a tile of 256 rows of 128 channels,
 // 0.25 for each of a row's parts beyond 32, and what is behind the prefixes as before.  A prefix that a die's L2 holds (4 MB) is read from there by all
-// sequences as fast.  32 heads of 128 channels over 8, 8 bits, apart | by itself: 8 behind 1000 keys 27 | 18, 64 41 | 28; 4 behind 8192 35 | 27, 8
-// 35 | 36, 16 37 | 55; 4 behind 32768 72 | 54, 8 72 | 90, 64 87 | 493.  16 heads over 1: 16 behind 32768 94 | 38.  32 over 32: 8 behind 2048 35 | 31, 12 39 | 47.  The numbers
-// are fitted to these and their like; the one miss seen is 16 in two groups behind 8192 with up to 7800 keys of their own, 71 | 66.
+// sequences as fast.  32 heads of 128 channels over 8, 8 bits, apart | by itself: 8 behind 1000 keys 27 | 18, 64 41 | 28; 4 behind 8192 32 | 27, 8
+// 32 | 36, 16 33 | 54; 4 behind 32768 52 | 53, 8 52 | 88, 64 80 | 498.  16 heads over 1: 16 behind 32768 94 | 38.  32 over 32: 8 behind 2048 35 | 31, 12 39 | 47.  The
+// numbers are fitted to caches some of whose scales lie below 2^-18 (apart: 4 or 8 behind 32768 73, 64 116), and cautious elsewhere.  Misses seen: 16 in two
+// groups behind 8192 with up to 7800 keys of their own 71 | 66; 256 channels, 16 heads over 4, 64 behind 2048 111 | 61, 16 behind 8192 100 | 63, both gone
+// through apart; 4 bits, 8 behind 32768 50 | 66, 16 behind 8192 32 | 41, neither; 2 of 64 of 8400 keys behind 8192 227 | 198, apart, as if all were behind it.
 bool prefixes_pay(const AttendArgs& a, int bits) {
   const double key = (double)a.c.heads * a.d * 2 * bits / 8 * 1e-6;   // megabytes
   const double tiles = (double)ceil_div((int64_t)a.t * a.group, 256) + a.groups - 1, prefix = a.max_shared;

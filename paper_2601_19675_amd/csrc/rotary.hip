@@ -9,7 +9,7 @@
 // is rounded to a key's type, and decides its codes, is the exact value but for 2^-50.
 //
 // 16384 tokens, 40 heads of 128 bfloat16 channels (336 MB): 68 to 70 us, 4.9 TB/s, the rate of a large copy; 16 tokens 3.5 to 3.7 us, all latency.  Four
-// prompts of up to 4096 tokens, 32 heads of each kind, into 4 bits (401 MB): 118 us in a kernel trace, 3.4 TB/s, some way from a copy.  (Eight pairs to a
+// prompts of up to 4096 tokens, 32 heads of each kind, into 4 bits (401 MB): 111 to 118 us in kernel traces, 3.4 to 3.6 TB/s, some way from a copy.  (Eight pairs to a
 // lane take 142 to 181 registers and leave two or three waves to a SIMD: 78, 4.8 and, traced, 137 us.)
 #include <algorithm>
 #include <cmath>
@@ -103,7 +103,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   rotary_rows<DT, LANES>(a, blockIdx.x / a.slices, blockIdx.x % a.slices);
 }
 
-// Any widths: a thread has one pair, or two channels that stay as they are, of a token's heads.
+// Any widths: a thread has one pair, or two channels that stay as they are, of a token's heads.  16384 tokens, 40 heads of bfloat16: 96 channels of
+// which 24 turn 78 us (252 MB, 3.2 TB/s), 80 of which 20 turn 74; in whole runs, with 96 and 80 turning, 42 and 39.
 template <int DT>
 __global__ __launch_bounds__(256) void rotary_any_kernel(RotaryArgs a, int64_t first_tile) {
   using ST = typename StoredType<DT>::type;
