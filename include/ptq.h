@@ -569,7 +569,7 @@ ptq_status ptq_rotary(const void* X, int64_t x_token, int64_t x_head, ptq_dtype 
  *   PTQ_ROTARY_TURNS    f_j (k + (1 - k) / factor), k = clamp((turns_j - slow) / (fast - slow), 0, 1), turns_j = context f_j / (2 pi): pairs that
  *                       turn more than `fast` times over `context` tokens stay, those that turn less than `slow` times have f / factor
  * PTQ_ROTARY_PLAIN leaves them, and ignores what follows it.  (The magnitude that some of these go with is ptq_rotary's scale.)
- * rot even, >= 2; base > 0; factor > 0; with TURNS context > 0, fast > slow; all finite.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE.
+ * rot even, 2 to 65536; base > 0; factor > 0; with TURNS context > 0, fast > slow; all finite.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE.
  */
 typedef enum { PTQ_ROTARY_PLAIN = 0, PTQ_ROTARY_LINEAR = 1, PTQ_ROTARY_BASE = 2, PTQ_ROTARY_TURNS = 3 } ptq_rotary_scaling;
 ptq_status ptq_rotary_frequencies(double* freq, int64_t rot, double base, ptq_rotary_scaling scaling, double factor, double context,
@@ -618,7 +618,7 @@ ptq_status ptq_kv_cache_copy_pages(const uint8_t* from_codes, const float* from_
  *           strides; otherwise it overlaps none of the others.  K and V whose bases lie on 16 bytes and whose strides are multiples
  *           of 8 and below 2^24 take the shorter way.
  * cu        b + 1 int32 on the device.  A prompt that would begin before token 0 or end past t is left out, and so are tokens from max_n of a prompt on.
- * max_n     no prompt is longer.     b <= 65535; t <= 2^24; max_n hq / hkv <= 2^27.
+ * max_n     no prompt is longer; a bound far above them costs time (1.5 ns for each b max_n hq / 128).     b <= 65535; t <= 2^24; max_n hq / hkv <= 2^27.
  * hq        a multiple of hkv, at most 65535.     d  a multiple of 16, at most 256.
  * softmax_scale  up to 2e38 either way.     window  >= 0.
  * No workspace.  Errors: PTQ_ERR_ARG, PTQ_ERR_SHAPE, PTQ_ERR_DTYPE.
